@@ -1,0 +1,694 @@
+"""The 8-bit cache's operators as timed cases, each beside its plain form.
+
+A cache held in 8 bits is a paged pool of E4M3 codes with one E8M0 scale byte e, standing for 2^(e - 127), per
+block of slots, KV head, layer and tensor.  Four kinds of passes:
+
+  store    chunks of bf16 or fp32 keys and values re-rotated, quantised and spliced into the pool
+  attend   causal (and windowed) GQA attention of bf16 queries over the pool
+  fork     branches of a sampling step: the old branches' pages are freed, the parents forked again
+  compact  the used pages of a fragmented pool moved to its front
+
+  listed()              the fixed cases
+  draw(rng)             one more case of the same ranges
+  prepare(case, seed)   inputs on the GPU, made from the seed alone
+  run(state)            one pass: plain torch, or with `own` the library's calls
+  work(case)            bytes and flops the pass cannot do without
+  exact(case, seed)     the same outputs from the definitions in 64 bits
+"""
+import math
+import random
+
+import torch
+
+own = False
+
+E4M3, E8M0 = torch.float8_e4m3fn, torch.float8_e8m0fnu
+TYPES = {"bf16": torch.bfloat16, "f32": torch.float32, "e4m3": E4M3}
+BYTES = {"bf16": 2, "f32": 4, "e4m3": 1}
+
+
+# ---- the cases ------------------------------------------------------------------
+
+def _store(dtype, layers, kv_heads, head_dim, seqs, chunks, live_min, live_max, page, block, theta, style="half",
+           turn=True):
+    """`seqs` sequences of live_min..live_max tokens, each continued by the library's chunks (their lengths as text)
+    in an order of its own; turn: the chunks come from other positions than they go to."""
+    return dict(kind="store", dtype=dtype, layers=layers, kv_heads=kv_heads, head_dim=head_dim, seqs=seqs,
+                chunks=",".join(str(n) for n in chunks), live_min=live_min, live_max=live_max, page=page, block=block,
+                theta=theta, style=style, turn=turn)
+
+
+def _attend(layers, seqs, heads, kv_heads, head_dim, queries, kv_min, kv_max, page, block, window=0, ragged=False):
+    """The last `queries` tokens (ragged: up to as many) of each of `seqs` caches of kv_min..kv_max slots."""
+    return dict(kind="attend", layers=layers, seqs=seqs, heads=heads, kv_heads=kv_heads, head_dim=head_dim,
+                queries=queries, kv_min=kv_min, kv_max=kv_max, page=page, block=block, window=window, ragged=ragged)
+
+
+def _fork(dtype, layers, kv_heads, head_dim, parents, ways, len_min, len_max, page, block):
+    """`parents` sequences of len_min..len_max tokens with `ways` branches each."""
+    return dict(kind="fork", dtype=dtype, layers=layers, kv_heads=kv_heads, head_dim=head_dim, parents=parents, ways=ways,
+                len_min=len_min, len_max=len_max, page=page, block=block)
+
+
+def _compact(dtype, layers, kv_heads, head_dim, pages, used, moves, seqs, page, block):
+    """A pool of `pages` pages, `used` of them in use by `seqs` sequences, `moves` of those behind the first `used`."""
+    return dict(kind="compact", dtype=dtype, layers=layers, kv_heads=kv_heads, head_dim=head_dim, pages=pages, used=used,
+                moves=moves, seqs=seqs, page=page, block=block)
+
+
+def listed():
+    def named(name, case):
+        return dict(case, name=name)
+
+    return [
+        # Token-by-token generation: one new token for each of 64 contexts, one layer of the 8B shape, as a model
+        # issues it.  Almost every block keeps earlier tokens.
+        named("store_decode_step", _store("bf16", 1, 8, 128, 64, (1,), 1000, 9000, 64, 32, 500000.0, turn=False)),
+        # A 4096-token skill moved into every layer of an 8B-class cache.
+        named("store_skill", _store("bf16", 32, 8, 128, 1, (4096,), 2000, 2000, 64, 64, 500000.0)),
+        # Many users, one library: 16 contexts continued by three skills of odd lengths back to back, so that blocks
+        # hold the end of one skill and the beginning of the next (a pipeline stage of 4 layers).
+        named("store_compose", _store("bf16", 4, 8, 128, 16, (700, 1301, 2051), 20, 400, 128, 128, 500000.0)),
+        # A short fp32 chunk into a small model's cache.
+        named("store_f32_chunk", _store("f32", 1, 2, 64, 1, (301,), 77, 77, 32, 32, 10000.0, style="interleaved")),
+        # The smallest attention call: one query over a short cache of a small GQA model.
+        named("attend_one_short", _attend(1, 1, 14, 2, 64, 1, 500, 500, 32, 32)),
+        # Token-by-token generation over 16 composed contexts, one layer of the 8B shape.
+        named("attend_decode", _attend(1, 16, 32, 8, 128, 1, 8448, 12544, 64, 64)),
+        # A 64-token suffix over a spliced 8k context, one layer.
+        named("attend_suffix", _attend(1, 1, 32, 8, 128, 64, 8256, 8256, 64, 32)),
+        # A long prefill: 1024 suffix tokens over a 49k spliced context, one layer.
+        named("attend_prefill", _attend(1, 1, 28, 4, 128, 1024, 50176, 50176, 128, 128)),
+        # A few branches of one context in a small model.
+        named("fork_few", _fork("e4m3", 2, 2, 64, 1, 4, 333, 333, 32, 32)),
+        # Best-of-8 sampling of 16 contexts: the branches are dropped and forked again from their parents.
+        named("fork_sampling", _fork("e4m3", 8, 8, 128, 16, 8, 1000, 4000, 64, 64)),
+        # A small pool after a few requests have ended.
+        named("compact_small", _compact("e4m3", 2, 2, 64, 97, 60, 11, 7, 32, 32)),
+        # A fragmented bf16 pool before it is shrunk.
+        named("compact_pool", _compact("bf16", 4, 8, 128, 1000, 700, 220, 24, 64, 64)),
+    ]
+
+
+MAX_BYTES = 8.0e8    # about the skill's
+MAX_FLOPS = 7.0e11   # about the long prefill's
+
+
+def _log_int(rng, lo, hi):
+    return max(lo, min(hi, int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))))
+
+
+def _draw_paging(rng):
+    page = rng.choice([32, 64, 64, 128, 256])
+    return page, rng.choice([b for b in (32, 64, 128) if b <= page])
+
+
+def _draw_store(rng):
+    page, block = _draw_paging(rng)
+    decode = rng.random() < 0.3
+    chunks = (1,) if decode else tuple(_log_int(rng, 1, 6000) for _ in range(rng.randint(1, 4)))
+    live = rng.choice([0, _log_int(rng, 1, 9000)])
+    return _store(rng.choice(["bf16", "bf16", "f32"]), _log_int(rng, 1, 32), rng.choice([1, 2, 4, 8]), rng.choice([64, 128]),
+                  _log_int(rng, 1, 128) if decode else _log_int(rng, 1, 16), chunks, live, live + rng.randint(0, 500), page, block,
+                  rng.choice([1e4, 5e5, 1e6]), rng.choice(["half", "half", "interleaved"]), not decode)
+
+
+def _draw_attend(rng):
+    page, block = _draw_paging(rng)
+    decode = rng.random() < 0.4
+    seqs = _log_int(rng, 1, 64) if decode else rng.choice([1, 1, 2, 5, 16])
+    heads, kv_heads, d = rng.choice([(32, 8, 128), (28, 4, 128), (14, 2, 64), (8, 8, 128), (16, 2, 64)])
+    kv_max = _log_int(rng, 32, 50176)
+    kv_min = rng.randint(max(1, kv_max // 2), kv_max)
+    queries = 1 if decode else min(kv_min, _log_int(rng, 2, 1024))
+    window = rng.choice([1000, 4096]) if rng.random() < 0.25 else 0
+    return _attend(rng.choice([1, 1, 2]), seqs, heads, kv_heads, d, queries, kv_min, kv_max, page, block, window,
+                   not decode and rng.random() < 0.5)
+
+
+def _draw_fork(rng):
+    page, block = _draw_paging(rng)
+    length = _log_int(rng, 40, 4000)
+    return _fork(rng.choice(["e4m3", "e4m3", "bf16"]), _log_int(rng, 1, 8), rng.choice([2, 4, 8]), rng.choice([64, 128]),
+                 _log_int(rng, 1, 16), rng.randint(1, 8), length, length + rng.randint(0, length), page, block)
+
+
+def _draw_compact(rng):
+    page, block = _draw_paging(rng)
+    pages = _log_int(rng, 16, 1000)
+    used = rng.randint(pages // 8 + 1, pages - 1)
+    moves = rng.randint(0, min(used, pages - used))
+    return _compact(rng.choice(["e4m3", "e4m3", "bf16"]), _log_int(rng, 1, 4), rng.choice([2, 4, 8]), rng.choice([64, 128]),
+                    pages, used, moves, rng.randint(1, min(24, used)), page, block)
+
+
+MAX_POOL_BYTES = 1.2e9   # of one tensor of a drawn case
+
+
+def draw(rng):
+    makers = [_draw_store, _draw_attend, _draw_attend, rng.choice([_draw_fork, _draw_compact])]
+    make = rng.choice(makers)
+    while True:
+        case = make(rng)
+        w = work(case)
+        if w["bytes"] <= MAX_BYTES and w["flops"] <= MAX_FLOPS and _pool_bytes(case) <= MAX_POOL_BYTES:
+            return case
+
+
+# ---- geometry (fixed by the case, not by the seed) --------------------------------
+
+def _rng(case):
+    return random.Random(sum((i + 1) * int(v) for i, v in enumerate(v for v in case.values() if isinstance(v, int))))
+
+
+def _plan(case):
+    """Segments of a store (source slot, sequence, tokens, source position, destination position), the sequences'
+    lengths before it and the source's slots."""
+    chunks = [int(n) for n in case["chunks"].split(",")]
+    r = _rng(case)
+    live = [r.randint(case["live_min"], case["live_max"]) for _ in range(case["seqs"])]
+    if chunks == [1]:   # every sequence has a new token of its own
+        return [(s, s, 1, n + 100 * case["turn"], n) for s, n in enumerate(live)], live, len(live)
+    first = [sum(chunks[:i]) for i in range(len(chunks))]
+    at = [r.randint(0, 2048) for _ in chunks]
+    segs = []
+    for s, n in enumerate(live):
+        order = list(range(len(chunks)))
+        r.shuffle(order)
+        pos = n
+        for c in order:
+            segs.append((first[c], s, chunks[c], at[c] if case["turn"] else pos, pos))
+            pos += chunks[c]
+    return segs, live, sum(chunks)
+
+
+def _lengths(case):
+    """(queries, cache length) of the sequences of an attention case."""
+    r = _rng(case)
+    out = []
+    for _ in range(case["seqs"]):
+        kv = r.randint(case["kv_min"], case["kv_max"])
+        out.append((r.randint(1, case["queries"]) if case["ragged"] else case["queries"], kv))
+    return out
+
+
+def _parents(case):
+    r = _rng(case)
+    return [r.randint(case["len_min"], case["len_max"]) for _ in range(case["parents"])]
+
+
+def _shape(case):
+    """(pages of the pool, block-table shape) of a case."""
+    page = case["page"]
+    if case["kind"] == "store":
+        _, live, _ = _plan(case)
+        per = -(-(max(live) + sum(int(n) for n in case["chunks"].split(","))) // page)
+        return per * case["seqs"] + 8, (case["seqs"], per)
+    if case["kind"] == "attend":
+        per = max(-(-kv // page) for _, kv in _lengths(case))
+        return per * case["seqs"] + 8, (case["seqs"], per)
+    if case["kind"] == "fork":
+        lens = _parents(case)
+        own_pages = sum(-(-n // page) for n in lens)
+        return own_pages + 2 * len(lens) * case["ways"] + 8, (len(lens) * (1 + case["ways"]), -(-max(lens) // page) + 2)
+    return case["pages"], (case["seqs"], -(-case["used"] // case["seqs"]) + 3)
+
+
+def _pool_bytes(case):
+    pages = _shape(case)[0]
+    return pages * case["page"] * case["layers"] * case["kv_heads"] * case["head_dim"] * BYTES[_pool_type(case)]
+
+
+def _pool_type(case):
+    return case["dtype"] if case["kind"] in ("fork", "compact") else "e4m3"
+
+
+# ---- inputs -------------------------------------------------------------------------
+
+class _Random:
+    """Draws of one seeded generator, in order, on the GPU."""
+
+    def __init__(self, seed):
+        self.g = torch.Generator(device="cuda")
+        self.g.manual_seed(seed)
+
+    def normal(self, shape, dtype, gain=1.0):
+        return torch.empty(shape, dtype=dtype, device="cuda").normal_(0.0, gain, generator=self.g)
+
+    def codes(self, shape):
+        """What N(0,1) values of a block with scale 2^-6 are held as."""
+        return self.normal(shape, torch.bfloat16, 64.0).clamp_(-448, 448).to(E4M3)
+
+    def exponents(self, shape):
+        return torch.randint(120, 123, shape, dtype=torch.uint8, device="cuda", generator=self.g)
+
+    def permutation(self, n):
+        return torch.randperm(n, generator=self.g, device="cuda")
+
+
+def _ints(values, dtype=torch.int32):
+    return torch.tensor(values, dtype=dtype, device="cuda")
+
+
+def _pool(case, n, pages):
+    shape = (case["layers"], pages, case["page"], case["kv_heads"], case["head_dim"])
+    if _pool_type(case) != "e4m3":
+        return dict(k=n.normal(shape, TYPES[case["dtype"]]), v=n.normal(shape, TYPES[case["dtype"]]))
+    scale = (case["layers"], pages, case["page"] // case["block"], case["kv_heads"])
+    return dict(k=n.codes(shape), v=n.codes(shape), ks=n.exponents(scale), vs=n.exponents(scale))
+
+
+def _inputs(case, seed):
+    n = _Random(seed)
+    L, H, d, page = case["layers"], case["kv_heads"], case["head_dim"], case["page"]
+    pages, table = _shape(case)
+    s = _pool(case, n, pages)
+    order = n.permutation(pages).to(torch.int32)
+    if case["kind"] in ("store", "attend"):
+        s["table"] = order[:table[0] * table[1]].view(table).contiguous()
+    if case["kind"] == "store":
+        segs, live, slots = _plan(case)
+        s["src_k"], s["src_v"] = (n.normal((L, H, slots, d), TYPES[case["dtype"]]) for _ in "kv")
+        s["kv_len"] = _ints(live)
+        tokens = [torch.tensor([[seq, src0 + i, dst0 + i, dst0 - pos0] for i in range(t)])
+                  for src0, seq, t, pos0, dst0 in segs]
+        s["seq"], s["src"], s["dst"], s["delta"] = torch.cat(tokens).to("cuda").unbind(1)
+    elif case["kind"] == "attend":
+        lens = _lengths(case)
+        s["q"] = n.normal((L, sum(q for q, _ in lens), case["heads"], d), torch.bfloat16, 2.0)
+        s["q_pos"] = _ints([kv - q + i for q, kv in lens for i in range(q)])
+        s["kv_len"] = _ints([kv for _, kv in lens])
+        s["cu_q"] = _ints([0] + torch.tensor([q for q, _ in lens]).cumsum(0).tolist())
+        s["out"] = torch.zeros_like(s["q"])
+    elif case["kind"] == "fork":
+        # The branches of the step before share their parent's whole pages and hold a last page of their own.
+        lens, ways, ids = _parents(case), case["ways"], order.tolist()
+        rows = torch.full(table, -1, dtype=torch.int32)
+        ref = torch.zeros(pages, dtype=torch.int32)
+        for p, length in enumerate(lens):
+            for e in range(-(-length // page)):
+                rows[p, e] = ids.pop()
+                ref[rows[p, e]] = 1 + ways * (e < length // page)
+        for b in range(len(lens) * ways):
+            length = lens[b // ways]
+            rows[len(lens) + b, :length // page] = rows[b // ways, :length // page]
+            if length % page:
+                rows[len(lens) + b, length // page] = ids.pop()
+                ref[rows[len(lens) + b, length // page]] = 1
+        s["table"], s["ref"] = rows.cuda(), ref.cuda()
+        s["parent"] = _ints([b // ways for b in range(len(lens) * ways)])
+        s["child"] = _ints([len(lens) + b for b in range(len(lens) * ways)])
+        s["length"] = _ints([lens[b // ways] for b in range(len(lens) * ways)])
+    else:
+        used, moves = case["used"], case["moves"]
+        front, back = n.permutation(used)[:used - moves], used + n.permutation(pages - used)[:moves]
+        ids = torch.cat([front, back])[n.permutation(used)].to(torch.int32)
+        s["ref"] = torch.zeros(pages, dtype=torch.int32, device="cuda")
+        s["table"] = torch.full(table, -1, dtype=torch.int32, device="cuda")
+        where = torch.arange(used, device="cuda")
+        s["table"][where % table[0], where // table[0]] = ids
+        s["ref"][ids.long()] = 1
+        # the first sequence's first page is shared by all the others (a common prompt)
+        s["table"][:, -1] = s["table"][0, 0]
+        s["ref"][ids[0].long()] += table[0]
+        s["table_out"], s["ref_out"], s["n_used"] = torch.empty_like(s["table"]), torch.empty_like(s["ref"]), _ints([0])
+    return s
+
+
+def prepare(case, seed):
+    s = _inputs(case, seed)
+    s["case"] = case
+    s["scale"] = 1.0 / math.sqrt(case["head_dim"])
+    if case["kind"] == "store":
+        segs = _plan(case)[0]
+        s["records"] = [dict(src_slot0=a, seq=b, n_tokens=t, src_pos0=p, dst_pos0=e) for a, b, t, p, e in segs]
+        s["longest"] = max(t for _, _, t, _, _ in segs)
+    elif case["kind"] == "attend":
+        s["max_kv"] = max(kv for _, kv in _lengths(case))
+        s["max_q"] = max(q for q, _ in _lengths(case))
+    s["kept"] = {}   # the descriptors and workspaces that a program keeps beside its caches, made at its first call
+    return s
+
+
+# ---- one pass: the library's calls ----------------------------------------------------
+
+def _ok(pkv, status):
+    if status != pkv.PKV_OK:
+        raise pkv.PkvError(status, pkv.pkv_last_error())
+
+
+def _plan_own(pkv, s):
+    c, kept = s["case"], s["kept"]
+    if c["kind"] == "store":
+        style = pkv.PKV_ROPE_HALF if c["style"] == "half" else pkv.PKV_ROPE_INTERLEAVED
+        kept["segs"] = pkv.make_segments_q8(s["records"], "cuda")
+        kept["layout"] = pkv.make_layout_q8(s["src_k"], s["src_v"], s["k"], s["v"], s["table"], rope_style=style)
+        kept["paging"] = pkv.make_paging(s["table"], s["k"], s["v"])
+        kept["scales"] = pkv.make_block_scales(s["ks"], s["vs"], c["page"])
+    elif c["kind"] == "attend":
+        kept["scales"] = pkv.make_block_scales(s["ks"], s["vs"], c["page"])
+        kept["paging"] = pkv.make_paging(s["table"], s["k"], s["v"])
+        kept["desc"] = pkv.make_attn_desc_q8(s["q"], s["k"], s["v"], s["out"], s["table"], s["max_kv"],
+                                             n_seqs=c["seqs"], cu_q=s["cu_q"], max_q=s["max_q"], window=c["window"])
+        kept["bytes"] = pkv.pkv_attention_q8_workspace_size(kept["desc"], c["heads"], c["kv_heads"], c["head_dim"])
+        kept["workspace"] = torch.empty(max(16, kept["bytes"]), dtype=torch.uint8, device="cuda")
+    else:
+        kept["pool"] = pkv.make_page_pool([s[name] for name in ("k", "v", "ks", "vs") if name in s], s["table"], c["page"])
+        n = s["child"].numel() if c["kind"] == "fork" else 0
+        if n:
+            kept["forks"] = pkv.make_forks([dict(parent=p, child=b, n_tokens=t) for p, b, t in
+                                            zip(s["parent"].tolist(), s["child"].tolist(), s["length"].tolist())], "cuda")
+        kept["bytes"] = pkv.pkv_pages_workspace_size(kept["pool"], n)
+        kept["workspace"] = torch.empty(max(16, kept["bytes"]), dtype=torch.uint8, device="cuda")
+    return kept
+
+
+def _run_own(s):
+    from paper_2606_17107_amd import pkv
+
+    c = s["case"]
+    k = s["kept"] or _plan_own(pkv, s)
+    if c["kind"] == "store":
+        _ok(pkv, pkv.pkv_reposition_splice_q8(s["src_k"], s["src_v"], s["k"], s["v"], k["segs"], len(s["records"]),
+                                              s["longest"], s["kv_len"], c["seqs"], None, c["theta"], c["head_dim"],
+                                              k["layout"], k["paging"], k["scales"]))
+    elif c["kind"] == "attend":
+        _ok(pkv, pkv.pkv_suffix_attention_q8(s["q"], s["k"], s["v"], s["out"], s["q_pos"], s["kv_len"], c["heads"],
+                                             c["kv_heads"], c["head_dim"], s["scale"], k["desc"], k["paging"],
+                                             k["scales"], k["workspace"], k["bytes"]))
+    elif c["kind"] == "fork":
+        n = s["child"].numel()
+        _ok(pkv, pkv.pkv_pages_free(k["pool"], s["ref"], s["table"], s["child"], None, n))
+        _ok(pkv, pkv.pkv_pages_fork(k["pool"], s["ref"], s["table"], s["table"], k["forks"], n, k["workspace"],
+                                    k["bytes"]))
+    else:
+        _ok(pkv, pkv.pkv_pages_compact(k["pool"], s["ref"], s["ref_out"], s["table"], s["table_out"], s["n_used"],
+                                       k["workspace"], k["bytes"]))
+
+
+# ---- one pass: the plain forms ---------------------------------------------------------
+
+def _turn(k, delta, case):
+    """Keys [L, H, tokens, d] in 32 bits turned by delta positions; the angles are formed in 64 bits."""
+    r = case["head_dim"]
+    w = case["theta"] ** (-torch.arange(0, r, 2, dtype=torch.float64, device="cuda") / r)
+    angle = delta.double()[:, None] * w
+    c, s = angle.cos().float(), angle.sin().float()
+    if case["style"] == "half":
+        a, b = k[..., : r // 2], k[..., r // 2:]
+        return torch.cat([a * c - b * s, a * s + b * c], -1)
+    a, b = k[..., 0::2], k[..., 1::2]
+    return torch.stack([a * c - b * s, a * s + b * c], -1).flatten(-2)
+
+
+def _store_plain(s):
+    c = s["case"]
+    page, block = c["page"], c["block"]
+    L, H, d = c["layers"], c["kv_heads"], c["head_dim"]
+    at = s["dst"] // block                                  # logical block of each token
+    touched, inverse = torch.unique(s["seq"] * 2 ** 32 + at, return_inverse=True)
+    seq, at = touched // 2 ** 32, touched % 2 ** 32
+    nb = touched.numel()
+    slots = at[:, None] * block + torch.arange(block, device="cuda")     # logical slots of the touched blocks
+    pages = s["table"].long()[seq, at * block // page]
+    inside = slots % page
+    place = inverse * block + s["dst"] % block
+    written = torch.zeros(nb * block, dtype=torch.bool, device="cuda")
+    written[place] = True
+    written = written.view(nb, block)
+    kept = ~written & (slots < s["kv_len"][seq][:, None])
+    for name in "kv":
+        x = s["src_" + name][:, :, s["src"]].float()
+        if name == "k":
+            x = _turn(x, s["delta"], c)
+        new = torch.zeros(L, H, nb * block, d, device="cuda")
+        new[:, :, place] = x
+        new = new.view(L, H, nb, block, d).permute(0, 2, 3, 1, 4)         # as the pool: [L, nb, block, H, d]
+        pool, scale = s[name], s[name + "s"]
+        codes = pool.view(torch.uint8)
+        held = codes[:, pages[:, None], inside]
+        row = (pages, inside[:, 0] // block)
+        old = torch.where(kept.any(1)[:, None], scale[:, row[0], row[1]].int(), 0)
+        bits = new.abs().nan_to_num(0.0, 0.0).amax((2, 4)).view(torch.int32)
+        need = ((bits >> 23) - 8 + ((bits & 0x7FFFFF) > 0x600000).int()).clamp(min=1)
+        e = torch.maximum(need, old)
+        up, down = (127 - e).float().exp2(), (old - e).float().exp2()
+        fresh = (new * up[:, :, None, :, None]).to(E4M3).view(torch.uint8)
+        again = (held.view(E4M3).float() * down[:, :, None, :, None]).to(E4M3).view(torch.uint8)
+        held = torch.where(written[:, :, None, None], fresh, torch.where(kept[:, :, None, None], again, held))
+        codes[:, pages[:, None], inside] = held
+        scale[:, row[0], row[1]] = e.to(torch.uint8)
+
+
+def _values(s, name):
+    """What the cache's tables lead to, in 32 bits: [L, H, sequences, slots, d]."""
+    c = s["case"]
+    ids = s["table"].long()
+    x = s[name].view(torch.uint8)[:, ids].view(E4M3).float()              # [L, S, pages, page, H, d]
+    e = (s[name + "s"][:, ids].int() - 127).float().exp2()                # [L, S, pages, blocks, H]
+    x = x.view(x.shape[:3] + (-1, c["block"]) + x.shape[4:]) * e[:, :, :, :, None, :, None]
+    x = x.reshape(x.shape[:2] + (-1,) + x.shape[5:])[:, :, : s["max_kv"]]
+    return x.permute(0, 3, 1, 2, 4)
+
+
+def _attend_plain(s):
+    c = s["case"]
+    L, S, H, G, d = c["layers"], c["seqs"], c["kv_heads"], c["heads"] // c["kv_heads"], c["head_dim"]
+    mq, mk = s["max_q"], s["max_kv"]
+    first, last = s["cu_q"][:-1].long(), s["cu_q"][1:].long()
+    i = torch.arange(mq, device="cuda")
+    real = i < (last - first)[:, None]                                     # [S, mq]
+    rows = torch.minimum(first[:, None] + i, last[:, None] - 1)
+    q = s["q"][:, rows].float().view(L, S, mq, H, G, d).permute(0, 3, 1, 2, 4, 5).reshape(L, H, S, mq * G, d)
+    x = q @ _values(s, "k").transpose(-1, -2).contiguous() * s["scale"]
+    pos, j = s["q_pos"].long()[rows], torch.arange(mk, device="cuda")
+    seen = (j <= pos[..., None]) & (j < s["kv_len"][:, None, None])
+    if c["window"]:
+        seen &= j > pos[..., None] - c["window"]
+    seen = seen[:, :, None].expand(S, mq, G, mk).reshape(S, mq * G, mk)
+    x = torch.where(seen, x, -math.inf)
+    p = torch.exp(x - x.amax(-1, keepdim=True).clamp(min=-3e38))
+    total = p.sum(-1, keepdim=True)
+    o = (p @ _values(s, "v").contiguous()) / total.clamp(min=1e-30)
+    o = o.view(L, H, S, mq, G, d).permute(0, 2, 3, 1, 4, 5).reshape(L, S, mq, H * G, d)
+    s["out"][:, rows[real]] = o[:, real].to(torch.bfloat16)
+
+
+def _tensors(s):
+    return [s[name].view(torch.uint8) if s[name].dtype is E4M3 else s[name] for name in ("k", "v", "ks", "vs") if name in s]
+
+
+def _fork_plain(s):
+    c = s["case"]
+    page, child, parent, length = c["page"], s["child"].long(), s["parent"].long(), s["length"].long()
+    table, ref = s["table"], s["ref"]
+    # the old branches' pages are given back
+    held = table[child]
+    ref.index_add_(0, held.clamp(min=0).flatten().long(), -(held >= 0).int().flatten())
+    # whole pages are shared, a partly filled last page is copied into the lowest free one
+    free = torch.argsort((ref != 0).int(), stable=True)
+    whole, tail = length // page, length % page
+    needs = tail > 0
+    fresh = free[(needs.cumsum(0) - 1).clamp(min=0)]
+    e = torch.arange(table.shape[1], device="cuda")
+    share = e < whole[:, None]
+    rows = torch.where(share, table[parent], -1)
+    ref.index_add_(0, rows.clamp(min=0).flatten().long(), share.int().flatten())
+    ref.index_add_(0, fresh, needs.int())
+    last = (e == whole[:, None]) & needs[:, None]
+    table[child] = torch.where(last, fresh[:, None].int(), rows)
+    source = table[parent, whole.clamp(max=table.shape[1] - 1)].long()
+    source, fresh, tail = source[needs], fresh[needs], tail[needs]
+    for t in _tensors(s):
+        per = page // t.shape[2]                                           # slots of one entry of dim 2
+        live = torch.arange(t.shape[2], device="cuda") * per < tail[:, None]
+        live = live.view(live.shape + (1,) * (t.dim() - 3))
+        t[:, fresh] = torch.where(live, t[:, source], t[:, fresh])
+
+
+def _compact_plain(s):
+    ref = s["ref"]
+    used = ref > 0
+    n = used.sum()
+    place = torch.arange(ref.numel(), device="cuda")
+    moving, holes = used & (place >= n), ~used & (place < n)
+    src, dst = place[moving], place[holes]
+    to = torch.where(used, place, -1)
+    to[src] = dst
+    s["ref_out"].zero_()
+    s["ref_out"][to[used]] = ref[used]
+    held = s["table"].long()
+    s["table_out"].copy_(torch.where((held >= 0) & (held < ref.numel()), to[held.clamp(0, ref.numel() - 1)], held))
+    s["n_used"].copy_(n.view(1))
+    for t in _tensors(s):
+        t[:, dst] = t[:, src]
+
+
+def run(s):
+    kind = s["case"]["kind"]
+    if own:
+        _run_own(s)
+    else:
+        {"store": _store_plain, "attend": _attend_plain, "fork": _fork_plain, "compact": _compact_plain}[kind](s)
+    if kind == "attend":
+        return s["out"]
+    scales = (s["ks"].view(E8M0), s["vs"].view(E8M0)) if "ks" in s else ()
+    if kind == "store":
+        return (s["k"], s["v"]) + scales
+    if kind == "fork":
+        return (s["k"], s["v"]) + scales + (s["table"], s["ref"])
+    return (s["k"], s["v"]) + scales + (s["table_out"], s["ref_out"], s["n_used"])
+
+
+# ---- what a pass cannot do without -----------------------------------------------------
+
+def work(case):
+    L, H, d = case["layers"], case["kv_heads"], case["head_dim"]
+    if case["kind"] == "store":
+        segs, live, slots = _plan(case)
+        tokens = sum(t for _, _, t, _, _ in segs)
+        read = min(slots, tokens) * BYTES[case["dtype"]]
+        return {"bytes": 2 * L * H * d * (read + tokens) + 2 * L * H * -(-tokens // case["block"]),
+                "flops": 5 * tokens * L * H * d}
+    if case["kind"] == "attend":
+        keys = pairs = rows = 0
+        for nq, kv in _lengths(case):
+            w = case["window"]
+            first = max(0, kv - nq - w + 1) if w else 0
+            keys += kv - first
+            rows += nq
+            pairs += sum(min(kv - nq + i + 1, w) if w else kv - nq + i + 1 for i in range(nq))
+        return {"bytes": L * (2 * keys * H * d + rows * case["heads"] * d * 4), "flops": 4 * d * case["heads"] * pairs * L}
+    slot = 2 * L * H * (d * BYTES[case["dtype"]] + (1.0 / case["block"] if case["dtype"] == "e4m3" else 0.0))
+    pages, table = _shape(case)
+    if case["kind"] == "fork":
+        copied = sum(n % case["page"] for n in _parents(case)) * case["ways"]
+        return {"bytes": 2 * copied * slot + 8 * table[0] * table[1], "flops": 0}
+    return {"bytes": 2 * case["moves"] * case["page"] * slot + 8 * table[0] * table[1] + 8 * pages, "flops": 0}
+
+
+# ---- the same outputs in 64 bits ---------------------------------------------------------
+
+def _held_exactly(x):
+    """E4M3 values nearest to x (ties to even): 3 bits behind the leading one, steps of 2^-9 below 2^-6."""
+    step = torch.exp2(torch.floor(torch.log2(x.abs().clamp(min=2.0 ** -6))) - 3)
+    return torch.round(x / step) * step
+
+
+def _store_exact(case, s):
+    block, page = case["block"], case["page"]
+    d = case["head_dim"]
+    segs, live, _ = _plan(case)
+    w = torch.tensor([case["theta"] ** (-2.0 * i / d) for i in range(d // 2)], dtype=torch.float64, device="cuda")
+    result = [s["k"].double(), s["v"].double(), torch.exp2(s["ks"].double() - 127), torch.exp2(s["vs"].double() - 127)]
+    for seq in range(case["seqs"]):
+        mine = [g for g in segs if g[1] == seq]
+        lo = min(g[4] for g in mine) // block
+        hi = -(-max(g[4] + g[2] for g in mine) // block)
+        slots = torch.arange(lo * block, hi * block, device="cuda")
+        ids, inside = s["table"][seq].long()[slots // page], slots % page
+        new = torch.zeros_like(slots, dtype=torch.bool)
+        for g in mine:
+            new[g[4] - lo * block:g[4] + g[2] - lo * block] = True
+        kept = ~new & (slots < live[seq])
+        for t, name in enumerate(("src_k", "src_v")):
+            x = result[t][:, ids, inside].transpose(1, 2).contiguous()    # [L, H, slots, d], held codes for now
+            for src0, _, n, pos0, dst0 in mine:
+                y = s[name][:, :, src0:src0 + n].double()
+                if t == 0:
+                    c, sn = torch.cos((dst0 - pos0) * w), torch.sin((dst0 - pos0) * w)
+                    if case["style"] == "half":
+                        a, b = y[..., :d // 2].clone(), y[..., d // 2:].clone()
+                        y[..., :d // 2], y[..., d // 2:] = a * c - b * sn, b * c + a * sn
+                    else:
+                        a, b = y[..., ::2].clone(), y[..., 1::2].clone()
+                        y[..., ::2], y[..., 1::2] = a * c - b * sn, b * c + a * sn
+                x[:, :, dst0 - lo * block:dst0 + n - lo * block] = y
+            x = x.view(x.shape[:2] + (hi - lo, block, d))
+            fresh, stay = new.view(-1, block), kept.view(-1, block)
+            top = (x.abs() * fresh[:, :, None]).amax((3, 4))               # [L, H, blocks]
+            scale = torch.exp2(torch.ceil(torch.log2(top.clamp(min=2.0 ** -1000) / 448))).clamp(min=2.0 ** -126)
+            at = (ids[::block], inside[::block] // block)
+            before = result[2 + t][:, at[0], at[1]].transpose(1, 2)
+            scale = torch.where(stay.any(1), torch.maximum(scale, before), scale)
+            y = torch.where(fresh[:, :, None], _held_exactly(x / scale[..., None, None]),
+                            torch.where(stay[:, :, None], _held_exactly(x * (before / scale)[..., None, None]), x))
+            result[t][:, ids, inside] = y.reshape(y.shape[:2] + (-1, d)).transpose(1, 2)
+            result[2 + t][:, at[0], at[1]] = scale.transpose(1, 2)
+    return tuple(result)
+
+
+def _attend_exact(case, s):
+    G, page, block = case["heads"] // case["kv_heads"], case["page"], case["block"]
+    out = torch.zeros(s["q"].shape, dtype=torch.float64, device="cuda")
+    row = 0
+    for i, (nq, kv) in enumerate(_lengths(case)):
+        j = torch.arange(kv, device="cuda")
+        ids, inside = s["table"][i].long()[j // page], j % page
+        for layer in range(case["layers"]):
+            for g in range(case["kv_heads"]):
+                k, v = (s[t][layer, :, :, g].double()[ids, inside] *
+                        torch.exp2(s[t + "s"][layer, ids, inside // block, g].double() - 127)[:, None] for t in "kv")
+                at = row
+                while at < row + nq:
+                    n = min(row + nq - at, max(1, int(1.5e8 // (kv * G))))
+                    q = s["q"][layer, at:at + n, g * G:(g + 1) * G].double().reshape(n * G, -1)
+                    x = ((q @ k.t().contiguous()) * s["scale"]).view(n, G, kv)
+                    p = s["q_pos"][at:at + n].long()[:, None, None]
+                    hidden = j > p
+                    if case["window"]:
+                        hidden = hidden | (j <= p - case["window"])
+                    weight = torch.softmax(x.masked_fill(hidden, -math.inf), -1)
+                    out[layer, at:at + n, g * G:(g + 1) * G] = (weight.view(n * G, kv) @ v).view(n, G, -1)
+                    at += n
+        row += nq
+    return out
+
+
+def _pages_exact(case, s):
+    """The pages' contents after the pass (copied values in 64 bits) and, worked out entry by entry, table and counts."""
+    page = case["page"]
+    table, ref = s["table"].tolist(), s["ref"].tolist()
+    copies, counts = [], []                                                # (source, destination, slots)
+    if case["kind"] == "fork":
+        jobs = list(zip(s["parent"].tolist(), s["child"].tolist(), s["length"].tolist()))
+        for _, child, _ in jobs:
+            for p in table[child]:
+                if p >= 0:
+                    ref[p] -= 1
+        free = iter([p for p, n in enumerate(ref) if n == 0])
+        for parent, child, length in jobs:
+            whole = length // page
+            table[child] = [p if e < whole else -1 for e, p in enumerate(table[parent])]
+            for p in table[child][:whole]:
+                ref[p] += 1
+            if length % page:
+                table[child][whole] = next(free)
+                ref[table[child][whole]] = 1
+                copies.append((table[parent][whole], table[child][whole], length % page))
+    else:
+        n = sum(1 for r in ref if r > 0)
+        holes = iter([p for p in range(n) if ref[p] == 0])
+        to = {p: p if p < n else next(holes) for p in range(len(ref)) if ref[p] > 0}
+        copies = [(p, h, page) for p, h in to.items() if p != h]
+        table = [[to[p] if p >= 0 else p for p in r] for r in table]
+        after = [0] * len(ref)
+        for p, h in to.items():
+            after[h] = ref[p]
+        ref, counts = after, [[n]]
+    pools = []
+    for name in ("k", "v", "ks", "vs"):
+        if name in s:
+            t = s[name]
+            x = torch.exp2(t.double() - 127) if t.dtype is torch.uint8 else t.double()
+            for a, b, slots in copies:
+                n = -(-slots * t.shape[2] // page)
+                x[:, b, :n] = x[:, a, :n]
+            pools.append(x)
+    return tuple(pools) + tuple(_ints(x) for x in [table, ref] + counts)
+
+
+def exact(case, seed):
+    s = _inputs(case, seed)
+    s["scale"] = 1.0 / math.sqrt(case["head_dim"])
+    return {"store": _store_exact, "attend": _attend_exact, "fork": _pages_exact, "compact": _pages_exact}[case["kind"]](case, s)
