@@ -341,16 +341,16 @@ def _plan_own(pkv, s):
     c, kept = s["case"], s["kept"]
     if c["kind"] == "store":
         style = pkv.PKV_ROPE_HALF if c["style"] == "half" else pkv.PKV_ROPE_INTERLEAVED
-        kept["segs"] = pkv.make_segments_q8(s["records"], "cuda")
-        kept["layout"] = pkv.make_layout_q8(s["src_k"], s["src_v"], s["k"], s["v"], s["table"], rope_style=style)
+        kept["segs"] = pkv.make_segments_quant(s["records"], "cuda")
+        kept["layout"] = pkv.make_layout_quant(s["src_k"], s["src_v"], s["k"], s["v"], s["table"], rope_style=style)
         kept["paging"] = pkv.make_paging(s["table"], s["k"], s["v"])
         kept["scales"] = pkv.make_block_scales(s["ks"], s["vs"], c["page"])
     elif c["kind"] == "attend":
         kept["scales"] = pkv.make_block_scales(s["ks"], s["vs"], c["page"])
         kept["paging"] = pkv.make_paging(s["table"], s["k"], s["v"])
-        kept["desc"] = pkv.make_attn_desc_q8(s["q"], s["k"], s["v"], s["out"], s["table"], s["max_kv"],
+        kept["desc"] = pkv.make_attn_desc_quant(s["q"], s["k"], s["v"], s["out"], s["table"], s["max_kv"],
                                              n_seqs=c["seqs"], cu_q=s["cu_q"], max_q=s["max_q"], window=c["window"])
-        kept["bytes"] = pkv.pkv_attention_q8_workspace_size(kept["desc"], c["heads"], c["kv_heads"], c["head_dim"])
+        kept["bytes"] = pkv.pkv_attention_quant_workspace_size(kept["desc"], c["heads"], c["kv_heads"], c["head_dim"])
         kept["workspace"] = torch.empty(max(16, kept["bytes"]), dtype=torch.uint8, device="cuda")
     else:
         kept["pool"] = pkv.make_page_pool([s[name] for name in ("k", "v", "ks", "vs") if name in s], s["table"], c["page"])
@@ -369,11 +369,11 @@ def _run_own(s):
     c = s["case"]
     k = s["kept"] or _plan_own(pkv, s)
     if c["kind"] == "store":
-        _ok(pkv, pkv.pkv_reposition_splice_q8(s["src_k"], s["src_v"], s["k"], s["v"], k["segs"], len(s["records"]),
+        _ok(pkv, pkv.pkv_reposition_splice_quant(s["src_k"], s["src_v"], s["k"], s["v"], k["segs"], len(s["records"]),
                                               s["longest"], s["kv_len"], c["seqs"], None, c["theta"], c["head_dim"],
                                               k["layout"], k["paging"], k["scales"]))
     elif c["kind"] == "attend":
-        _ok(pkv, pkv.pkv_suffix_attention_q8(s["q"], s["k"], s["v"], s["out"], s["q_pos"], s["kv_len"], c["heads"],
+        _ok(pkv, pkv.pkv_suffix_attention_quant(s["q"], s["k"], s["v"], s["out"], s["q_pos"], s["kv_len"], c["heads"],
                                              c["kv_heads"], c["head_dim"], s["scale"], k["desc"], k["paging"],
                                              k["scales"], k["workspace"], k["bytes"]))
     elif c["kind"] == "fork":
