@@ -579,6 +579,7 @@ def source_hash(files):
 KERNEL_SOURCES = {   # the kernel's translation unit first, then the headers it includes and its dispatch
     "splice_kernel": ["paper_2606_17107_amd/csrc/splice.hip", "paper_2606_17107_amd/csrc/pkv_internal.h"],
     "attn_gqa_bf16": ["paper_2606_17107_amd/csrc/attn_gqa_bf16.hip", "paper_2606_17107_amd/csrc/attn_gqa_tile.h",
+                      "paper_2606_17107_amd/csrc/attn_gqa_tile_q8.h",
                       "paper_2606_17107_amd/csrc/attn_common.h", "paper_2606_17107_amd/csrc/attention.hip",
                       "paper_2606_17107_amd/csrc/attn_columns.h", "paper_2606_17107_amd/csrc/pkv_internal.h"],
     "attn_mla_bf16": ["paper_2606_17107_amd/csrc/attn_mla_bf16.hip", "paper_2606_17107_amd/csrc/attn_mla_tile.h",

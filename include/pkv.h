@@ -348,6 +348,170 @@ pkv_status pkv_suffix_attention_noalloc(const void* q, const void* k_cache, cons
                                         const pkv_attn_desc* desc, void* stream);
 
 /* ---------------------------------------------------------------------------
+ * Cache held in 8 bits
+ * ------------------------------------------------------------------------- */
+
+/* A paged cache of E4M3 codes (1 sign, 4 exponent, 3 fraction bits, bias 7, finite
+ * up to 448, 0x7f and 0xff NaN, no infinities) with one scale byte e per block of
+ * block_tokens slots, KV head, layer and tensor: a code of value c stands for
+ * c * 2^(e - 127), exactly a bf16 number.  Pools and block tables are those of
+ * pkv_paged_cache with one byte per element; the scale of (layer l, kv head h, page
+ * P, block b of the page) is at l*stride[0] + h*stride[1] + P*stride[2] +
+ * b*stride[3].  The library writes e in [1, 254]; over a block with e of 0 or 255 a
+ * result is undefined.  Values go through paging->v_block_table when it is set, their
+ * scales too. */
+typedef struct pkv_block_scales {
+    int32_t block_tokens;      /* slots that share a scale: 32, 64 or 128, at most page_size */
+    int32_t reserved;          /* must be 0 */
+    uint8_t* k_scale;          /* device */
+    uint8_t* v_scale;          /* device; NULL without a V tensor */
+    int64_t k_stride[4];       /* {layer, head, page, block in page}, bytes */
+    int64_t v_stride[4];
+} pkv_block_scales;
+
+/* One chunk of a pkv_reposition_splice_quant call: source tokens src_slot0 ..
+ * src_slot0+n_tokens-1, encoded at positions src_pos0 .., move to positions (= logical
+ * slots) dst_pos0 .. of sequence seq.  delta = dst_pos0 - src_pos0; 0 for tokens that
+ * are at their position already (new tokens of a prefill or of token-by-token
+ * generation). */
+typedef struct pkv_segment_quant {
+    int64_t src_slot0;
+    int32_t seq;               /* row of the block table */
+    int32_t n_tokens;
+    int32_t src_pos0;
+    int32_t dst_pos0;
+} pkv_segment_quant;
+
+/* Reposition + splice into a paged cache held in 8 bits (Sec. 5; Sec. 8: the cache
+ * keeps per-token KV, so the operation carries over).  The source is bf16 or fp32 as
+ * in pkv_reposition_splice_batched; rows are turned by delta with the arithmetic of
+ * that call (coefficients in fp64 rounded to fp32) and quantised without an
+ * intermediate rounding.  For a block that gets rows x_t, with `kept` the block's
+ * other slots below kv_len[seq] (the slots in use before the call):
+ *     need = the smallest e >= 1 with max |x_t| <= 448 * 2^(e - 127)
+ *     e    = need if nothing is kept, else max(need, the block's old e)
+ *     code = E4M3(x_t * 2^(127 - e)), to the nearest, ties to even
+ *     kept code = E4M3(code * 2^(old e - e)) where e grew, else unchanged
+ * A NaN or an infinity is stored as NaN and does not enter the maximum.  Slots that
+ * are neither written nor kept are left as they are, and blocks that get no row
+ * altogether.  Segments of one call may share a block (chunks spliced back to back);
+ * they must not write the same slot, and different sequences must not write into the
+ * same page.  kv_len is read only: the caller raises it afterwards.
+ * layout: dtype of the source, n_tokens its slots; dst_capacity the logical slots of
+ * every sequence (at most 2^30); dst strides in bytes; reserved 0.  head_dim 64 or 128;
+ * v_dim head_dim, or 0 without values.  rope_offset a multiple of 8, rope_dim of 16.
+ * omega: host fp64 [rope_dim/2] per-pair frequencies as in pkv_reposition_splice_freqs,
+ * or NULL for rope_theta^(-2i/rope_dim).  segs: DEVICE array; max_seg_tokens: at least
+ * every n_tokens (longer segments are spliced all the same, by fewer workgroups).
+ * kv_len: device int32 [n_seqs].  A token whose sequence, slot, source slot or page
+ * entry is out of range is skipped (and *layout->err_flag set).
+ * Errors: PKV_ERR_NULL, PKV_ERR_SHAPE, PKV_ERR_ALIGN (pools and sources 16 bytes, segs 8),
+ * PKV_ERR_ALIAS (two of sources, pools and scales overlap), PKV_ERR_UNSUPPORTED (dtype,
+ * style, geometry, more than 65535 segments, a grid beyond the device's limits),
+ * PKV_ERR_DEVICE. */
+pkv_status pkv_reposition_splice_quant(const void* src_k, const void* src_v, void* k_pages, void* v_pages,
+                                    const pkv_segment_quant* segs, int32_t n_segs, int32_t max_seg_tokens,
+                                    const int32_t* kv_len, int32_t n_seqs, const double* omega, float rope_theta,
+                                    int32_t rope_dim, const pkv_layout* layout, const pkv_paged_cache* paging,
+                                    const pkv_block_scales* scales, void* stream);
+
+/* Bytes of device workspace pkv_suffix_attention_quant needs for `desc`; 0 when no split
+ * is used, and on invalid arguments. */
+size_t pkv_attention_quant_workspace_size(const pkv_attn_desc* desc, int32_t n_q_heads, int32_t n_kv_heads,
+                                       int32_t head_dim);
+
+/* Suffix attention over a paged cache held in 8 bits: as pkv_suffix_attention_paged
+ * with keys and values code * scale, which the kernels form exactly.  desc->dtype is
+ * that of q and out, PKV_BF16; k and v strides are in bytes; GQA only.  A row's result
+ * does not depend on the contents of slots that it does not see, NaN codes included.
+ * Errors: as pkv_suffix_attention_paged; PKV_ERR_NULL (scales, k_scale, v_scale),
+ * PKV_ERR_SHAPE (block_tokens, reserved, negative strides), PKV_ERR_UNSUPPORTED (MLA,
+ * a dtype other than PKV_BF16), PKV_ERR_ALIAS (out overlaps the scales too). */
+pkv_status pkv_suffix_attention_quant(const void* q, const void* k_pages, const void* v_pages, void* out,
+                                   const int32_t* q_pos, const int32_t* kv_len, int32_t n_q_heads,
+                                   int32_t n_kv_heads, int32_t head_dim, float scale, const pkv_attn_desc* desc,
+                                   const pkv_paged_cache* paging, const pkv_block_scales* scales, void* workspace,
+                                   size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * Pages of a cache: free, fork, compact
+ * ------------------------------------------------------------------------- */
+
+/* One tensor of a page pool, in bytes: the page P of layer l is n_slots x n_heads rows
+ * of row_bytes, row (s, h) at l*layer_stride + P*page_stride + s*slot_stride +
+ * h*head_stride.  Any dtype; the scales of a cache held in 8 bits are a tensor of
+ * their own with n_slots = blocks per page.  n_slots divides page_size. */
+typedef struct pkv_page_tensor {
+    void* data;
+    int64_t layer_stride, page_stride, slot_stride, head_stride;
+    int32_t n_layers, n_slots, n_heads, row_bytes;
+} pkv_page_tensor;
+
+/* A page pool and the block tables over it ([n_seqs][max_pages], -1 = no page).  The
+ * caller keeps ref: device int32 [n_pages], how many table entries refer to each page,
+ * 0 for a free one. */
+typedef struct pkv_page_pool {
+    int32_t page_size;         /* slots per page: a power of two, 32 .. 2^20 */
+    int32_t n_tensors;         /* 1 .. 4 */
+    int32_t n_seqs;
+    int32_t max_pages;
+    int64_t n_pages;
+    pkv_page_tensor tensors[4];
+    int32_t* err_flag;         /* optional device int32: set to 1 where a call says so */
+} pkv_page_pool;
+
+/* Branch of a sequence: row child becomes the first n_tokens slots of row parent. */
+typedef struct pkv_fork {
+    int32_t parent, child, n_tokens, reserved;
+} pkv_fork;
+
+/* Bytes of device workspace of pkv_pages_fork with n_forks records, or (n_forks 0) of
+ * pkv_pages_compact.  0 on invalid arguments.  The workspace is scratch: nothing in it
+ * needs clearing, and calls that overlap in time need one each. */
+size_t pkv_pages_workspace_size(const pkv_page_pool* pool, int32_t n_forks);
+
+/* Give back pages of n sequences: of row seqs[i], every entry from page
+ * ceil(keep[i] / page_size) on is set to -1 and the count of its page lowered by one.
+ * keep: device int32 [n], slots to keep (negative: 0), or NULL for none.  A sequence
+ * listed twice gives its pages back once.  A sequence out of range is skipped, an entry
+ * outside the pool is set to -1 without a page, and a count is not lowered below 0;
+ * each sets *err_flag.
+ * Errors: PKV_ERR_NULL, PKV_ERR_SHAPE, PKV_ERR_UNSUPPORTED, PKV_ERR_DEVICE.  (The pool's
+ * tensors are checked but not read.) */
+pkv_status pkv_pages_free(const pkv_page_pool* pool, int32_t* ref, int32_t* block_table, const int32_t* seqs,
+                          const int32_t* keep, int32_t n, void* stream);
+
+/* Fork n_forks sequences.  For each record, row child of table_out becomes row parent
+ * of table_in up to n_tokens: the whole pages are shared (their counts go up by one), a
+ * last page that is filled in part is copied, its live slots only (for scales: the
+ * blocks with live slots), to a free page whose count becomes 1, and the rest of the
+ * row is -1.  New pages are the lowest free ones, in the order of the records.  What
+ * row child held before is not given back (pkv_pages_free does).  table_out may be
+ * table_in or another table (beams that swap places).  forks: DEVICE array.
+ * Skipped records, which leave their child's row alone and set *err_flag: a row or
+ * length out of range; a child that a record before it names; with table_out equal to
+ * table_in, a parent that is a child of some record in range.  Also flagged: a free page
+ * is missing, or the parent has no page where one is needed (the entry is -1).
+ * Errors: PKV_ERR_NULL, PKV_ERR_SHAPE (also a workspace that is too small), PKV_ERR_ALIGN
+ * (forks and workspace 16 bytes), PKV_ERR_ALIAS (tables that overlap in part, or tensors),
+ * PKV_ERR_UNSUPPORTED (more than 65535 records; 2^31 units in one tensor's page),
+ * PKV_ERR_DEVICE. */
+pkv_status pkv_pages_fork(const pkv_page_pool* pool, int32_t* ref, const int32_t* table_in, int32_t* table_out,
+                          const pkv_fork* forks, int32_t n_forks, void* workspace, size_t workspace_bytes,
+                          void* stream);
+
+/* Move the pages in use to the front of the pool.  With n = the pages whose count is
+ * above 0, the k-th of those from index n on is copied to the k-th free page below n,
+ * in page order; ref_out and table_out are ref_in and table_in with the pages renamed
+ * (either may be its input), *n_used = n (device int32).  Entries outside the pool
+ * are kept as they are; one of a page with count 0 becomes -1 and sets *err_flag.  The
+ * contents of pages from index n on are left as they were.
+ * Errors: as pkv_pages_fork; PKV_ERR_ALIAS also for counts that overlap in part. */
+pkv_status pkv_pages_compact(const pkv_page_pool* pool, const int32_t* ref_in, int32_t* ref_out,
+                             const int32_t* table_in, int32_t* table_out, int32_t* n_used, void* workspace,
+                             size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
  * Diagnostics
  * ------------------------------------------------------------------------- */
 

@@ -8,9 +8,11 @@
 
 namespace pkv {
 
-hipError_t launch_attn_gqa_bf16(const AttnArgs& a, const Plan& p, dim3 grid, hipStream_t stream);
+hipError_t launch_attn_gqa_bf16(const AttnArgs& a, const Plan& p, const BlockScales* scales, dim3 grid,
+                                hipStream_t stream);
 hipError_t launch_attn_mla_bf16(const AttnArgs& a, const Plan& p, dim3 grid, hipStream_t stream);
-hipError_t launch_attn_gqa_rows(const AttnArgs& a, const ColPlan& p, dim3 grid, hipStream_t stream);
+hipError_t launch_attn_gqa_rows(const AttnArgs& a, const ColPlan& p, const BlockScales* scales, dim3 grid,
+                                hipStream_t stream);
 hipError_t launch_attn_mla_rows(const AttnArgs& a, const ColPlan& p, dim3 grid, hipStream_t stream);
 
 namespace {
@@ -577,7 +579,7 @@ Plan make_plan(const AttnArgs& a, int splits, int rows = 0) {
 int wgs_per_cu(const AttnArgs& a, const Plan& p) {
     if (a.variant == 1) return 1;                     // MLA: two 36 KB stages, one wave per SIMD
     const int tile = 32;                              // keys per K/V tile
-    const int lds = p.ns * 2 * tile * a.head_dim * 2;
+    const int lds = p.ns * 2 * tile * a.head_dim * (a.dtype == 2 ? 1 : 2);
     const int n = (160 * 1024) / lds;
     return n < 1 ? 1 : (n > 2 ? 2 : n);               // two waves per SIMD at most (registers)
 }
@@ -639,7 +641,7 @@ bool col_long_enough(const AttnArgs& a, int64_t rows) {
 }
 
 bool col_route(const AttnArgs& a) {
-    if (!a.auto_splits || a.dtype != 0 || a.n_seqs > kColMaxSeqs) return false;
+    if (!a.auto_splits || a.dtype == 1 || a.n_seqs > kColMaxSeqs) return false;
     const int64_t rows = (int64_t)a.max_q * (a.n_heads / a.n_kv_heads);
     if (rows < 1 || rows > (a.variant == 1 ? kRowsMla : kRowsGqa) || !col_long_enough(a, rows))
         return false;
@@ -746,7 +748,7 @@ hipError_t launch_combine(const AttnArgs& a, bool columns, hipStream_t stream) {
                      : launch_combine_groups<4, false>(a, stream);
 }
 
-hipError_t launch_columns(const AttnArgs& a, hipStream_t stream) {
+hipError_t launch_columns(const AttnArgs& a, const BlockScales* scales, hipStream_t stream) {
     ColPlan p;
     p.G = a.n_heads / a.n_kv_heads;
     p.streams = a.n_layers * a.n_kv_heads;
@@ -763,15 +765,15 @@ hipError_t launch_columns(const AttnArgs& a, hipStream_t stream) {
     if (cols > 0x7fffffff) return hipErrorInvalidValue;
     const dim3 grid((unsigned)cols);
     const hipError_t e = a.variant == 1 ? launch_attn_mla_rows(a, p, grid, stream)
-                                        : launch_attn_gqa_rows(a, p, grid, stream);
+                                        : launch_attn_gqa_rows(a, p, scales, grid, stream);
     if (e != hipSuccess || p.columns == 0) return e;
     return launch_combine(a, true, stream);
 }
 
 }  // namespace
 
-hipError_t launch_attention(const AttnArgs& a, hipStream_t stream) {
-    if (col_route(a)) return launch_columns(a, stream);
+hipError_t launch_attention(const AttnArgs& a, const BlockScales* scales, hipStream_t stream) {
+    if (col_route(a)) return launch_columns(a, scales, stream);
     Plan p = make_plan(a, a.n_splits < 1 ? 1 : a.n_splits);
     // fp32 calls of at most one workgroup of 32 rows per CU split the keys over
     // its waves.
@@ -781,7 +783,7 @@ hipError_t launch_attention(const AttnArgs& a, hipStream_t stream) {
     if (n_wg <= 0) return hipSuccess;
     if (n_wg > 0x7fffffff) return hipErrorInvalidValue;
     // More workgroups than the CUs hold at once (bf16 GQA): the order matters.
-    p.longest_first = a.dtype == 0 && a.variant == 0 && n_wg > kCUs * (int64_t)wgs_per_cu(a, p) && order_pays(a);
+    p.longest_first = a.dtype != 1 && a.variant == 0 && n_wg > kCUs * (int64_t)wgs_per_cu(a, p) && order_pays(a);
     dim3 grid((unsigned)n_wg);
     hipError_t e;
     if (keys) {
@@ -797,7 +799,7 @@ hipError_t launch_attention(const AttnArgs& a, hipStream_t stream) {
             hipLaunchKernelGGL((attn_gqa_f32<128>), grid, dim3(128), 0, stream, a, p);
         e = hipGetLastError();
     } else {
-        e = a.variant == 1 ? launch_attn_mla_bf16(a, p, grid, stream) : launch_attn_gqa_bf16(a, p, grid, stream);
+        e = a.variant == 1 ? launch_attn_mla_bf16(a, p, grid, stream) : launch_attn_gqa_bf16(a, p, scales, grid, stream);
     }
     if (e != hipSuccess || p.splits == 1) return e;
     return launch_combine(a, false, stream);

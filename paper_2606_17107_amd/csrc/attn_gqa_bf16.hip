@@ -18,9 +18,12 @@
 //   * V stays row-major ([key][channel]) in LDS; the transposed A operand of
 //     the PV product comes from ds_read_b64_tr_b16, with the keys of each
 //     16-key step ordered as the P^T accumulator holds them.
+//   * A cache held in 8 bits (Q8, paged): the same schedule over tiles of codes,
+//     which become bf16 at the operand registers (attn_gqa_tile_q8.h).
 #include <type_traits>
 
 #include "attn_gqa_tile.h"
+#include "attn_gqa_tile_q8.h"
 
 namespace pkv {
 namespace {
@@ -38,8 +41,10 @@ constexpr int kAhead = 3;    // LDS operand reads issued this many operands ahea
 // kFull: every row block but the last of a sequence is full.  kFew: no sequence
 // fills its one row block.  kOrdered: sequences are dispatched longest first.
 enum { kFull, kFew, kOrdered };
-template <int D, bool PAGED, int FORM>
-__global__ __launch_bounds__(kWaves * 64, 2) void attn_gqa_bf16_kernel(AttnArgs a, Plan p) {
+template <int D, bool PAGED, int FORM, bool Q8>
+__global__ __launch_bounds__(kWaves * 64, 2) void attn_gqa_bf16_kernel(AttnArgs a, Plan p, ScaleArg<Q8> sa) {
+    static_assert(PAGED || !Q8, "a cache held in 8 bits is paged");
+    using Elem = std::conditional_t<Q8, uint8_t, uint16_t>;
     // The arguments of the set-up are asked for together: left alone, their loads sink
     // to their uses, one scalar round trip after another (64 queries x 4 heads over
     // 8256 keys, 8 kv heads: 30.0 us a call, 29.6 with this).
@@ -47,7 +52,8 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_gqa_bf16_kernel(AttnArgs 
                  "s"(a.q_pos), "s"(a.kv_len), "s"(a.cu_q), "s"(a.kv_base), "s"(a.cache_slots), "s"(a.total_q),
                  "s"(a.max_kv_len), "s"(a.window), "s"(a.n_kv_heads), "s"(a.n_layers));
     constexpr int QB = kQB, NW = kWaves, NS = kStages;
-    constexpr int CH = D / 8;              // 16-byte chunks per row
+    constexpr int EB = sizeof(Elem);       // bytes per element of the cache
+    constexpr int CH = D * EB / 16;        // 16-byte chunks per row
     constexpr int BN = 32;                 // keys per tile
     constexpr int NKB = BN / 32;           // 32-key blocks per tile
     constexpr int KBLK = BN * CH / 64;     // 64-lane LDS-DMA blocks per K (or V) tile
@@ -62,10 +68,10 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_gqa_bf16_kernel(AttnArgs 
     // compile-time constants after unrolling, so one address register per
     // operand serves every stage through the 16-bit immediate offset of the
     // LDS read (K stages within 48 KB of the block, V stages of the V half).
-    __shared__ __attribute__((aligned(16))) uint16_t stage_lds[2 * NS * TE];
+    __shared__ __attribute__((aligned(16))) Elem stage_lds[2 * NS * TE];
     __shared__ int red[NW], red_min[NW], red_start[NW], red_smax[NW];
-    auto kst = [&](int st) __attribute__((always_inline)) -> uint16_t* { return stage_lds + st * TE; };
-    auto vst = [&](int st) __attribute__((always_inline)) -> uint16_t* { return stage_lds + (NS + st) * TE; };
+    auto kst = [&](int st) __attribute__((always_inline)) -> Elem* { return stage_lds + st * TE; };
+    auto vst = [&](int st) __attribute__((always_inline)) -> Elem* { return stage_lds + (NS + st) * TE; };
 
     int group, rb;
     if (!decode(p, group, rb)) return;
@@ -118,7 +124,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_gqa_bf16_kernel(AttnArgs 
         for (int ks = 0; ks < KS; ++ks) v[ks] = u32x4{0u, 0u, 0u, 0u};
         if (FORM == kFull || row_ok[qb]) {
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) v[ks] = *(const u32x4*)(qrow + ks * 16 + hl * 8);
+            for (int ks = 0; ks < KS; ++ks) v[ks] = *(const u32x4*)(qrow + (Q8 ? q8_channel(ks, hl) : ks * 16 + hl * 8));
         }
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) qf[qb][ks] = __builtin_bit_cast(bf16x8, v[ks]);
@@ -166,10 +172,10 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_gqa_bf16_kernel(AttnArgs 
     const int loop_end = min(hi, k_begin + run);
     const int n_tiles = loop_end > k_begin ? (loop_end - k_begin + BN - 1) / BN : 0;
 
-    const uint16_t* kbase = (const uint16_t*)a.k + (int64_t)layer * a.k_stride[0] +
-                            (int64_t)kvh * a.k_stride[1] + si.base * a.k_stride[2];
-    const uint16_t* vbase = (const uint16_t*)a.v + (int64_t)layer * a.v_stride[0] +
-                            (int64_t)kvh * a.v_stride[1] + si.base * a.v_stride[2];
+    const Elem* kbase = (const Elem*)a.k + (int64_t)layer * a.k_stride[0] +
+                        (int64_t)kvh * a.k_stride[1] + si.base * a.k_stride[2];
+    const Elem* vbase = (const Elem*)a.v + (int64_t)layer * a.v_stride[0] +
+                        (int64_t)kvh * a.v_stride[1] + si.base * a.v_stride[2];
     const int64_t kss = a.k_stride[2], vss = a.v_stride[2];
     const int last_key = loop_end - 1;
 
@@ -181,13 +187,14 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_gqa_bf16_kernel(AttnArgs 
     const bool wave_v = wave * PER >= KBLK;
     const int blk0 = (wave * PER) % KBLK;
     const char* const tens = (const char*)(wave_v ? vbase : kbase);
-    const int64_t trow = (wave_v ? vss : kss) * 2;   // bytes between keys
+    const int64_t trow = (wave_v ? vss : kss) * EB;   // bytes between keys
     auto dma_key = [&](int i) __attribute__((always_inline)) { return ((blk0 + i) * 64 + lane) / CH; };
     uint32_t src_off[PER];   // bytes from the tile's first key
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
         const int key = dma_key(i);
-        const int logical = (lane % CH) ^ (wave_v ? swz_v<D>(key) : swz_k<D>(key));
+        const int logical = (lane % CH) ^ (wave_v ? (Q8 ? swz_v8<D>(key) : swz_v<D>(key))
+                                                  : (Q8 ? swz_k8<D>(key) : swz_k<D>(key)));
         src_off[i] = (uint32_t)(key * trow + logical * 16);
     }
     // Stage the tile starting at key t0.  A tile that runs past the last
@@ -198,14 +205,14 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_gqa_bf16_kernel(AttnArgs 
     // Waves that move V blocks read V's own block table when there is one.
     if constexpr (PAGED)
         pw.init(wave_v && a.v_block_table ? a.v_block_table : a.block_table, a, seq, k_begin >> a.page_shift);
-    const int64_t tpage = (wave_v ? a.v_page_stride : a.k_page_stride) * 2;   // bytes between pages
-    auto issue = [&](int t0, uint16_t* ks_dst, uint16_t* vs_dst) __attribute__((always_inline)) {
+    const int64_t tpage = (wave_v ? a.v_page_stride : a.k_page_stride) * EB;   // bytes between pages
+    auto issue = [&](int t0, Elem* ks_dst, Elem* vs_dst) __attribute__((always_inline)) {
         const char* tile;
         if constexpr (PAGED)
             tile = tens + pw.offset(a, t0, tpage, trow);
         else
             tile = tens + (int64_t)t0 * trow;
-        const uint32_t lds0 = lds_addr_of((wave_v ? vs_dst : ks_dst) + blk0 * 64 * 8);
+        const uint32_t lds0 = lds_addr_of((wave_v ? vs_dst : ks_dst) + blk0 * 64 * (16 / EB));
         if (t0 + BN <= loop_end) {
 #pragma unroll
             for (int i = 0; i < PER; ++i) lds_dma16(lds0 + i * 1024, tile, src_off[i]);
@@ -218,13 +225,30 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_gqa_bf16_kernel(AttnArgs 
         }
     };
 
-    int kofs[KS], vofs[DB];
-    gqa_operand_offsets<D>(lane, kofs, vofs);
-    auto k_operand = [&](const uint16_t* ks_src, int ks, int kb) __attribute__((always_inline)) {
-        return __builtin_bit_cast(bf16x8, *(const u32x4*)(ks_src + kofs[ks] + kb * 32 * D));
+    // An operand as it is read from LDS (k_read, v_read) and as it enters the MFMA
+    // (k_value, v_value): the same in bf16; in 8 bits one read holds the codes of two
+    // k-steps, and es has the exponents of the tile's scales.
+    constexpr int KR = Q8 ? KS / 2 : KS;   // K reads per tile
+    constexpr int KQ = KS / KR;            // k-steps of one
+    int kofs[KR], vofs[DB];
+    if constexpr (Q8) gqa_operand_offsets_q8<D>(lane, kofs, vofs);
+    else gqa_operand_offsets<D>(lane, kofs, vofs);
+    auto k_read = [&](const Elem* ks_src, int kr, int kb) __attribute__((always_inline)) {
+        const u32x4 w = *(const u32x4*)(ks_src + kofs[kr] + kb * 32 * D);
+        if constexpr (Q8) return w;
+        else return __builtin_bit_cast(bf16x8, w);
     };
-    auto v_operand = [&](const uint16_t* vs_src, int st, int db) __attribute__((always_inline)) {
-        return gqa_v_operand<D>(vs_src + vofs[db] + st * 16 * D);
+    auto k_value = [&](const auto& w, int ks, uint32_t es) __attribute__((always_inline)) {
+        if constexpr (Q8) return q8_to_bf16(w[(ks & 1) * 2], w[(ks & 1) * 2 + 1], q8_k_scale(es));
+        else return w;
+    };
+    auto v_read = [&](const Elem* vs_src, int st, int db) __attribute__((always_inline)) {
+        if constexpr (Q8) return q8_v_read(vs_src + vofs[db] + st * 16 * D);
+        else return gqa_v_operand<D>(vs_src + vofs[db] + st * 16 * D);
+    };
+    auto v_value = [&](const auto& w, uint32_t es) __attribute__((always_inline)) {
+        if constexpr (Q8) return q8_to_bf16(w[0], w[1], q8_v_scale(es));
+        else return w;
     };
 
     f32x16 o[DB][QB];
@@ -243,7 +267,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_gqa_bf16_kernel(AttnArgs 
     const float sc2 = a.scale * kLog2e;
 
     // Raw scores S^T = K Q^T of the tile held in K stage ks_src.
-    auto qk = [&](const uint16_t* ks_src, f32x16 (&s)[NKB][QB]) __attribute__((always_inline)) {
+    auto qk = [&](const Elem* ks_src, uint32_t es, f32x16 (&s)[NKB][QB]) __attribute__((always_inline)) {
 #pragma unroll
         for (int kb = 0; kb < NKB; ++kb)
 #pragma unroll
@@ -252,14 +276,14 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_gqa_bf16_kernel(AttnArgs 
         for (int ks = 0; ks < KS; ++ks) {
 #pragma unroll
             for (int kb = 0; kb < NKB; ++kb) {
-                const bf16x8 kf = k_operand(ks_src, ks, kb);
+                const bf16x8 kf = k_value(k_read(ks_src, ks / KQ, kb), ks, es);
 #pragma unroll
                 for (int qb = 0; qb < QB; ++qb)
                     s[kb][qb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[qb][ks], s[kb][qb], 0, 0, 0);
             }
         }
         // Keep the K-operand reads one or two MFMAs ahead instead of all at once.
-        sched_reads_mfma<NKB * KS, 1, QB>();
+        if constexpr (!Q8) sched_reads_mfma<NKB * KS, 1, QB>();
     };
 
     // Softmax, part 1 (branchy, before the overlapped region): mask the raw
@@ -345,7 +369,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_gqa_bf16_kernel(AttnArgs 
     };
 
     // O^T += V^T P^T for the tile held in V stage vs_src.
-    auto pv = [&](const uint16_t* vs_src, const bf16x8 (&pb)[QB][2 * NKB]) __attribute__((always_inline)) {
+    auto pv = [&](const Elem* vs_src, uint32_t es, const bf16x8 (&pb)[QB][2 * NKB]) __attribute__((always_inline)) {
         // Lane group g (16 lanes) reads channels 32db + 16(g&1) .. +15 for
         // keys {16st + 8b + 4(g>>1) + 0..3}, b = 0, 1: the key order of the
         // P^T accumulator rows.
@@ -353,13 +377,46 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_gqa_bf16_kernel(AttnArgs 
         for (int st = 0; st < 2 * NKB; ++st) {
 #pragma unroll
             for (int db = 0; db < DB; ++db) {
-                const bf16x8 vf = v_operand(vs_src, st, db);
+                const bf16x8 vf = v_value(v_read(vs_src, st, db), es);
 #pragma unroll
                 for (int qb = 0; qb < QB; ++qb)
                     o[db][qb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pb[qb][st], o[db][qb], 0, 0, 0);
             }
         }
-        sched_reads_mfma<2 * NKB * DB, 2, QB>();
+        if constexpr (!Q8) sched_reads_mfma<2 * NKB * DB, 2, QB>();
+    };
+    // The same in 8 bits for a tile that has NaN codes and keys that some row does not
+    // see: a NaN reaches only the rows that see its key.
+    auto nan_codes = [&](const auto* vs_src) __attribute__((always_inline)) {
+        uint32_t nans = 0;
+#pragma unroll
+        for (int q = 0; q < 2 * DB; ++q) {
+            const auto w = v_read(vs_src, q / DB, q % DB);
+            nans |= q8_nan_bytes(w[0]) | q8_nan_bytes(w[1]);
+        }
+        return __builtin_amdgcn_ballot_w64(nans != 0) != 0;
+    };
+    auto pv_nan = [&](const auto* vs_src, uint32_t es, int t0, const bf16x8 (&pb)[QB][2 * NKB]) __attribute__((always_inline)) {
+        static_assert(QB == 1 && NKB == 1, "one row block and key block");
+#pragma unroll
+        for (int st = 0; st < 2; ++st) {
+            f32x8 seen;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int key = t0 + st * 16 + (e >> 2) * 8 + hl * 4 + (e & 3);
+                seen[e] = key < row_end[0] && key >= row_start[0] ? 1.0f : 0.0f;
+            }
+            const bf16x8 sees = __builtin_convertvector(seen, bf16x8);
+#pragma unroll
+            for (int db = 0; db < DB; ++db) {
+                bf16x8 vf, nf;
+                q8_split_nan(v_read(vs_src, st, db), q8_v_scale(es), vf, nf);
+                o[db][0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pb[0][st], o[db][0], 0, 0, 0);
+                const f32x16 n = __builtin_amdgcn_mfma_f32_32x32x16_bf16(nf, sees, f32x16{}, 0, 0, 0);
+#pragma unroll
+                for (int r = 0; r < 16; ++r) o[db][0][r] = n[r] > 0.f ? __builtin_nanf("") : o[db][0][r];
+            }
+        }
     };
 
     // Processing order.  The pipelined schedule takes the F tiles that need
@@ -374,6 +431,22 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_gqa_bf16_kernel(AttnArgs 
         const int t = i < F ? i + n_lead : (i < F + n_lead ? i - F : i);
         return k_begin + t * BN;
     };
+
+    // In 8 bits: the exponents of the tiles' scales, for the tiles from `first` on.
+    ScaleWindow scale_win;
+    auto load_scales = [&](int first) __attribute__((always_inline)) {
+        if constexpr (Q8) scale_win.load(a, sa, seq, layer, kvh, first, n_tiles, key_of);
+    };
+    auto more_scales = [&](int first, int last) __attribute__((always_inline)) {   // tiles first .. last are next
+        if constexpr (Q8) {
+            if (!scale_win.holds(first, last)) load_scales(first);
+        }
+    };
+    auto exponents = [&](int i) __attribute__((always_inline)) -> uint32_t {
+        if constexpr (Q8) return scale_win.at(i);
+        else return 0u;
+    };
+    load_scales(0);
 
     // Tiles are staged through NS LDS stages: tile i lives in stage i % NS
     // and is issued NS-1 tiles ahead of its use.  Wait until at most
@@ -401,20 +474,28 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_gqa_bf16_kernel(AttnArgs 
         const int ahead = i + NS - 1;
         if (ahead < n_tiles) issue(key_of(ahead), kst((S + NS - 1) % NS), vst((S + NS - 1) % NS));
         f32x16 sc[NKB][QB];
-        qk(kst(S), sc);
-        bf16x8 pb[QB][2 * NKB];
         const int t0 = key_of(i);
+        const uint32_t es = exponents(i);
+        qk(kst(S), es, sc);
+        bf16x8 pb[QB][2 * NKB];
         if (t0 + BN > wmin || t0 < wsmax) {
             row_max(t0, sc, std::true_type{});
             probs(t0, sc, pb, std::true_type{});
+            if constexpr (Q8) {
+                if (nan_codes(vst(S))) {
+                    pv_nan(vst(S), es, t0, pb);
+                    return;
+                }
+            }
         } else {
             row_max(t0, sc, std::false_type{});
             probs(t0, sc, pb, std::false_type{});
         }
-        pv(vst(S), pb);
+        pv(vst(S), es, pb);
     };
     auto plain_from = [&](int first) __attribute__((always_inline)) {
         for (int t = first - first % NS; t < n_tiles; t += NS) {
+            more_scales(t, t + NS - 1);
             static_for<0, NS>([&](auto s_tag) {
                 const int i = t + decltype(s_tag)::value;
                 if (i >= first && i < n_tiles) plain_tile(i, s_tag);
@@ -454,19 +535,23 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_gqa_bf16_kernel(AttnArgs 
         // Written as fenced groups of one K operand's MFMAs, their share of
         // the VALU work and the operand read kAhead steps ahead, so
         // the LDS reads stay in flight across MFMAs.
-        auto seg1 = [&](const uint16_t* ks_src, int kbn, f32x16 (&cur)[QB], f32x16 (&nxt)[QB],
+        // (In 8 bits an operand is converted one group ahead of its MFMAs.)
+        auto seg1 = [&](const Elem* ks_src, uint32_t es, int kbn, f32x16 (&cur)[QB], f32x16 (&nxt)[QB],
                         bf16x8 (&pb)[QB][2]) __attribute__((always_inline)) {
-            constexpr int A = kAhead < KS ? kAhead : KS;
+            constexpr int A = kAhead < KR ? kAhead : KR;
             constexpr int PER_K = 16 / KS;   // probabilities per k-step and row block
-            bf16x8 kop[KS];
+            decltype(k_read(ks_src, 0, kbn)) kop[KR];
 #pragma unroll
-            for (int q = 0; q < A; ++q) kop[q] = k_operand(ks_src, q, kbn);
+            for (int q = 0; q < A; ++q) kop[q] = k_read(ks_src, q, kbn);
             __builtin_amdgcn_sched_barrier(0);
+            bf16x8 kf;
+            if constexpr (Q8) kf = k_value(kop[0], 0, es);
 #pragma unroll
             for (int q = 0; q < KS; ++q) {
 #pragma unroll
                 for (int qb = 0; qb < QB; ++qb) {
-                    nxt[qb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kop[q], qf[qb][q], q == 0 ? f32x16{} : nxt[qb],
+                    if constexpr (!Q8) kf = kop[q];
+                    nxt[qb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[qb][q], q == 0 ? f32x16{} : nxt[qb],
                                                                      0, 0, 0);
                     const float neg_m = -m_run[qb];
 #pragma unroll
@@ -482,7 +567,10 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_gqa_bf16_kernel(AttnArgs 
                         }
                     }
                 }
-                if (q + A < KS) kop[q + A] = k_operand(ks_src, q + A, kbn);
+                if (q % KQ == KQ - 1 && q / KQ + A < KR) kop[q / KQ + A] = k_read(ks_src, q / KQ + A, kbn);
+                if constexpr (Q8) {
+                    if (q + 1 < KS) kf = k_value(kop[(q + 1) / KQ], q + 1, es);
+                }
                 __builtin_amdgcn_sched_barrier(0);
             }
         };
@@ -490,16 +578,18 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_gqa_bf16_kernel(AttnArgs 
         // Segment 2: O^T += V^T P^T for key block kbc of the V stage; the row
         // maxima of nxt (over both lanes of a row, into mx) and the row sums
         // of pb alongside, in fenced groups as in segment 1.
-        auto seg2 = [&](const uint16_t* vs_src, int kbc, const bf16x8 (&pb)[QB][2], const f32x16 (&nxt)[QB],
+        auto seg2 = [&](const Elem* vs_src, uint32_t es, int kbc, const bf16x8 (&pb)[QB][2], const f32x16 (&nxt)[QB],
                         float (&mx)[QB]) __attribute__((always_inline)) {
             constexpr int NQ = 2 * DB;                 // V operands: two 16-key steps x DB channel blocks
             constexpr int A = kAhead < NQ ? kAhead : NQ;
             constexpr int PER_M = 16 / NQ;             // maxima per operand and row block
             constexpr int PER_D = 8 / NQ > 0 ? 8 / NQ : 1;   // sum steps per operand and row block
-            bf16x8 vop[NQ];
+            decltype(v_read(vs_src, 0, 0)) vop[NQ];
 #pragma unroll
-            for (int q = 0; q < A; ++q) vop[q] = v_operand(vs_src, 2 * kbc + q / DB, q % DB);
+            for (int q = 0; q < A; ++q) vop[q] = v_read(vs_src, 2 * kbc + q / DB, q % DB);
             __builtin_amdgcn_sched_barrier(0);
+            bf16x8 vf;
+            if constexpr (Q8) vf = v_value(vop[0], es);
             float m0[QB], m1[QB], l0[QB], l1[QB];
 #pragma unroll
             for (int qb = 0; qb < QB; ++qb) {
@@ -513,7 +603,8 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_gqa_bf16_kernel(AttnArgs 
                 const int h = q / DB, db = q % DB;
 #pragma unroll
                 for (int qb = 0; qb < QB; ++qb) {
-                    o[db][qb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vop[q], pb[qb][h], o[db][qb], 0, 0, 0);
+                    if constexpr (!Q8) vf = vop[q];
+                    o[db][qb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pb[qb][h], o[db][qb], 0, 0, 0);
 #pragma unroll
                     for (int r = q * PER_M; r < (q + 1) * PER_M; r += 2) {
                         m0[qb] = fmaxf(m0[qb], nxt[qb][r]);
@@ -527,7 +618,10 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_gqa_bf16_kernel(AttnArgs 
                         else l0[qb] = __builtin_amdgcn_fdot2_f32_bf16((bf16x2){pp[e], pp[e + 1]}, ones, l0[qb], false);
                     }
                 }
-                if (q + A < NQ) vop[q + A] = v_operand(vs_src, 2 * kbc + (q + A) / DB, (q + A) % DB);
+                if (q + A < NQ) vop[q + A] = v_read(vs_src, 2 * kbc + (q + A) / DB, (q + A) % DB);
+                if constexpr (Q8) {
+                    if (q + 1 < NQ) vf = v_value(vop[q + 1], es);
+                }
                 __builtin_amdgcn_sched_barrier(0);
             }
 #pragma unroll
@@ -559,17 +653,18 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_gqa_bf16_kernel(AttnArgs 
 
         // One step: scores of the next tile from ks_next, the current tile's
         // probabilities and PV from vs_cur.
-        auto half_step = [&](const uint16_t* ks_next, int kbn, const uint16_t* vs_cur, int kbc, f32x16 (&cur)[QB],
-                             f32x16 (&nxt)[QB]) __attribute__((always_inline)) {
+        auto half_step = [&](const Elem* ks_next, uint32_t es_next, int kbn, const Elem* vs_cur, uint32_t es_cur, int kbc,
+                             f32x16 (&cur)[QB], f32x16 (&nxt)[QB]) __attribute__((always_inline)) {
             bf16x8 pb[QB][2];
             float mx[QB];
-            seg1(ks_next, kbn, cur, nxt, pb);
+            seg1(ks_next, es_next, kbn, cur, nxt, pb);
             __builtin_amdgcn_s_setprio(1);
-            seg2(vs_cur, kbc, pb, nxt, mx);
+            seg2(vs_cur, es_cur, kbc, pb, nxt, mx);
             __builtin_amdgcn_s_setprio(0);
             move_max(mx);
         };
 
+        uint32_t es_cur = 0;   // exponents of the tile whose scores are held
         auto iteration = [&](int i, auto u_tag, f32x16 (&cur)[QB], f32x16 (&nxt)[QB]) __attribute__((always_inline)) {
             constexpr int U = decltype(u_tag)::value;
             wait_outstanding(min(i + NS - 2, n_tiles - 1) - (i + 1));   // tile i+1 has landed
@@ -577,7 +672,9 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_gqa_bf16_kernel(AttnArgs 
             bare_barrier();
             if (i + NS - 1 < n_tiles)
                 issue(key_of(i + NS - 1), kst((U + NS - 1) % NS), vst((U + NS - 1) % NS));
-            half_step(kst((U + 1) % NS), 0, vst(U), 0, cur, nxt);
+            const uint32_t es = es_cur;
+            es_cur = exponents(i + 1);
+            half_step(kst((U + 1) % NS), es_cur, 0, vst(U), es, 0, cur, nxt);
         };
 
         // Last pipelined tile: probabilities and PV without overlap; issues
@@ -611,7 +708,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_gqa_bf16_kernel(AttnArgs 
             for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int db = 0; db < DB; ++db) {
-                    const bf16x8 vf = v_operand(vst(U), h, db);
+                    const bf16x8 vf = v_value(v_read(vst(U), h, db), es_cur);
 #pragma unroll
                     for (int qb = 0; qb < QB; ++qb)
                         o[db][qb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pb[qb][h], o[db][qb], 0, 0, 0);
@@ -623,12 +720,13 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_gqa_bf16_kernel(AttnArgs 
             wait_outstanding(min(NS - 2, n_tiles - 1));
             lds_reads_done();
             bare_barrier();
+            es_cur = exponents(0);
             // scores of tile 0 and their maxima
 #pragma unroll
             for (int qb = 0; qb < QB; ++qb) sA[qb] = f32x16{};
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
-                const bf16x8 kf = k_operand(kst(0), ks, 0);
+                const bf16x8 kf = k_value(k_read(kst(0), ks / KQ, 0), ks, es_cur);
 #pragma unroll
                 for (int qb = 0; qb < QB; ++qb)
                     sA[qb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[qb][ks], sA[qb], 0, 0, 0);
@@ -647,6 +745,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_gqa_bf16_kernel(AttnArgs 
                 move_max(mx);
             }
             for (int t = 0; t + 1 < F; t += NS) {
+                more_scales(t, t + NS);
                 static_for<0, NS>([&](auto u_tag) {
                     constexpr int u = decltype(u_tag)::value;
                     const int i = t + u;
@@ -709,28 +808,35 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_gqa_bf16_kernel(AttnArgs 
     }
 }
 
-template <int D, bool PAGED>
-hipError_t launch_d(const AttnArgs& a, const Plan& p, dim3 grid, hipStream_t stream) {
+template <int D, bool PAGED, bool Q8>
+hipError_t launch_d(const AttnArgs& a, const Plan& p, const ScaleArg<Q8>& sa, dim3 grid, hipStream_t stream) {
     if (p.nw != kWaves || p.qb != kQB || p.ns != kStages) return hipErrorInvalidValue;
     const dim3 block(kWaves * 64);
     if (p.longest_first)
-        hipLaunchKernelGGL((attn_gqa_bf16_kernel<D, PAGED, kOrdered>), grid, block, 0, stream, a, p);
+        hipLaunchKernelGGL((attn_gqa_bf16_kernel<D, PAGED, kOrdered, Q8>), grid, block, 0, stream, a, p, sa);
     else if ((int64_t)a.max_q * p.G < p.BM)
-        hipLaunchKernelGGL((attn_gqa_bf16_kernel<D, PAGED, kFew>), grid, block, 0, stream, a, p);
+        hipLaunchKernelGGL((attn_gqa_bf16_kernel<D, PAGED, kFew, Q8>), grid, block, 0, stream, a, p, sa);
     else
-        hipLaunchKernelGGL((attn_gqa_bf16_kernel<D, PAGED, kFull>), grid, block, 0, stream, a, p);
+        hipLaunchKernelGGL((attn_gqa_bf16_kernel<D, PAGED, kFull, Q8>), grid, block, 0, stream, a, p, sa);
     return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_attn_gqa_bf16(const AttnArgs& a, const Plan& p, dim3 grid, hipStream_t stream) {
-    if (a.block_table) {
-        if (a.head_dim == 64) return launch_d<64, true>(a, p, grid, stream);
-        return launch_d<128, true>(a, p, grid, stream);
+hipError_t launch_attn_gqa_bf16(const AttnArgs& a, const Plan& p, const BlockScales* scales, dim3 grid,
+                                hipStream_t stream) {
+    if (scales) {
+        const ScaleArg<true> sa{*scales};
+        return a.head_dim == 64 ? launch_d<64, true, true>(a, p, sa, grid, stream)
+                                : launch_d<128, true, true>(a, p, sa, grid, stream);
     }
-    if (a.head_dim == 64) return launch_d<64, false>(a, p, grid, stream);
-    return launch_d<128, false>(a, p, grid, stream);
+    const ScaleArg<false> none;
+    if (a.block_table) {
+        if (a.head_dim == 64) return launch_d<64, true, false>(a, p, none, grid, stream);
+        return launch_d<128, true, false>(a, p, none, grid, stream);
+    }
+    if (a.head_dim == 64) return launch_d<64, false, false>(a, p, none, grid, stream);
+    return launch_d<128, false, false>(a, p, none, grid, stream);
 }
 
 }  // namespace pkv

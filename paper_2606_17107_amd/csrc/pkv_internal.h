@@ -62,7 +62,120 @@ struct SpliceArgs {
 
 hipError_t launch_splice(const SpliceArgs& a, hipStream_t stream);
 
+// ---- reposition + splice into a cache held in 8 bits ---------------------------
+
+struct StoreSegment {   // same layout as pkv_segment_quant in pkv.h
+    int64_t src_slot0;
+    int32_t seq;
+    int32_t n_tokens;
+    int32_t src_pos0;
+    int32_t dst_pos0;
+};
+
+struct StoreArgs {
+    const char* src_k;
+    const char* src_v;        // may be null
+    uint8_t* dst_k;
+    uint8_t* dst_v;
+    const StoreSegment* segs;
+    int32_t n_segs;
+    int32_t max_seg_tokens;
+    const int32_t* kv_len;    // slots in use before the call, per sequence
+    int32_t n_seqs;
+    int32_t elem_bytes;       // of the source: 2 (bf16) or 4 (fp32)
+    int32_t rope_style;
+    int32_t n_layers;
+    int32_t n_kv_heads;
+    int32_t head_dim;
+    int32_t rope_offset;
+    int32_t rope_dim;
+    int64_t n_src;            // source slots
+    int64_t dst_capacity;     // logical slots per sequence
+    double theta;
+    const double* omega;      // host, rope_dim/2 per-pair frequencies, or null (theta schedule)
+    int64_t src_k_stride[3];  // elements
+    int64_t src_v_stride[3];
+    int64_t dst_k_stride[3];  // bytes
+    int64_t dst_v_stride[3];
+    int32_t* err_flag;
+    const int32_t* block_table;
+    const int32_t* v_block_table;  // may be null (block_table)
+    int32_t page_shift;
+    int32_t max_pages;
+    int64_t n_pages;
+    int64_t dst_k_page_stride;
+    int64_t dst_v_page_stride;
+    int32_t block_tokens;     // 32, 64 or 128
+    uint8_t* k_scale;
+    uint8_t* v_scale;
+    int64_t k_scale_stride[4];   // {layer, head, page, block in page}
+    int64_t v_scale_stride[4];
+};
+
+bool store_fits(const StoreArgs& a);   // the launch is within the grid's limits
+hipError_t launch_store(const StoreArgs& a, hipStream_t stream);
+
+// ---- pages -----------------------------------------------------------------------
+
+// One tensor of a page pool as the copies see it: a page of a layer is `slots` runs
+// of `heads` rows; row bytes are moved in units of 2^unit_shift bytes.
+struct PageTensor {
+    char* data;
+    int64_t layer_stride, page_stride, slot_stride, head_stride;   // bytes
+    int32_t layers, slots, heads;
+    int32_t row_units;        // units of one row
+    int32_t unit_shift;       // 0 .. 4
+    int32_t slot_tokens;      // cache slots of one of `slots`
+};
+struct PageMove {
+    int32_t src, dst;
+    int32_t tokens;           // live slots of the page
+    int32_t ref;
+};
+struct PageFork {   // same layout as pkv_fork in pkv.h
+    int32_t parent, child, n_tokens, reserved;
+};
+struct PagesArgs {
+    PageTensor tensors[4];
+    int32_t n_tensors;
+    int32_t page_size, page_shift;
+    int32_t n_seqs, max_pages;
+    int64_t n_pages;
+    int32_t* err_flag;
+    const int32_t* ref_in;
+    int32_t* ref;             // counts (fork, free), new counts (compact)
+    const int32_t* table_in;
+    int32_t* table;
+    const PageFork* forks;
+    int32_t n;                // forks, or sequences to free
+    const int32_t* seqs;
+    const int32_t* keep;
+    int32_t* n_used;
+    // workspace
+    int32_t* head;            // [0]: number of moves
+    PageMove* moves;
+    int32_t* pages;           // fork: a new page per fork, -1 none, -2 skipped; compact: new index per page, -1 free
+    int32_t* found;           // fork: free pages in ascending order
+    int32_t* claim;           // fork: lowest record that names the row as its child
+};
+
+size_t pages_workspace_bytes(const PagesArgs& a, int n_forks);   // n_forks 0: of a compaction
+void pages_set_workspace(PagesArgs& a, int n_forks, void* ws);
+hipError_t launch_pages_free(const PagesArgs& a, hipStream_t stream);
+hipError_t launch_pages_fork(const PagesArgs& a, hipStream_t stream);
+hipError_t launch_pages_compact(const PagesArgs& a, hipStream_t stream);
+
 // ---- suffix attention --------------------------------------------------------
+
+// Addresses and strides of the block scales of a cache held in 8 bits: one byte e
+// per block of slots, KV head, layer and tensor, for 2^(e - 127).
+struct BlockScales {
+    const uint8_t* k;
+    const uint8_t* v;
+    int64_t k_stride[4];   // {layer, head, page, block in page}
+    int64_t v_stride[4];
+    int32_t block_shift;   // log2 of the slots that share a scale
+};
 
 struct AttnArgs {
     const void* q;
@@ -76,7 +189,7 @@ struct AttnArgs {
     float* lse_out;           // may be null
     float* ws_o;              // split partial outputs (fp32) or null
     float* ws_lse;            // split partial log-sum-exp (fp32) or null
-    int32_t dtype;            // 0 bf16, 1 fp32
+    int32_t dtype;            // 0 bf16, 1 fp32, 2 bf16 queries and outputs over a paged cache of E4M3 codes
     int32_t variant;          // 0 GQA, 1 MLA
     int32_t n_layers;
     int32_t n_seqs;
@@ -110,6 +223,6 @@ struct AttnArgs {
 // Split plan shared by the workspace query and the launcher.
 int attention_splits(const AttnArgs& a);
 size_t attention_workspace_bytes(const AttnArgs& a, int n_splits);
-hipError_t launch_attention(const AttnArgs& a, hipStream_t stream);
+hipError_t launch_attention(const AttnArgs& a, const BlockScales* scales, hipStream_t stream);   // scales: dtype 2
 
 }  // namespace pkv

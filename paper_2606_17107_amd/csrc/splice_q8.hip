@@ -1,0 +1,418 @@
+// Reposition + splice into a cache held in 8 bits: re-rotate a chunk's keys by
+// delta = dst_pos - src_pos as splice.hip does, quantise keys and values to E4M3
+// codes with one power-of-two scale per block of slots, KV head, layer and tensor,
+// and write codes and scales into the paged destination.
+//
+// For a block that receives the rows x_t and keeps the rows that it held before in
+// other slots below the sequence's length:
+//     need = the smallest e in [1, 254] with max |x_t| <= 448 * 2^(e - 127)
+//     e    = need, or max(need, old e) if the block keeps a row
+//     code = E4M3(x_t * 2^(127 - e))  to the nearest, ties to even
+// and where e grew, kept codes become E4M3(code * 2^(old e - e)).  Products with
+// powers of two are exact, so each stored value is rounded once; a kept row loses
+// nothing but what falls below E4M3's smallest step.  A NaN or an infinity is
+// stored as NaN (E4M3 has no infinity) and does not enter the maximum.
+//
+// Design (a stream of 2 or 4 bytes read and 1 written per element):
+//   * A wave owns 32 slots of one (layer, tensor, KV head): 8 lanes a row at head
+//     size 128, two 8-channel chunks a lane (the two halves of its rotary pairs), all
+//     of its rows in registers as fp32 between the maximum and the codes, so the
+//     source is read once.  Blocks of 64 and 128 slots are 2 and 4 waves of one
+//     workgroup that exchange their maxima through LDS; with blocks of 32 slots the
+//     four waves of a workgroup take four heads.
+//   * A block is written by one owner, the first segment (by number) that touches
+//     it; the owner gathers the rows of all segments that end or begin there, so that
+//     chunks spliced back to back in one call share a block's scale.  Every wave finds
+//     the segments by looking through the records, 64 at a time.
+//   * cos and sin come from fp64 (angle, reduction by pi/2 and Taylor series) and are
+//     rounded to fp32 once: an E4M3 code depends on the rotated value's last bits only
+//     near a rounding boundary, and there the fp32 rotation decides as exactly as it can.
+#include <math.h>
+
+#include "attn_columns.h"
+
+namespace pkv {
+namespace {
+
+constexpr int kWaves = 4;
+constexpr int kSub = 32;           // slots per wave
+constexpr int kPairs = 64;         // most rotary pairs of a row
+constexpr int64_t kMaxGridX = 0xffffffffll / (kWaves * 64);   // blocks: HIP refuses 2^32 threads in one dimension
+
+struct Freqs {
+    double w[kPairs];
+};
+
+// Launch geometry: workgroup (x, y) takes units ((y * parts + part) * per_wg ..) of
+// spot x / parts, where a spot is a segment's k-th block and a unit one (layer,
+// tensor, head); the parts of a row of heads are neighbours.
+struct StoreGeo {
+    int seg0;              // first segment of this launch
+    int spots_per_seg;     // blocks of the longest segment
+    int parts;             // workgroups that share the heads of a slot
+    int units;             // layers x tensors x heads
+    int tensors;           // 2, or 1 without values
+    int rope_c0, rope_nc;  // rotary chunks of 8 channels: first, number
+};
+
+__device__ inline uint32_t pack4(float a, float b, float c, float d) {
+    const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, lo, true);
+}
+__device__ inline float exp2_int(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }   // -126 <= e <= 127
+
+// cos and sin of delta * omega, fp64 throughout and rounded once.
+__device__ inline void turn(int64_t delta, double omega, float& c, float& s) {
+    const double x = (double)delta * omega;
+    const double k = rint(x * 0.63661977236758134308);            // 2/pi
+    double r = fma(-k, 1.5707963267948966192, x);                // pi/2, leading part
+    r = fma(-k, 6.123233995736766036e-17, r);                    // pi/2, trailing part
+    const double z = r * r;
+    double ps = fma(z, 1.0 / 6227020800.0, -1.0 / 39916800.0);   // 1/13!, -1/11!
+    ps = fma(z, ps, 1.0 / 362880.0);
+    ps = fma(z, ps, -1.0 / 5040.0);
+    ps = fma(z, ps, 1.0 / 120.0);
+    ps = fma(z, ps, -1.0 / 6.0);
+    const double sr = fma(r * z, ps, r);
+    double pc = fma(z, -1.0 / 87178291200.0, 1.0 / 479001600.0);   // -1/14!, 1/12!
+    pc = fma(z, pc, -1.0 / 3628800.0);
+    pc = fma(z, pc, 1.0 / 40320.0);
+    pc = fma(z, pc, -1.0 / 720.0);
+    pc = fma(z, pc, 1.0 / 24.0);
+    pc = fma(z, pc, -0.5);
+    const double cr = fma(z, pc, 1.0);
+    const int q = (int)((int64_t)k & 3);
+    const float sa = (float)((q & 1) ? cr : sr);
+    const float ca = (float)((q & 1) ? sr : cr);
+    s = (q & 2) ? -sa : sa;
+    c = ((q + 1) & 2) ? -ca : ca;
+}
+
+// Eight channels of a source row as fp32.
+template <bool F32>
+__device__ inline void load8(const char* p, float* x) {
+    if constexpr (F32) {
+        const f32x4 a = *(const f32x4*)p, b = *(const f32x4*)(p + 16);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[i] = a[i];
+            x[4 + i] = b[i];
+        }
+    } else {
+        const u32x4 a = *(const u32x4*)p;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[2 * i] = __uint_as_float(a[i] << 16);
+            x[2 * i + 1] = __uint_as_float(a[i] & 0xffff0000u);
+        }
+    }
+}
+
+// D: head size.  SUBS: waves (of 32 slots) per scale block.  INTER: interleaved pairs.
+template <int D, int SUBS, bool F32, bool INTER>
+__global__ __launch_bounds__(kWaves * 64) void store_kernel(StoreArgs a, StoreGeo g, Freqs ft) {
+    constexpr int LPT = D / 16;           // lanes per row
+    constexpr int TPS = 64 / LPT;         // rows per step
+    constexpr int STEPS = kSub / TPS;
+    constexpr int BT = SUBS * kSub;       // slots per scale block
+    constexpr int EB = F32 ? 4 : 2;
+    __shared__ int top_lds[2][kWaves], any_lds[2][kWaves];
+
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63;
+    const int spot = (int)(blockIdx.x / (uint32_t)g.parts), part = (int)(blockIdx.x - (uint32_t)spot * g.parts);
+    const int seg_i = g.seg0 + spot / g.spots_per_seg, k0 = spot % g.spots_per_seg;
+    const int unit = (blockIdx.y * g.parts + part) * (kWaves / SUBS) + wave / SUBS;
+    const bool working = unit < g.units;   // the others only meet the barriers
+    const int sub = wave % SUBS;
+    const int head = working ? unit % a.n_kv_heads : 0;
+    const int rest = working ? unit / a.n_kv_heads : 0;
+    const int tensor = rest % g.tensors, layer = rest / g.tensors;
+    const bool is_k = tensor == 0;
+
+    const StoreSegment mine = a.segs[seg_i];
+    const bool teller = blockIdx.y == 0 && part == 0 && threadIdx.x == 0 && k0 == 0;   // reports what is out of range
+    auto flag = [&]() __attribute__((always_inline)) {
+        if (a.err_flag) *a.err_flag = 1;
+    };
+    const int64_t end = (int64_t)mine.dst_pos0 + mine.n_tokens;   // one past the last destination slot
+    if (mine.n_tokens <= 0) return;
+    if (teller && (mine.seq < 0 || mine.seq >= a.n_seqs || mine.dst_pos0 < 0 || end > a.dst_capacity ||
+                   mine.src_slot0 < 0 || mine.src_slot0 > a.n_src - mine.n_tokens))
+        flag();
+    if (mine.seq < 0 || mine.seq >= a.n_seqs) return;
+    const int live = a.kv_len[mine.seq];
+
+    // This lane's chunks of 8 channels: rotary lanes hold a chunk and its partner.
+    const int cl = lane % LPT, row0 = lane / LPT;
+    const int half_r = is_k ? g.rope_nc >> 1 : 0;
+    const bool rope = cl < half_r;
+    int ca, cb;
+    if (rope) {
+        ca = g.rope_c0 + cl;
+        cb = ca + half_r;
+    } else if (is_k) {
+        const int i0 = cl - half_r, i1 = i0 + ((D / 8 - g.rope_nc) >> 1);
+        ca = i0 < g.rope_c0 ? i0 : i0 + g.rope_nc;
+        cb = i1 < g.rope_c0 ? i1 : i1 + g.rope_nc;
+    } else {
+        ca = cl;
+        cb = cl + LPT;
+    }
+    const char* const src = (is_k ? a.src_k : a.src_v) + ((int64_t)layer * (is_k ? a.src_k_stride[0] : a.src_v_stride[0]) +
+                                                          (int64_t)head * (is_k ? a.src_k_stride[1] : a.src_v_stride[1])) * EB;
+    const int64_t src_row = (is_k ? a.src_k_stride[2] : a.src_v_stride[2]) * EB;
+    uint8_t* const dst = (is_k ? a.dst_k : a.dst_v) + (int64_t)layer * (is_k ? a.dst_k_stride[0] : a.dst_v_stride[0]) +
+                         (int64_t)head * (is_k ? a.dst_k_stride[1] : a.dst_v_stride[1]);
+    const int64_t dst_row = is_k ? a.dst_k_stride[2] : a.dst_v_stride[2];
+    const int64_t dst_page = is_k ? a.dst_k_page_stride : a.dst_v_page_stride;
+    const int32_t* const table =
+        (!is_k && a.v_block_table ? a.v_block_table : a.block_table) + (int64_t)mine.seq * a.max_pages;
+    uint8_t* const scales = (is_k ? a.k_scale : a.v_scale) + (int64_t)layer * (is_k ? a.k_scale_stride[0] : a.v_scale_stride[0]) +
+                            (int64_t)head * (is_k ? a.k_scale_stride[1] : a.v_scale_stride[1]);
+
+    // The segment's blocks k0, k0 + spots_per_seg, .. (one, unless a segment is longer than the stated bound).
+    int turn_no = 0;
+#pragma unroll 1
+    for (int64_t b = max((int64_t)mine.dst_pos0, (int64_t)0) / BT + k0; b * BT < min(end, a.dst_capacity);
+         b += g.spots_per_seg, turn_no ^= 1) {
+        const int64_t slot0 = b * BT;                       // the block's first slot
+        const int first = (int)slot0 + sub * kSub + row0;   // this lane's slots: first, + TPS, ..
+        const int64_t block_end = min(slot0 + BT, a.dst_capacity);
+        const int entry = (int)(slot0 >> a.page_shift);
+        const int page = table[entry];
+        const bool in_pool = (int64_t)page >= 0 && (int64_t)page < a.n_pages;
+        if (working && !in_pool && sub == 0 && lane == 0) flag();
+        const int64_t at = (int64_t)(in_pool ? page : 0);
+        const int inside = (int)(slot0 & ((1 << a.page_shift) - 1));
+        uint8_t* const scale_at = scales + at * (is_k ? a.k_scale_stride[2] : a.v_scale_stride[2]) +
+                                  (inside / BT) * (is_k ? a.k_scale_stride[3] : a.v_scale_stride[3]);
+        const int old = working ? (int)*scale_at : 0;
+        uint8_t* const rows = dst + at * dst_page + (int64_t)(inside + sub * kSub + row0) * dst_row;
+
+        float x[STEPS][16];
+        bool has[STEPS];
+#pragma unroll
+        for (int t = 0; t < STEPS; ++t) {
+            has[t] = false;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[t][i] = 0.f;
+        }
+        // Every segment that touches the block, by number; the first one owns it.
+        bool owner = true, found = false;
+#pragma unroll 1
+        for (int j0 = 0; j0 < a.n_segs && owner; j0 += 64) {
+            const int j = j0 + lane;
+            bool touches = false;
+            if (j < a.n_segs) {
+                const StoreSegment s = a.segs[j];
+                touches = s.seq == mine.seq && s.n_tokens > 0 && s.dst_pos0 < block_end &&
+                          (int64_t)s.dst_pos0 + s.n_tokens > slot0;
+            }
+            uint64_t hits = __builtin_amdgcn_ballot_w64(touches);
+            while (hits) {
+                const int h = j0 + __builtin_ctzll(hits);
+                hits &= hits - 1;
+                if (!found) {
+                    found = true;
+                    owner = h == seg_i;
+                    if (!owner) break;
+                }
+                const StoreSegment s = a.segs[h];
+                float raw[STEPS][16];
+                bool take[STEPS];
+#pragma unroll
+                for (int t = 0; t < STEPS; ++t) {
+                    const int64_t r = (int64_t)first + t * TPS - s.dst_pos0;
+                    const int64_t from = s.src_slot0 + r;
+                    take[t] = working && !has[t] && r >= 0 && r < s.n_tokens && first + t * TPS < block_end && from >= 0 &&
+                              from < a.n_src;
+                    const char* const p = src + (take[t] ? from : 0) * src_row;
+                    if (take[t]) {
+                        load8<F32>(p + ca * 8 * EB, raw[t]);
+                        load8<F32>(p + cb * 8 * EB, raw[t] + 8);
+                    }
+                }
+                const int64_t delta = (int64_t)s.dst_pos0 - s.src_pos0;
+                if (is_k && delta != 0) {   // uniform
+                    float c1, s1;
+                    turn(delta, ft.w[lane], c1, s1);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        // coefficient i of the lane's chunks: HALF, pairs 8 cl ..; INTERLEAVED, 4 pairs of each chunk
+                        const int pair = INTER ? (i < 4 ? cl * 4 + i : (half_r + cl) * 4 + i - 4) : cl * 8 + i;
+                        const float c = __shfl(c1, pair & 63), sn = __shfl(s1, pair & 63);
+                        const int ia = INTER ? 2 * i : i, ib = INTER ? 2 * i + 1 : i + 8;
+                        if (rope) {
+#pragma unroll
+                            for (int t = 0; t < STEPS; ++t) {
+                                const float u = raw[t][ia], v = raw[t][ib];
+                                raw[t][ia] = fmaf(u, c, -(v * sn));
+                                raw[t][ib] = fmaf(u, sn, v * c);
+                            }
+                        }
+                    }
+                }
+#pragma unroll
+                for (int t = 0; t < STEPS; ++t) {
+                    has[t] = has[t] || take[t];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) x[t][i] = take[t] ? raw[t][i] : x[t][i];
+                }
+            }
+        }
+        if (!owner) continue;   // uniform over the workgroup
+
+        // The largest finite magnitude, and whether the block gets and keeps rows.
+        float m = 0.f;
+#pragma unroll
+        for (int t = 0; t < STEPS; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) m = fmaxf(m, fabsf(x[t][i]));   // (passes over a NaN)
+        if (__builtin_amdgcn_ballot_w64(m == INFINITY) != 0) {
+            m = 0.f;
+#pragma unroll
+            for (int t = 0; t < STEPS; ++t)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) m = fmaxf(m, fabsf(x[t][i]) < INFINITY ? fabsf(x[t][i]) : 0.f);
+        }
+        bool gets = false, keeps = false;
+        bool kept[STEPS];
+#pragma unroll
+        for (int t = 0; t < STEPS; ++t) {
+            kept[t] = working && !has[t] && first + t * TPS < min((int64_t)live, block_end);
+            gets |= has[t];
+            keeps |= kept[t];
+        }
+        int top = wave_max_u((int)__float_as_uint(m));
+        int any = (__builtin_amdgcn_ballot_w64(gets) != 0 ? 1 : 0) | (__builtin_amdgcn_ballot_w64(keeps) != 0 ? 2 : 0);
+        if constexpr (SUBS > 1) {
+            // (two sets of words: a wave may be one block ahead)
+            if (lane == 0) {
+                top_lds[turn_no][wave] = top;
+                any_lds[turn_no][wave] = any;
+            }
+            __syncthreads();
+#pragma unroll
+            for (int w = 0; w < SUBS; ++w) {
+                top = max(top, top_lds[turn_no][wave / SUBS * SUBS + w]);
+                any |= any_lds[turn_no][wave / SUBS * SUBS + w];
+            }
+        }
+        if (!working || !in_pool || !(any & 1)) continue;
+        // 448 = 1.75 * 2^8 is the largest code.
+        const int need = (top >> 23) - 8 + ((top & 0x7fffff) > 0x600000 ? 1 : 0);
+        int e = max(need, 1);
+        if (any & 2) e = max(e, old);
+        const float up = __uint_as_float((uint32_t)(254 - min(e, 254)) << 23);   // 2^(127 - e)
+#pragma unroll
+        for (int t = 0; t < STEPS; ++t) {
+            if (!has[t]) continue;
+            uint8_t* const p = rows + (int64_t)(t * TPS) * dst_row;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const float* y = x[t] + 8 * h;
+                u32x2 w;
+                w[0] = pack4(y[0] * up, y[1] * up, y[2] * up, y[3] * up);
+                w[1] = pack4(y[4] * up, y[5] * up, y[6] * up, y[7] * up);
+                __builtin_nontemporal_store(w, (u32x2*)(p + (h ? cb : ca) * 8));
+            }
+        }
+        if ((any & 2) && e > old) {
+            // 2^(old - e): codes below 2^-18 of the largest one vanish, so no smaller factor is needed
+            const float down = exp2_int(max(old - e, -126));
+#pragma unroll
+            for (int t = 0; t < STEPS; ++t) {
+                if (!kept[t]) continue;
+                uint8_t* const p = rows + (int64_t)(t * TPS) * dst_row;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    u32x2* const q = (u32x2*)(p + (h ? cb : ca) * 8);
+                    u32x2 w = *q;
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[i], false);
+                        const auto hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[i], true);
+                        w[i] = pack4(lo[0] * down, lo[1] * down, hi[0] * down, hi[1] * down);
+                    }
+                    *q = w;
+                }
+            }
+        }
+        if (sub == 0 && lane == 0 && (!(any & 2) || e != old)) *scale_at = (uint8_t)e;
+    }
+}
+
+template <int D, int SUBS>
+void launch_geo(const StoreArgs& a, const StoreGeo& g, const Freqs& f, dim3 grid, hipStream_t stream) {
+    const dim3 block(kWaves * 64);
+    if (a.elem_bytes == 4) {
+        if (a.rope_style) hipLaunchKernelGGL((store_kernel<D, SUBS, true, true>), grid, block, 0, stream, a, g, f);
+        else hipLaunchKernelGGL((store_kernel<D, SUBS, true, false>), grid, block, 0, stream, a, g, f);
+    } else {
+        if (a.rope_style) hipLaunchKernelGGL((store_kernel<D, SUBS, false, true>), grid, block, 0, stream, a, g, f);
+        else hipLaunchKernelGGL((store_kernel<D, SUBS, false, false>), grid, block, 0, stream, a, g, f);
+    }
+}
+
+}  // namespace
+
+namespace {
+
+// Grid of a call: per segment (x) and over the units (y).
+struct StoreGrid {
+    int64_t per_seg, y;
+};
+StoreGrid make_geo(const StoreArgs& a, StoreGeo& g) {
+    const int bt = a.block_tokens, per_wg = kWaves / (bt / kSub);
+    const int64_t longest = a.max_seg_tokens < a.dst_capacity ? a.max_seg_tokens : a.dst_capacity;
+    g.spots_per_seg = (int)((longest + bt - 2) / bt + 1);   // blocks that so many slots can touch
+    g.tensors = a.src_v ? 2 : 1;
+    const int64_t units = (int64_t)a.n_layers * g.tensors * a.n_kv_heads;
+    g.units = units < 0x7fffffff ? (int)units : 0x7fffffff;
+    g.parts = a.n_kv_heads > per_wg ? (a.n_kv_heads + per_wg - 1) / per_wg : 1;
+    g.rope_c0 = a.rope_offset / 8;
+    g.rope_nc = a.rope_dim / 8;
+    const int64_t groups = (units + per_wg - 1) / per_wg;
+    return {(int64_t)g.spots_per_seg * g.parts, (groups + g.parts - 1) / g.parts};
+}
+
+}  // namespace
+
+bool store_fits(const StoreArgs& a) {
+    StoreGeo g;
+    const StoreGrid n = make_geo(a, g);
+    return n.y <= 65535 && n.per_seg <= kMaxGridX;
+}
+
+hipError_t launch_store(const StoreArgs& a, hipStream_t stream) {
+    StoreGeo g;
+    const StoreGrid size = make_geo(a, g);
+    const int subs = a.block_tokens / kSub;
+    Freqs f;
+    if (a.omega) {
+        for (int i = 0; i < kPairs; ++i) f.w[i] = i < a.rope_dim / 2 ? a.omega[i] : 0.0;
+    } else {
+        for (int i = 0; i < kPairs; ++i) f.w[i] = i < a.rope_dim / 2 ? pow(a.theta, -2.0 * i / a.rope_dim) : 0.0;
+    }
+    const int64_t at_once = kMaxGridX / size.per_seg;   // segments per launch
+    for (int64_t s = 0; s < a.n_segs; s += at_once) {
+        const int64_t n = a.n_segs - s < at_once ? a.n_segs - s : at_once;
+        g.seg0 = (int)s;
+        const dim3 grid((unsigned)(n * size.per_seg), (unsigned)size.y);
+        if (a.head_dim == 64) {
+            if (subs == 1) launch_geo<64, 1>(a, g, f, grid, stream);
+            else if (subs == 2) launch_geo<64, 2>(a, g, f, grid, stream);
+            else launch_geo<64, 4>(a, g, f, grid, stream);
+        } else {
+            if (subs == 1) launch_geo<128, 1>(a, g, f, grid, stream);
+            else if (subs == 2) launch_geo<128, 2>(a, g, f, grid, stream);
+            else launch_geo<128, 4>(a, g, f, grid, stream);
+        }
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+}  // namespace pkv

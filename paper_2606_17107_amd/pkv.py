@@ -34,6 +34,7 @@ PKV_ATTN_GQA = 0
 PKV_ATTN_MLA = 1
 
 _i64x3 = ctypes.c_int64 * 3
+_i64x4 = ctypes.c_int64 * 4
 
 
 class pkv_layout(ctypes.Structure):
@@ -73,9 +74,46 @@ class pkv_paged_cache(ctypes.Structure):
     ]
 
 
+class pkv_block_scales(ctypes.Structure):
+    _fields_ = [
+        ("block_tokens", ctypes.c_int32), ("reserved", ctypes.c_int32), ("k_scale", ctypes.c_void_p),
+        ("v_scale", ctypes.c_void_p), ("k_stride", _i64x4), ("v_stride", _i64x4),
+    ]
+
+
+class pkv_segment_quant(ctypes.Structure):
+    _fields_ = [
+        ("src_slot0", ctypes.c_int64), ("seq", ctypes.c_int32), ("n_tokens", ctypes.c_int32),
+        ("src_pos0", ctypes.c_int32), ("dst_pos0", ctypes.c_int32),
+    ]
+
+
+class pkv_page_tensor(ctypes.Structure):
+    _fields_ = [
+        ("data", ctypes.c_void_p), ("layer_stride", ctypes.c_int64), ("page_stride", ctypes.c_int64),
+        ("slot_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64), ("n_layers", ctypes.c_int32),
+        ("n_slots", ctypes.c_int32), ("n_heads", ctypes.c_int32), ("row_bytes", ctypes.c_int32),
+    ]
+
+
+class pkv_page_pool(ctypes.Structure):
+    _fields_ = [
+        ("page_size", ctypes.c_int32), ("n_tensors", ctypes.c_int32), ("n_seqs", ctypes.c_int32),
+        ("max_pages", ctypes.c_int32), ("n_pages", ctypes.c_int64), ("tensors", pkv_page_tensor * 4),
+        ("err_flag", ctypes.c_void_p),
+    ]
+
+
+class pkv_fork(ctypes.Structure):
+    _fields_ = [("parent", ctypes.c_int32), ("child", ctypes.c_int32), ("n_tokens", ctypes.c_int32),
+                ("reserved", ctypes.c_int32)]
+
+
 SYMBOLS = ("pkv_reposition_splice", "pkv_reposition_splice_freqs", "pkv_reposition_splice_paged",
            "pkv_reposition_splice_batched", "pkv_attention_workspace_size", "pkv_suffix_attention",
-           "pkv_suffix_attention_paged", "pkv_suffix_attention_noalloc", "pkv_last_error", "pkv_version")
+           "pkv_suffix_attention_paged", "pkv_suffix_attention_noalloc", "pkv_reposition_splice_quant",
+           "pkv_attention_quant_workspace_size", "pkv_suffix_attention_quant", "pkv_pages_workspace_size", "pkv_pages_free",
+           "pkv_pages_fork", "pkv_pages_compact", "pkv_last_error", "pkv_version")
 PKV_NOALLOC_SCRATCH_BYTES = 64 << 20
 
 _lib = None
@@ -122,6 +160,24 @@ def lib() -> ctypes.CDLL:
     L.pkv_suffix_attention_noalloc.restype = ctypes.c_int
     L.pkv_suffix_attention_noalloc.argtypes = [P, P, P, P, P, P, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32,
                                                ctypes.c_float, ctypes.POINTER(pkv_attn_desc), P]
+    I, F = ctypes.c_int32, ctypes.c_float
+    D, A, S = ctypes.POINTER(pkv_attn_desc), ctypes.POINTER(pkv_paged_cache), ctypes.POINTER(pkv_block_scales)
+    pool = ctypes.POINTER(pkv_page_pool)
+    L.pkv_reposition_splice_quant.restype = ctypes.c_int
+    L.pkv_reposition_splice_quant.argtypes = [P, P, P, P, P, I, I, P, I, ctypes.POINTER(ctypes.c_double), F, I,
+                                           ctypes.POINTER(pkv_layout), A, S, P]
+    L.pkv_attention_quant_workspace_size.restype = ctypes.c_size_t
+    L.pkv_attention_quant_workspace_size.argtypes = [D, I, I, I]
+    L.pkv_suffix_attention_quant.restype = ctypes.c_int
+    L.pkv_suffix_attention_quant.argtypes = [P, P, P, P, P, P, I, I, I, F, D, A, S, P, ctypes.c_size_t, P]
+    L.pkv_pages_workspace_size.restype = ctypes.c_size_t
+    L.pkv_pages_workspace_size.argtypes = [pool, I]
+    L.pkv_pages_free.restype = ctypes.c_int
+    L.pkv_pages_free.argtypes = [pool, P, P, P, P, I, P]
+    L.pkv_pages_fork.restype = ctypes.c_int
+    L.pkv_pages_fork.argtypes = [pool, P, P, P, P, I, P, ctypes.c_size_t, P]
+    L.pkv_pages_compact.restype = ctypes.c_int
+    L.pkv_pages_compact.argtypes = [pool, P, P, P, P, P, P, ctypes.c_size_t, P]
     L.pkv_last_error.restype = ctypes.c_char_p
     L.pkv_last_error.argtypes = []
     L.pkv_version.restype = ctypes.c_int32
@@ -293,6 +349,54 @@ def pkv_suffix_attention_noalloc(q, k_cache, v_cache, out, q_pos, kv_len, n_q_he
         _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(out), _ptr(q_pos), _ptr(kv_len), int(n_q_heads),
         int(n_kv_heads), int(head_dim), float(scale), ctypes.byref(desc) if desc is not None else None,
         _stream(stream))
+
+
+def _ref(struct):
+    return ctypes.byref(struct) if struct is not None else None
+
+
+def _doubles(omega):
+    return None if omega is None else (ctypes.c_double * len(omega))(*[float(x) for x in omega])
+
+
+def pkv_reposition_splice_quant(src_k, src_v, k_pages, v_pages, segs, n_segs, max_seg_tokens, kv_len, n_seqs, omega,
+                             rope_theta, rope_dim, layout, paging, scales, stream=None) -> int:
+    return lib().pkv_reposition_splice_quant(_ptr(src_k), _ptr(src_v), _ptr(k_pages), _ptr(v_pages), _ptr(segs), int(n_segs),
+                                          int(max_seg_tokens), _ptr(kv_len), int(n_seqs), _doubles(omega),
+                                          float(rope_theta), int(rope_dim), _ref(layout), _ref(paging), _ref(scales),
+                                          _stream(stream))
+
+
+def pkv_attention_quant_workspace_size(desc, n_q_heads, n_kv_heads, head_dim) -> int:
+    return int(lib().pkv_attention_quant_workspace_size(_ref(desc), int(n_q_heads), int(n_kv_heads), int(head_dim)))
+
+
+def pkv_suffix_attention_quant(q, k_pages, v_pages, out, q_pos, kv_len, n_q_heads, n_kv_heads, head_dim, scale, desc,
+                            paging, scales, workspace, workspace_bytes, stream=None) -> int:
+    return lib().pkv_suffix_attention_quant(_ptr(q), _ptr(k_pages), _ptr(v_pages), _ptr(out), _ptr(q_pos), _ptr(kv_len),
+                                         int(n_q_heads), int(n_kv_heads), int(head_dim), float(scale), _ref(desc),
+                                         _ref(paging), _ref(scales), _ptr(workspace), int(workspace_bytes),
+                                         _stream(stream))
+
+
+def pkv_pages_workspace_size(pool, n_forks) -> int:
+    return int(lib().pkv_pages_workspace_size(_ref(pool), int(n_forks)))
+
+
+def pkv_pages_free(pool, ref, block_table, seqs, keep, n, stream=None) -> int:
+    return lib().pkv_pages_free(_ref(pool), _ptr(ref), _ptr(block_table), _ptr(seqs), _ptr(keep), int(n),
+                                _stream(stream))
+
+
+def pkv_pages_fork(pool, ref, table_in, table_out, forks, n_forks, workspace, workspace_bytes, stream=None) -> int:
+    return lib().pkv_pages_fork(_ref(pool), _ptr(ref), _ptr(table_in), _ptr(table_out), _ptr(forks), int(n_forks),
+                                _ptr(workspace), int(workspace_bytes), _stream(stream))
+
+
+def pkv_pages_compact(pool, ref_in, ref_out, table_in, table_out, n_used, workspace, workspace_bytes,
+                      stream=None) -> int:
+    return lib().pkv_pages_compact(_ref(pool), _ptr(ref_in), _ptr(ref_out), _ptr(table_in), _ptr(table_out),
+                                   _ptr(n_used), _ptr(workspace), int(workspace_bytes), _stream(stream))
 
 
 def pkv_last_error() -> str:
@@ -498,3 +602,247 @@ def suffix_attention_paged(q, k_pool, v_pool, out, q_pos, kv_len, block_table, s
         _keep_until_done(workspace, stream)
     _check(pkv_suffix_attention_paged(q, k_pool, v_pool, out, q_pos, kv_len, H, Hkv, D, scale, d, pg, workspace,
                                       need, stream))
+
+
+# ---- caches held in 8 bits ---------------------------------------------------
+# Pools as above, of torch.float8_e4m3fn (or torch.uint8) codes; the scales of a
+# pool are [layer][page][block in page][kv_head] bytes e (torch.uint8 or
+# torch.float8_e8m0fnu) for 2^(e - 127).
+
+_CODE_TYPES = tuple(t for t in (torch.uint8, getattr(torch, "float8_e4m3fn", None)) if t is not None)
+_SCALE_TYPES = tuple(t for t in (torch.uint8, getattr(torch, "float8_e8m0fnu", None)) if t is not None)
+
+
+def _check_q8_cache(dev, k_pool, v_pool, k_scale, v_scale, block_table, v_block_table, kv_len) -> None:
+    """Types, shapes and devices of an 8-bit cache; v_pool and v_scale may both be None."""
+    _need(block_table, "block_table", dev, torch.int32, contiguous=True)
+    if block_table.dim() != 2:
+        raise ValueError("block_table is [n_seqs][max_pages]")
+    for pool, scale, name in ((k_pool, k_scale, "k"), (v_pool, v_scale, "v")):
+        if pool is None and scale is None and name == "v":
+            continue
+        for t, what, types, dim in ((pool, "_pool", _CODE_TYPES, 5), (scale, "_scale", _SCALE_TYPES, 4)):
+            if t is None:
+                raise TypeError("%s%s is required" % (name, what))
+            _need(t, name + what, dev)
+            if t.dtype not in types:
+                raise TypeError("%s%s must be one of %s, got %s" % (name, what, types, t.dtype))
+            if t.dim() != dim:
+                raise ValueError("%s%s must have %d dimensions" % (name, what, dim))
+        if pool.shape != k_pool.shape or scale.shape != k_scale.shape:
+            raise ValueError("keys and values have different shapes")
+        L, pages, page, H = pool.shape[:4]
+        if (scale.shape[0], scale.shape[1], scale.shape[3]) != (L, pages, H) or scale.shape[2] < 1 or page % scale.shape[2]:
+            raise ValueError("%s_scale %s does not fit the pool %s" % (name, tuple(scale.shape), tuple(pool.shape)))
+    _need(kv_len, "kv_len", dev, torch.int32, block_table.shape[0], contiguous=True)
+    if v_block_table is not None:
+        _need(v_block_table, "v_block_table", dev, torch.int32, contiguous=True)
+        if v_block_table.shape != block_table.shape:
+            raise ValueError("block_table and v_block_table have different shapes")
+
+
+def make_block_scales(k_scale: torch.Tensor, v_scale: Optional[torch.Tensor], page_size: int) -> pkv_block_scales:
+    """Scales [layer][page][block][kv_head] of pools with pages of page_size slots."""
+    def strides(t):
+        return _i64x4(0, 0, 0, 0) if t is None else _i64x4(t.stride(0), t.stride(3), t.stride(1), t.stride(2))
+
+    return pkv_block_scales(page_size // k_scale.shape[2], 0, k_scale.data_ptr(),
+                            None if v_scale is None else v_scale.data_ptr(), strides(k_scale), strides(v_scale))
+
+
+def make_segments_quant(segs: Sequence[dict], device) -> torch.Tensor:
+    """Pack segment dicts (src_slot0, seq, n_tokens, src_pos0, dst_pos0) into a device buffer of
+    pkv_segment_quant records."""
+    arr = (pkv_segment_quant * max(1, len(segs)))()
+    for i, s in enumerate(segs):
+        arr[i] = pkv_segment_quant(int(s["src_slot0"]), int(s["seq"]), int(s["n_tokens"]), int(s["src_pos0"]),
+                                int(s["dst_pos0"]))
+    return torch.frombuffer(bytearray(bytes(arr)), dtype=torch.uint8).to(device)
+
+
+def make_layout_quant(src_k: torch.Tensor, src_v: Optional[torch.Tensor], k_pool: torch.Tensor,
+                   v_pool: Optional[torch.Tensor], block_table: torch.Tensor, rope_offset: int = 0,
+                   rope_style: int = PKV_ROPE_HALF, dst_capacity: Optional[int] = None,
+                   err_flag: Optional[torch.Tensor] = None) -> pkv_layout:
+    """Layout of a splice of [layer][kv_head][slot][channel] sources into 8-bit pools."""
+    L = make_layout(src_k, src_v, src_k, src_v, rope_offset, rope_style, err_flag=err_flag)
+    L.dst_capacity = block_table.shape[1] * k_pool.shape[2] if dst_capacity is None else int(dst_capacity)
+    L.dst_k_stride = pool_strides3(k_pool)
+    L.dst_v_stride = pool_strides3(v_pool)
+    return L
+
+
+def reposition_splice_quant(src_k, src_v, k_pool, v_pool, k_scale, v_scale, segs_dev, n_segs, max_seg_tokens, kv_len,
+                         block_table, rope_theta, rope_dim, rope_offset=0, rope_style=PKV_ROPE_HALF, omega=None,
+                         dst_capacity=None, err_flag=None, stream=None, v_block_table=None) -> None:
+    """Tensor-level call of pkv_reposition_splice_quant (segs_dev: make_segments_quant; kv_len: the slots in use
+    before the call, one for each row of block_table)."""
+    dev = _gpu_device(src_k, "src_k")
+    _need(src_v, "src_v", dev, src_k.dtype)
+    _need(err_flag, "err_flag", dev, torch.int32, 1)
+    _check_q8_cache(dev, k_pool, v_pool, k_scale, v_scale, block_table, v_block_table, kv_len)
+    if (src_v is None) != (v_pool is None):
+        raise ValueError("src_v and v_pool are given both or not at all")
+    if src_k.dim() != 4 or (src_v is not None and src_v.shape != src_k.shape):
+        raise ValueError("sources are [layer][kv_head][slot][channel], both of one shape")
+    if (src_k.shape[0], src_k.shape[1], src_k.shape[3]) != (k_pool.shape[0], k_pool.shape[3], k_pool.shape[4]):
+        raise ValueError("the source %s does not fit the pool %s" % (tuple(src_k.shape), tuple(k_pool.shape)))
+    if omega is not None and len(omega) < int(rope_dim) // 2:
+        raise ValueError("omega holds %d frequencies, the call reads %d" % (len(omega), int(rope_dim) // 2))
+    _need(segs_dev, "segs_dev", dev, torch.uint8, int(n_segs) * ctypes.sizeof(pkv_segment_quant), contiguous=True)
+    layout = make_layout_quant(src_k, src_v, k_pool, v_pool, block_table, rope_offset, rope_style, dst_capacity, err_flag)
+    _check(pkv_reposition_splice_quant(src_k, src_v, k_pool, v_pool, segs_dev, n_segs, max_seg_tokens, kv_len,
+                                    block_table.shape[0], omega, rope_theta, rope_dim, layout,
+                                    make_paging(block_table, k_pool, v_pool, v_block_table),
+                                    make_block_scales(k_scale, v_scale, k_pool.shape[2]), stream))
+
+
+def make_attn_desc_quant(q: torch.Tensor, k_pool: torch.Tensor, v_pool: torch.Tensor, out: torch.Tensor,
+                      block_table: torch.Tensor, max_kv_len: int, n_seqs: int = 1, cu_q: Optional[torch.Tensor] = None,
+                      max_q: Optional[int] = None, n_splits: int = 0, lse_out: Optional[torch.Tensor] = None,
+                      window: int = 0, cache_slots: Optional[int] = None) -> pkv_attn_desc:
+    """Descriptor for q [L][rows][H][d] over 8-bit pools."""
+    assert q.stride(3) == 1 and out.stride(3) == 1
+    return pkv_attn_desc(_dtype_code(q), PKV_ATTN_GQA, q.shape[0], int(n_seqs), out.shape[3], q.shape[1],
+                         q.shape[1] if max_q is None else int(max_q), int(max_kv_len), int(n_splits), int(window),
+                         None if cu_q is None else cu_q.data_ptr(), None,
+                         block_table.shape[1] * k_pool.shape[2] if cache_slots is None else int(cache_slots),
+                         _i64x3(*q.stride()[:3]), pool_strides3(k_pool), pool_strides3(v_pool),
+                         _i64x3(*out.stride()[:3]), None if lse_out is None else lse_out.data_ptr())
+
+
+def suffix_attention_quant(q, k_pool, v_pool, k_scale, v_scale, out, q_pos, kv_len, block_table, scale, max_kv_len,
+                        n_seqs=1, cu_q=None, max_q=None, n_splits=0, lse_out=None, workspace=None, stream=None,
+                        window=0, cache_slots=None, v_block_table=None) -> None:
+    """Tensor-level call of pkv_suffix_attention_quant (allocates the workspace with torch if not given)."""
+    dev = _gpu_device(q, "q")
+    if out is None or v_pool is None:
+        raise TypeError("out and v_pool are required")
+    _need(out, "out", dev, q.dtype)
+    if q.dim() != 4 or out.shape != q.shape:
+        raise ValueError("q and out are [layer][row][q_head][channel], both of one shape")
+    L, rows, H, D = q.shape
+    _need(q_pos, "q_pos", dev, torch.int32, rows, contiguous=True)
+    _need(cu_q, "cu_q", dev, torch.int32, int(n_seqs) + 1, contiguous=True)
+    _need(lse_out, "lse_out", dev, torch.float32, L * rows * H, contiguous=True)
+    _need(workspace, "workspace", dev, contiguous=True)
+    _check_q8_cache(dev, k_pool, v_pool, k_scale, v_scale, block_table, v_block_table, None)
+    _need(kv_len, "kv_len", dev, torch.int32, int(n_seqs), contiguous=True)
+    if block_table.shape[0] < int(n_seqs):
+        raise ValueError("block_table has %d rows for %d sequences" % (block_table.shape[0], int(n_seqs)))
+    if k_pool.shape[0] != L or k_pool.shape[4] != D:
+        raise ValueError("the pool %s does not fit q %s" % (tuple(k_pool.shape), tuple(q.shape)))
+    if rows == 0:   # (an empty tensor has no address to pass down)
+        return
+    Hkv = k_pool.shape[3]
+    desc = make_attn_desc_quant(q, k_pool, v_pool, out, block_table, max_kv_len, n_seqs, cu_q, max_q, n_splits, lse_out,
+                             window, cache_slots)
+    need = pkv_attention_quant_workspace_size(desc, H, Hkv, D)
+    if need and (workspace is None or workspace.numel() * workspace.element_size() < need):
+        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+        _keep_until_done(workspace, stream)
+    _check(pkv_suffix_attention_quant(q, k_pool, v_pool, out, q_pos, kv_len, H, Hkv, D, scale, desc,
+                                   make_paging(block_table, k_pool, v_pool, v_block_table),
+                                   make_block_scales(k_scale, v_scale, k_pool.shape[2]), workspace, need, stream))
+
+
+# ---- pages ----------------------------------------------------------------------
+
+def make_page_pool(tensors: Sequence[torch.Tensor], block_table: torch.Tensor, page_size: int,
+                   err_flag: Optional[torch.Tensor] = None) -> pkv_page_pool:
+    """The tensors of a page pool, [layer][page][slot or block in page][kv_head] and, for pools, [channel]
+    (any strides, channels contiguous), under block tables of block_table's shape."""
+    if not 1 <= len(tensors) <= 4:
+        raise ValueError("a pool has 1 .. 4 tensors, got %d" % len(tensors))
+    pool = pkv_page_pool()
+    pool.page_size, pool.n_tensors = int(page_size), len(tensors)
+    pool.n_seqs, pool.max_pages = block_table.shape
+    pool.n_pages = tensors[0].shape[1]
+    for i, t in enumerate(tensors):
+        if t.dim() not in (4, 5) or t.shape[1] != pool.n_pages or (t.dim() == 5 and t.stride(4) != 1):
+            raise ValueError("tensor %d must be [layer][page][slot][kv_head] or [..][channel] with %d pages, got %s"
+                             % (i, pool.n_pages, tuple(t.shape)))
+        b = t.element_size()
+        st = t.stride()
+        pool.tensors[i] = pkv_page_tensor(t.data_ptr(), st[0] * b, st[1] * b, st[2] * b, st[3] * b, t.shape[0],
+                                          t.shape[2], t.shape[3], (t.shape[4] if t.dim() == 5 else 1) * b)
+    pool.err_flag = None if err_flag is None else err_flag.data_ptr()
+    return pool
+
+
+def make_forks(forks: Sequence[dict], device) -> torch.Tensor:
+    """Pack fork dicts (parent, child, n_tokens) into a device buffer of pkv_fork records."""
+    arr = (pkv_fork * max(1, len(forks)))()
+    for i, f in enumerate(forks):
+        arr[i] = pkv_fork(int(f["parent"]), int(f["child"]), int(f["n_tokens"]), 0)
+    return torch.frombuffer(bytearray(bytes(arr)), dtype=torch.uint8).to(device)
+
+
+def _check_pages_args(tensors, ref, block_table, page_size, err_flag) -> torch.device:
+    dev = _gpu_device(block_table, "block_table")
+    _need(block_table, "block_table", dev, torch.int32, contiguous=True)
+    if block_table.dim() != 2:
+        raise ValueError("block_table is [n_seqs][max_pages]")
+    for i, t in enumerate(tensors):
+        if t is None:
+            raise TypeError("tensor %d is None" % i)
+        _need(t, "tensor %d" % i, dev)
+    pages = tensors[0].shape[1] if tensors else 0
+    _need(ref, "ref", dev, torch.int32, pages, contiguous=True)
+    _need(err_flag, "err_flag", dev, torch.int32, 1)
+    return dev
+
+
+def _pages_workspace(pool, n_forks, workspace, dev, stream):
+    need = pkv_pages_workspace_size(pool, n_forks)
+    _need(workspace, "workspace", dev, contiguous=True)
+    if workspace is None or workspace.numel() * workspace.element_size() < need:
+        workspace = torch.empty(max(16, need), dtype=torch.uint8, device=dev)
+        _keep_until_done(workspace, stream)
+    return workspace, workspace.numel() * workspace.element_size()
+
+
+def pages_free(tensors, ref, block_table, page_size, seqs, keep=None, err_flag=None, stream=None) -> None:
+    """Tensor-level call of pkv_pages_free: rows seqs (int32) give back their pages behind the first keep
+    slots (int32, or None for all)."""
+    dev = _check_pages_args(tensors, ref, block_table, page_size, err_flag)
+    _need(seqs, "seqs", dev, torch.int32, contiguous=True)
+    _need(keep, "keep", dev, torch.int32, seqs.numel(), contiguous=True)
+    pool = make_page_pool(tensors, block_table, page_size, err_flag)
+    _check(pkv_pages_free(pool, ref, block_table, seqs, keep, seqs.numel(), stream))
+
+
+def pages_fork(tensors, ref, block_table, page_size, forks_dev, n_forks, block_table_out=None, err_flag=None,
+               workspace=None, stream=None) -> None:
+    """Tensor-level call of pkv_pages_fork (forks_dev: make_forks); children are rows of block_table_out,
+    by default block_table itself."""
+    dev = _check_pages_args(tensors, ref, block_table, page_size, err_flag)
+    _need(forks_dev, "forks_dev", dev, torch.uint8, int(n_forks) * ctypes.sizeof(pkv_fork), contiguous=True)
+    out = block_table if block_table_out is None else block_table_out
+    _need(out, "block_table_out", dev, torch.int32, contiguous=True)
+    if out.shape != block_table.shape:
+        raise ValueError("block_table and block_table_out have different shapes")
+    pool = make_page_pool(tensors, block_table, page_size, err_flag)
+    workspace, size = _pages_workspace(pool, n_forks, workspace, dev, stream)
+    _check(pkv_pages_fork(pool, ref, block_table, out, forks_dev, n_forks, workspace, size, stream))
+
+
+def pages_compact(tensors, ref, block_table, page_size, ref_out=None, block_table_out=None, n_used=None, err_flag=None,
+                  workspace=None, stream=None) -> torch.Tensor:
+    """Tensor-level call of pkv_pages_compact, in place unless other outputs are given; returns n_used
+    (int32 [1] on the device)."""
+    dev = _check_pages_args(tensors, ref, block_table, page_size, err_flag)
+    ref_out = ref if ref_out is None else ref_out
+    out = block_table if block_table_out is None else block_table_out
+    _need(ref_out, "ref_out", dev, torch.int32, tensors[0].shape[1], contiguous=True)
+    _need(out, "block_table_out", dev, torch.int32, contiguous=True)
+    if out.shape != block_table.shape:
+        raise ValueError("block_table and block_table_out have different shapes")
+    if n_used is None:
+        n_used = torch.empty(1, dtype=torch.int32, device=dev)
+        _keep_until_done(n_used, stream)
+    _need(n_used, "n_used", dev, torch.int32, 1)
+    pool = make_page_pool(tensors, block_table, page_size, err_flag)
+    workspace, size = _pages_workspace(pool, 0, workspace, dev, stream)
+    _check(pkv_pages_compact(pool, ref, ref_out, block_table, out, n_used, workspace, size, stream))
+    return n_used

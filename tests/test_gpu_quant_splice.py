@@ -1,0 +1,243 @@
+"""Reposition + splice into an 8-bit cache against the 64-bit reference: values, unmoved keys and every scale byte
+exactly, turned keys exactly or, where the fp32 rotation's error (2^-22 of the pair) reaches a rounding boundary, as
+the neighbouring code.  Slots that no call owns keep their bytes."""
+import numpy as np
+import pytest
+import torch
+
+import quant_ref as R
+from helpers import host_bits, log
+from paper_2606_17107_amd import pkv, synth
+
+pytestmark = pytest.mark.gpu
+
+HALF, INTER = 0, 1
+
+
+def theta_omega(theta, r):
+    return float(np.float32(theta)) ** (-2.0 * np.arange(r // 2) / r)
+
+
+class Case:
+    def __init__(self, L=2, H=2, d=128, page=64, block=32, seqs=1, cap=320, slots=400, dtype="bf16", seed=0, gain=1.0,
+                 values=True):
+        self.L, self.H, self.d, self.page, self.block, self.cap = L, H, d, page, block, cap
+        rng = np.random.default_rng(seed)
+        width = -(-cap // page)
+        self.P = seqs * width + 5
+        perm = rng.permutation(self.P)
+        self.table = perm[: seqs * width].reshape(seqs, width).astype(np.int32)
+        self.kv_len = np.zeros(seqs, np.int32)
+        shape = (L, self.P, page, H, d)
+        code = rng.integers(0, 127, shape) | (rng.integers(0, 2, shape) << 7)
+        self.k, self.v = code.astype(np.uint8), np.roll(code, 1).astype(np.uint8)
+        self.ks, self.vs = (rng.integers(118, 124, (L, self.P, page // block, H)).astype(np.uint8) for _ in "kv")
+        dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+        g = synth.Draws(seed + 1, "cpu")
+        self.src_k, self.src_v = (g.normal((L, H, slots, d), dt) * gain for _ in "kv")
+        self.values = values
+
+    def gpu(self, t):
+        return torch.from_numpy(t.copy()).cuda()
+
+    def run(self, segs, theta=1e4, offset=0, r=None, style=HALF, omega=None, longest=None, v_table=None, strided=False,
+            flagged=False, times=1, cap=None):
+        r = r or self.d
+        cap = self.cap if cap is None else cap
+        w = theta_omega(theta, r) if omega is None else np.asarray(omega)
+        k, v, ks, vs = (self.gpu(t) for t in (self.k, self.v, self.ks, self.vs))
+        src_k, src_v = self.src_k.cuda(), self.src_v.cuda()
+        if strided:   # token-major sources, pools and scales with room between rows
+            src_k, src_v = (t.permute(0, 2, 1, 3).contiguous().permute(0, 2, 1, 3) for t in (src_k, src_v))
+            wide = [torch.full(t.shape[:-1] + (t.shape[-1] + 16,), 0x5a, dtype=torch.uint8, device="cuda") for t in (k, v)]
+            for a, b in zip(wide, (k, v)):
+                a[..., : self.d] = b
+            k, v = (a[..., : self.d] for a in wide)
+            ks, vs = (torch.stack([t, t + 1], -1)[..., 0] for t in (ks, vs))
+        flag = torch.zeros(1, dtype=torch.int32, device="cuda")
+        table = self.gpu(self.table)
+        recs = pkv.make_segments_quant([dict(src_slot0=a, seq=b, n_tokens=n, src_pos0=p, dst_pos0=e)
+                                        for a, b, n, p, e in segs], "cuda")
+        for _ in range(times):
+            pkv.reposition_splice_quant(
+                src_k, src_v if self.values else None, k, v if self.values else None, ks, vs if self.values else None, recs,
+                len(segs), max([n for _, _, n, _, _ in segs] + [1]) if longest is None else longest, self.gpu(self.kv_len),
+                table, theta, r, rope_offset=offset, rope_style=style, omega=omega, dst_capacity=cap, err_flag=flag,
+                v_block_table=None if v_table is None else self.gpu(v_table))
+        torch.cuda.synchronize()
+        assert int(flag.item()) == int(flagged)
+        f64 = lambda t: t.double().numpy()   # noqa: E731
+        live = self.kv_len.tolist()
+        wk = R.store(f64(self.src_k), self.k, self.ks, segs, live, self.table, w, offset, style, cap, True)
+        differ = R.check_codes(k.cpu().numpy(), wk[0], wk[2], wk[3], "keys")
+        np.testing.assert_array_equal(ks.cpu().numpy(), wk[1])
+        if self.values:
+            wv = R.store(f64(self.src_v), self.v, self.vs, segs, live, self.table if v_table is None else v_table, w,
+                         offset, style, cap, False)
+            R.check_codes(v.cpu().numpy(), wv[0], wv[0], wv[0], "values")
+            np.testing.assert_array_equal(vs.cpu().numpy(), wv[1])
+        else:
+            np.testing.assert_array_equal(v.cpu().numpy(), self.v)
+        if strided:
+            assert all(bool((a[..., self.d:] == 0x5a).all()) for a in wide)
+        log("  %d of %d turned codes on the other side of a boundary" % (differ, wk[0].size))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("style", [HALF, INTER])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("page,block", [(32, 32), (64, 64), (256, 128), (128, 32)])
+def test_one_chunk(d, page, block, style, dtype):
+    """A chunk of odd length at an odd slot, between kept slots and behind the length."""
+    c = Case(d=d, page=page, block=block, dtype=dtype, seed=page + d)
+    c.kv_len[0] = 290      # the chunk's slots 45 .. 245 lie inside
+    c.run([(3, 0, 201, 17, 45)], style=style)
+    c.kv_len[0] = 45       # nothing behind it is kept
+    c.run([(3, 0, 201, 17, 45)], style=style)
+
+
+@pytest.mark.parametrize("block", [32, 64, 128])
+@pytest.mark.parametrize("order", [1, -1])
+def test_chunks_that_share_blocks(block, order):
+    """Chunks back to back, one of a single token, meet inside blocks; records in either order."""
+    c = Case(page=128, block=block, cap=384, seqs=3, seed=block)
+    c.kv_len[:] = [10, 0, 128]
+    segs = []
+    for s, p in enumerate((10, 0, 128)):
+        for n, src, pos in ((37, 5, 100), (1, 77, 3), (70, 100, 4000), (64, 200, p + 108)):
+            segs.append((src, s, n, pos, p))
+            p += n
+    c.run(segs[::order])
+
+
+def test_one_token_each_of_many_sequences():
+    """More records than one look of 64, in shuffled order; the calls repeat, which changes nothing."""
+    n = 150
+    c = Case(L=1, H=8, seqs=n, cap=64, page=32, block=32, slots=n, seed=3)
+    rng = np.random.default_rng(4)
+    c.kv_len[:] = rng.integers(0, 64, n)
+    segs = [(s, s, 1, 50, int(c.kv_len[s])) for s in rng.permutation(n)]
+    c.run(segs, times=3)
+
+
+@pytest.mark.parametrize("heads", [1, 3, 5, 8])
+def test_head_counts(heads):
+    c = Case(L=3, H=heads, page=64, block=64, seed=heads)
+    c.kv_len[0] = 5
+    c.run([(0, 0, 130, 9, 5)])
+
+
+def test_longer_than_the_stated_bound():
+    c = Case(page=64, block=32, seed=5)
+    c.run([(0, 0, 300, 0, 7), ], longest=1)
+
+
+def test_strided_tensors():
+    c = Case(page=64, block=32, seed=6)
+    c.kv_len[0] = 320
+    c.run([(11, 0, 97, 0, 63)], strided=True)
+
+
+def test_values_through_their_own_table():
+    c = Case(page=64, block=64, seed=7)
+    c.kv_len[0] = 33
+    free = np.setdiff1d(np.arange(c.P), c.table[0])
+    vt = c.table.copy()
+    vt[0, :3] = free[:3]
+    c.run([(0, 0, 150, 1, 33)], v_table=vt)
+
+
+def test_keys_alone():
+    Case(seed=8, values=False).run([(0, 0, 150, 1, 33)])
+
+
+@pytest.mark.parametrize("offset,r,style", [(64, 64, HALF), (8, 112, INTER), (96, 32, INTER), (0, 16, HALF)])
+def test_rotary_slice(offset, r, style):
+    c = Case(seed=9)
+    c.run([(0, 0, 60, 100, 3)], offset=offset, r=r, style=style)
+
+
+def test_frequency_table():
+    """Explicit frequencies, a third of them 0 (the spatial pairs of an image)."""
+    w = np.where(np.arange(64) % 3 == 0, 0.0, 1.0 / (1 + np.arange(64)))
+    Case(seed=10).run([(0, 0, 60, 100, 3)], omega=list(w))
+
+
+@pytest.mark.parametrize("delta", [2 ** 24 - 1, -(2 ** 24 - 1), -1])
+def test_far_moves(delta):
+    Case(L=1, seed=11).run([(0, 0, 60, 40 - delta, 40)])
+
+
+@pytest.mark.parametrize("gain,dtype", [(1e-38, "f32"), (1e-30, "bf16"), (1e30, "bf16"), (1e37, "f32"), (0.0, "bf16")])
+def test_magnitudes(gain, dtype):
+    """From scales at their smallest byte to the largest finite inputs; all zeros."""
+    c = Case(L=1, seed=12, gain=gain, dtype=dtype)
+    c.kv_len[0] = 20
+    c.run([(0, 0, 60, 40, 40)])
+    c.ks[:], c.vs[:] = 1, 1
+    c.run([(0, 0, 60, 40, 10)])
+
+
+def test_nonfinite_rows():
+    """NaN and infinities become NaN codes and leave the block's scale to the others (delta 0: rows as they are)."""
+    c = Case(L=1, seed=13)
+    for t in (c.src_k, c.src_v):
+        t[0, 0, 3, 5], t[0, 0, 4, 6], t[0, 1, 9, 127] = float("nan"), float("inf"), float("-inf")
+        t[0, 0, 40:] = float("nan")
+    c.kv_len[0] = 2
+    c.run([(0, 0, 100, 2, 2)])
+
+
+def test_out_of_range():
+    """Slots, sources, sequences and pages outside: those tokens are skipped and flagged, the others land."""
+    c = Case(page=32, block=32, seqs=2, cap=128, slots=100, seed=14)
+    c.kv_len[:] = [128, 60]
+    c.run([(0, 0, 50, 0, 100)], flagged=True)          # runs over the capacity
+    c.run([(0, 0, 50, 0, -20)], flagged=True)          # begins before slot 0
+    c.run([(80, 0, 50, 0, 10)], flagged=True)          # runs over the source
+    c.run([(-10, 0, 50, 0, 10)], flagged=True)
+    c.run([(0, 2, 50, 0, 10), (5, 1, 20, 0, 60)], flagged=True)
+    c.run([(0, -1, 50, 0, 10), (5, 1, 20, 0, 60)], flagged=True)
+    c.run([(0, 0, 0, 0, 10), (0, 1, -3, 0, 10)])       # nothing to do
+    c.run([(0, 0, 60, 7, 20)], cap=50, flagged=True)
+    c.table[0, 1] = c.P + 3
+    c.run([(0, 0, 80, 0, 10)], flagged=True)
+    c.table[0, 1] = -1
+    c.run([(0, 0, 80, 0, 10)], flagged=True)
+
+
+def test_side_stream_and_graph():
+    """The call on a stream that is not torch's current one, and captured and replayed with new contents."""
+    c = Case(L=1, H=4, seqs=2, seed=15)
+    c.kv_len[:] = [40, 0]
+    segs = [(0, 0, 100, 3, 40), (100, 1, 77, 0, 0)]
+    recs = pkv.make_segments_quant([dict(src_slot0=a, seq=b, n_tokens=n, src_pos0=p, dst_pos0=e) for a, b, n, p, e in segs], "cuda")
+    src_k, src_v, table, kv = c.src_k.cuda(), c.src_v.cuda(), c.gpu(c.table), c.gpu(c.kv_len)
+
+    def fresh():
+        return [c.gpu(t) for t in (c.k, c.v, c.ks, c.vs)]
+
+    def call(t, stream=None):
+        pkv.reposition_splice_quant(src_k, src_v, *t, recs, 2, 100, kv, table, 1e4, 128, stream=stream)
+
+    want = fresh()
+    call(want)
+    side = torch.cuda.Stream()
+    got = fresh()
+    torch.cuda.synchronize()
+    call(got, side)
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    got, start = fresh(), fresh()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(got)
+    for i in range(3):
+        src_k.mul_(-1.0)
+        for a, b in zip(got, start):
+            a.copy_(b)
+        graph.replay()
+        want = fresh()
+        call(want)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), i
