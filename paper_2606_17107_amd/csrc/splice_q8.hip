@@ -88,25 +88,27 @@ __device__ inline void turn(int64_t delta, double omega, float& c, float& s) {
     c = ((q + 1) & 2) ? -ca : ca;
 }
 
-// Eight channels of a source row as fp32.
+// Eight channels of a source row as they are loaded, and as fp32.
 template <bool F32>
-__device__ inline void load8(const char* p, float* x) {
-    if constexpr (F32) {
-        const f32x4 a = *(const f32x4*)p, b = *(const f32x4*)(p + 16);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            x[i] = a[i];
-            x[4 + i] = b[i];
-        }
-    } else {
-        const u32x4 a = *(const u32x4*)p;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            x[2 * i] = __uint_as_float(a[i] << 16);
-            x[2 * i + 1] = __uint_as_float(a[i] & 0xffff0000u);
-        }
+struct Raw8 {
+    u32x4 a, b;
+    __device__ __forceinline__ void load(const char* p) {
+        a = __builtin_nontemporal_load((const u32x4*)p);
+        b = __builtin_nontemporal_load((const u32x4*)(p + 16));
     }
-}
+    __device__ __forceinline__ float get(int i) const { return __uint_as_float(i < 4 ? a[i & 3] : b[i & 3]); }
+};
+template <>
+struct Raw8<false> {
+    u32x4 a;
+    __device__ __forceinline__ void load(const char* p) { a = *(const u32x4*)p; }
+    __device__ __forceinline__ float get(int i) const {
+        return __uint_as_float(i & 1 ? a[i >> 1] & 0xffff0000u : a[i >> 1] << 16);
+    }
+};
+
+// The value of lane l ^ 1.
+__device__ inline uint32_t swap1(uint32_t v) { return (uint32_t)dpp<0xb1>((int)v, (int)v); }   // quad_perm [1, 0, 3, 2]
 
 // D: head size.  SUBS: waves (of 32 slots) per scale block.  INTER: interleaved pairs.
 template <int D, int SUBS, bool F32, bool INTER>
@@ -159,6 +161,8 @@ __global__ __launch_bounds__(kWaves * 64) void store_kernel(StoreArgs a, StoreGe
         ca = cl;
         cb = cl + LPT;
     }
+    // Chunks of lanes 2m and 2m + 1 are neighbours, the first at an even place: 16 bytes of codes.
+    const bool pairs = !is_k || (g.rope_c0 % 2 == 0 && g.rope_nc % 4 == 0);
     const char* const src = (is_k ? a.src_k : a.src_v) + ((int64_t)layer * (is_k ? a.src_k_stride[0] : a.src_v_stride[0]) +
                                                           (int64_t)head * (is_k ? a.src_k_stride[1] : a.src_v_stride[1])) * EB;
     const int64_t src_row = (is_k ? a.src_k_stride[2] : a.src_v_stride[2]) * EB;
@@ -190,6 +194,13 @@ __global__ __launch_bounds__(kWaves * 64) void store_kernel(StoreArgs a, StoreGe
         const int old = working ? (int)*scale_at : 0;
         uint8_t* const rows = dst + at * dst_page + (int64_t)(inside + sub * kSub + row0) * dst_row;
 
+        // The records are looked through 64 at a time; the first look is under way before the rows.
+        auto touches = [&](int j) __attribute__((always_inline)) {
+            const StoreSegment s = a.segs[min(j, a.n_segs - 1)];
+            return j < a.n_segs && s.seq == mine.seq && s.n_tokens > 0 && s.dst_pos0 < block_end &&
+                   (int64_t)s.dst_pos0 + s.n_tokens > slot0;
+        };
+        bool first_look = touches(lane);
         float x[STEPS][16];
         bool has[STEPS];
 #pragma unroll
@@ -198,67 +209,71 @@ __global__ __launch_bounds__(kWaves * 64) void store_kernel(StoreArgs a, StoreGe
 #pragma unroll
             for (int i = 0; i < 16; ++i) x[t][i] = 0.f;
         }
-        // Every segment that touches the block, by number; the first one owns it.
-        bool owner = true, found = false;
+        // Rows of a record into the slots that no record before it took: all loads under way together for
+        // the block's own record, one step after another (fewer registers) for those that share the block.
+        auto gather = [&](const StoreSegment& s, auto ahead_tag) __attribute__((always_inline)) {
+            constexpr bool AHEAD = decltype(ahead_tag)::value;
+            Raw8<F32> raw[AHEAD ? STEPS : 1][2];
+            auto taken = [&](int t) __attribute__((always_inline)) {
+                const int64_t n = (int64_t)first + t * TPS - s.dst_pos0, from = s.src_slot0 + n;
+                return working && !has[t] && n >= 0 && n < s.n_tokens && first + t * TPS < block_end && from >= 0 &&
+                       from < a.n_src;
+            };
+            auto load = [&](int t) __attribute__((always_inline)) {
+                const char* const p = src + (s.src_slot0 + ((int64_t)first + t * TPS - s.dst_pos0)) * src_row;
+                raw[AHEAD ? t : 0][0].load(p + ca * 8 * EB);
+                raw[AHEAD ? t : 0][1].load(p + cb * 8 * EB);
+            };
+            bool take[STEPS];
+#pragma unroll
+            for (int t = 0; t < STEPS; ++t) {
+                take[t] = taken(t);
+                if (AHEAD && take[t]) load(t);
+            }
+            const int64_t delta = (int64_t)s.dst_pos0 - s.src_pos0;
+            const bool turns = is_k && delta != 0;   // uniform
+            float c1 = 1.f, s1 = 0.f;
+            if (turns) turn(delta, ft.w[lane], c1, s1);
+            float c[8], sn[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                // coefficient i of the lane's chunks: HALF, pairs 8 cl ..; INTERLEAVED, 4 pairs of each chunk
+                const int pair = INTER ? (i < 4 ? cl * 4 + i : (half_r + cl) * 4 + i - 4) : cl * 8 + i;
+                c[i] = __shfl(c1, pair & 63);
+                sn[i] = __shfl(s1, pair & 63);
+            }
+#pragma unroll
+            for (int t = 0; t < STEPS; ++t) {
+                if (!take[t]) continue;
+                if (!AHEAD) load(t);
+                has[t] = true;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) x[t][i] = raw[AHEAD ? t : 0][i >> 3].get(i & 7);
+                if (rope && turns) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const int ia = INTER ? 2 * i : i, ib = INTER ? 2 * i + 1 : i + 8;
+                        const float u = x[t][ia], v = x[t][ib];
+                        x[t][ia] = fmaf(u, c[i], -(v * sn[i]));
+                        x[t][ib] = fmaf(u, sn[i], v * c[i]);
+                    }
+                }
+            }
+        };
+        gather(mine, std::true_type{});
+        // Every other record that touches the block, by number; one below this segment's owns it.
+        bool owner = true;
 #pragma unroll 1
         for (int j0 = 0; j0 < a.n_segs && owner; j0 += 64) {
-            const int j = j0 + lane;
-            bool touches = false;
-            if (j < a.n_segs) {
-                const StoreSegment s = a.segs[j];
-                touches = s.seq == mine.seq && s.n_tokens > 0 && s.dst_pos0 < block_end &&
-                          (int64_t)s.dst_pos0 + s.n_tokens > slot0;
-            }
-            uint64_t hits = __builtin_amdgcn_ballot_w64(touches);
+            uint64_t hits = __builtin_amdgcn_ballot_w64(j0 == 0 ? first_look : touches(j0 + lane));
+            if (seg_i >= j0 && seg_i < j0 + 64) hits &= ~(1ull << (seg_i - j0));
+#pragma unroll 1
             while (hits) {
                 const int h = j0 + __builtin_ctzll(hits);
                 hits &= hits - 1;
-                if (!found) {
-                    found = true;
-                    owner = h == seg_i;
-                    if (!owner) break;
-                }
-                const StoreSegment s = a.segs[h];
-                float raw[STEPS][16];
-                bool take[STEPS];
-#pragma unroll
-                for (int t = 0; t < STEPS; ++t) {
-                    const int64_t r = (int64_t)first + t * TPS - s.dst_pos0;
-                    const int64_t from = s.src_slot0 + r;
-                    take[t] = working && !has[t] && r >= 0 && r < s.n_tokens && first + t * TPS < block_end && from >= 0 &&
-                              from < a.n_src;
-                    const char* const p = src + (take[t] ? from : 0) * src_row;
-                    if (take[t]) {
-                        load8<F32>(p + ca * 8 * EB, raw[t]);
-                        load8<F32>(p + cb * 8 * EB, raw[t] + 8);
-                    }
-                }
-                const int64_t delta = (int64_t)s.dst_pos0 - s.src_pos0;
-                if (is_k && delta != 0) {   // uniform
-                    float c1, s1;
-                    turn(delta, ft.w[lane], c1, s1);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        // coefficient i of the lane's chunks: HALF, pairs 8 cl ..; INTERLEAVED, 4 pairs of each chunk
-                        const int pair = INTER ? (i < 4 ? cl * 4 + i : (half_r + cl) * 4 + i - 4) : cl * 8 + i;
-                        const float c = __shfl(c1, pair & 63), sn = __shfl(s1, pair & 63);
-                        const int ia = INTER ? 2 * i : i, ib = INTER ? 2 * i + 1 : i + 8;
-                        if (rope) {
-#pragma unroll
-                            for (int t = 0; t < STEPS; ++t) {
-                                const float u = raw[t][ia], v = raw[t][ib];
-                                raw[t][ia] = fmaf(u, c, -(v * sn));
-                                raw[t][ib] = fmaf(u, sn, v * c);
-                            }
-                        }
-                    }
-                }
-#pragma unroll
-                for (int t = 0; t < STEPS; ++t) {
-                    has[t] = has[t] || take[t];
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) x[t][i] = take[t] ? raw[t][i] : x[t][i];
-                }
+                owner = h > seg_i;
+                if (!owner) break;
+                gather(a.segs[h], std::false_type{});
             }
         }
         if (!owner) continue;   // uniform over the workgroup
@@ -309,13 +324,23 @@ __global__ __launch_bounds__(kWaves * 64) void store_kernel(StoreArgs a, StoreGe
         for (int t = 0; t < STEPS; ++t) {
             if (!has[t]) continue;
             uint8_t* const p = rows + (int64_t)(t * TPS) * dst_row;
+            u32x2 w[2];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const float* y = x[t] + 8 * h;
-                u32x2 w;
-                w[0] = pack4(y[0] * up, y[1] * up, y[2] * up, y[3] * up);
-                w[1] = pack4(y[4] * up, y[5] * up, y[6] * up, y[7] * up);
-                __builtin_nontemporal_store(w, (u32x2*)(p + (h ? cb : ca) * 8));
+                w[h][0] = pack4(y[0] * up, y[1] * up, y[2] * up, y[3] * up);
+                w[h][1] = pack4(y[4] * up, y[5] * up, y[6] * up, y[7] * up);
+            }
+            if (pairs) {
+                // lanes 2m and 2m + 1 hold neighbouring chunks of either half of the row: one
+                // takes both of the first half, the other both of the second
+                const bool odd = lane & 1;
+                const uint32_t g0 = swap1(odd ? w[0][0] : w[1][0]), g1 = swap1(odd ? w[0][1] : w[1][1]);
+                const u32x4 v = odd ? u32x4{g0, g1, w[1][0], w[1][1]} : u32x4{w[0][0], w[0][1], g0, g1};
+                __builtin_nontemporal_store(v, (u32x4*)(p + (odd ? cb - 1 : ca) * 8));
+            } else {
+                __builtin_nontemporal_store(w[0], (u32x2*)(p + ca * 8));
+                __builtin_nontemporal_store(w[1], (u32x2*)(p + cb * 8));
             }
         }
         if ((any & 2) && e > old) {
