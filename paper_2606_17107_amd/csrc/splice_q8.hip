@@ -61,27 +61,24 @@ __device__ inline uint32_t pack4(float a, float b, float c, float d) {
 }
 __device__ inline float exp2_int(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }   // -126 <= e <= 127
 
-// cos and sin of delta * omega, fp64 throughout and rounded once.
-__device__ inline void turn(int64_t delta, double omega, float& c, float& s) {
-    const double x = (double)delta * omega;
+// cos and sin of delta * omega, fp64 throughout and rounded once.  The Taylor series
+// leave out terms below 2^-29.
+__device__ inline void turn(double delta, double omega, float& c, float& s) {
+    const double x = delta * omega;
     const double k = rint(x * 0.63661977236758134308);            // 2/pi
     double r = fma(-k, 1.5707963267948966192, x);                // pi/2, leading part
     r = fma(-k, 6.123233995736766036e-17, r);                    // pi/2, trailing part
+    const int q = (int)fma(-4.0, floor(k * 0.25), k);            // k mod 4
     const double z = r * r;
-    double ps = fma(z, 1.0 / 6227020800.0, -1.0 / 39916800.0);   // 1/13!, -1/11!
-    ps = fma(z, ps, 1.0 / 362880.0);
-    ps = fma(z, ps, -1.0 / 5040.0);
+    double ps = fma(z, 1.0 / 362880.0, -1.0 / 5040.0);           // 1/9!, -1/7!
     ps = fma(z, ps, 1.0 / 120.0);
     ps = fma(z, ps, -1.0 / 6.0);
     const double sr = fma(r * z, ps, r);
-    double pc = fma(z, -1.0 / 87178291200.0, 1.0 / 479001600.0);   // -1/14!, 1/12!
-    pc = fma(z, pc, -1.0 / 3628800.0);
-    pc = fma(z, pc, 1.0 / 40320.0);
+    double pc = fma(z, -1.0 / 3628800.0, 1.0 / 40320.0);         // -1/10!, 1/8!
     pc = fma(z, pc, -1.0 / 720.0);
     pc = fma(z, pc, 1.0 / 24.0);
     pc = fma(z, pc, -0.5);
     const double cr = fma(z, pc, 1.0);
-    const int q = (int)((int64_t)k & 3);
     const float sa = (float)((q & 1) ? cr : sr);
     const float ca = (float)((q & 1) ? sr : cr);
     s = (q & 2) ? -sa : sa;
@@ -119,6 +116,7 @@ __global__ __launch_bounds__(kWaves * 64) void store_kernel(StoreArgs a, StoreGe
     constexpr int BT = SUBS * kSub;       // slots per scale block
     constexpr int EB = F32 ? 4 : 2;
     __shared__ int top_lds[2][kWaves], any_lds[2][kWaves];
+    __shared__ __attribute__((aligned(16))) float coef_lds[kWaves][2 * kPairs];   // cos of all pairs, then sin
 
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int lane = threadIdx.x & 63;
@@ -142,7 +140,7 @@ __global__ __launch_bounds__(kWaves * 64) void store_kernel(StoreArgs a, StoreGe
     if (teller && (mine.seq < 0 || mine.seq >= a.n_seqs || mine.dst_pos0 < 0 || end > a.dst_capacity ||
                    mine.src_slot0 < 0 || mine.src_slot0 > a.n_src - mine.n_tokens))
         flag();
-    if (mine.seq < 0 || mine.seq >= a.n_seqs) return;
+    if (mine.seq < 0 || mine.seq >= a.n_seqs || a.n_src <= 0) return;
     const int live = a.kv_len[mine.seq];
 
     // This lane's chunks of 8 channels: rotary lanes hold a chunk and its partner.
@@ -194,109 +192,130 @@ __global__ __launch_bounds__(kWaves * 64) void store_kernel(StoreArgs a, StoreGe
         const int old = working ? (int)*scale_at : 0;
         uint8_t* const rows = dst + at * dst_page + (int64_t)(inside + sub * kSub + row0) * dst_row;
 
-        // The records are looked through 64 at a time; the first look is under way before the rows.
+        // Which record fills which slot: those that touch the block, by number (a slot that two
+        // records name goes to the first); one below this segment's owns the block. 
         auto touches = [&](int j) __attribute__((always_inline)) {
             const StoreSegment s = a.segs[min(j, a.n_segs - 1)];
             return j < a.n_segs && s.seq == mine.seq && s.n_tokens > 0 && s.dst_pos0 < block_end &&
                    (int64_t)s.dst_pos0 + s.n_tokens > slot0;
         };
-        bool first_look = touches(lane);
-        float x[STEPS][16];
-        bool has[STEPS];
+        int64_t off[STEPS];   // of the row in the source, bytes; a row that exists where a lane has none
+        int rec[STEPS];       // its record's place among those that touch the block, -1 none
 #pragma unroll
         for (int t = 0; t < STEPS; ++t) {
-            has[t] = false;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) x[t][i] = 0.f;
+            off[t] = 0;
+            rec[t] = -1;
         }
-        // Rows of a record into the slots that no record before it took: all loads under way together for
-        // the block's own record, one step after another (fewer registers) for those that share the block.
-        auto gather = [&](const StoreSegment& s, auto ahead_tag) __attribute__((always_inline)) {
-            constexpr bool AHEAD = decltype(ahead_tag)::value;
-            Raw8<F32> raw[AHEAD ? STEPS : 1][2];
-            auto taken = [&](int t) __attribute__((always_inline)) {
-                const int64_t n = (int64_t)first + t * TPS - s.dst_pos0, from = s.src_slot0 + n;
-                return working && !has[t] && n >= 0 && n < s.n_tokens && first + t * TPS < block_end && from >= 0 &&
-                       from < a.n_src;
-            };
-            auto load = [&](int t) __attribute__((always_inline)) {
-                const char* const p = src + (s.src_slot0 + ((int64_t)first + t * TPS - s.dst_pos0)) * src_row;
-                raw[AHEAD ? t : 0][0].load(p + ca * 8 * EB);
-                raw[AHEAD ? t : 0][1].load(p + cb * 8 * EB);
-            };
-            bool take[STEPS];
-#pragma unroll
-            for (int t = 0; t < STEPS; ++t) {
-                take[t] = taken(t);
-                if (AHEAD && take[t]) load(t);
-            }
-            const int64_t delta = (int64_t)s.dst_pos0 - s.src_pos0;
-            const bool turns = is_k && delta != 0;   // uniform
-            float c1 = 1.f, s1 = 0.f;
-            if (turns) turn(delta, ft.w[lane], c1, s1);
-            float c[8], sn[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                // coefficient i of the lane's chunks: HALF, pairs 8 cl ..; INTERLEAVED, 4 pairs of each chunk
-                const int pair = INTER ? (i < 4 ? cl * 4 + i : (half_r + cl) * 4 + i - 4) : cl * 8 + i;
-                c[i] = __shfl(c1, pair & 63);
-                sn[i] = __shfl(s1, pair & 63);
-            }
-#pragma unroll
-            for (int t = 0; t < STEPS; ++t) {
-                if (!take[t]) continue;
-                if (!AHEAD) load(t);
-                has[t] = true;
-#pragma unroll
-                for (int i = 0; i < 16; ++i) x[t][i] = raw[AHEAD ? t : 0][i >> 3].get(i & 7);
-                if (rope && turns) {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const int ia = INTER ? 2 * i : i, ib = INTER ? 2 * i + 1 : i + 8;
-                        const float u = x[t][ia], v = x[t][ib];
-                        x[t][ia] = fmaf(u, c[i], -(v * sn[i]));
-                        x[t][ib] = fmaf(u, sn[i], v * c[i]);
-                    }
-                }
-            }
-        };
-        gather(mine, std::true_type{});
-        // Every other record that touches the block, by number; one below this segment's owns it.
+        int records = 0;
         bool owner = true;
 #pragma unroll 1
         for (int j0 = 0; j0 < a.n_segs && owner; j0 += 64) {
-            uint64_t hits = __builtin_amdgcn_ballot_w64(j0 == 0 ? first_look : touches(j0 + lane));
-            if (seg_i >= j0 && seg_i < j0 + 64) hits &= ~(1ull << (seg_i - j0));
+            uint64_t hits = __builtin_amdgcn_ballot_w64(touches(j0 + lane));
 #pragma unroll 1
-            while (hits) {
+            for (; hits; hits &= hits - 1) {
                 const int h = j0 + __builtin_ctzll(hits);
-                hits &= hits - 1;
-                owner = h > seg_i;
+                owner = h >= seg_i;
                 if (!owner) break;
-                gather(a.segs[h], std::false_type{});
+                const StoreSegment s = a.segs[h];
+                // the block's slots [lo, hi) that the record fills from rows that exist
+                const int64_t shift = (int64_t)s.dst_pos0 - s.src_slot0;   // slot - source slot
+                const int lo = (int)max(max(slot0, (int64_t)s.dst_pos0), shift);
+                const int hi = (int)min(min(block_end, (int64_t)s.dst_pos0 + s.n_tokens), shift + a.n_src);
+#pragma unroll
+                for (int t = 0; t < STEPS; ++t) {
+                    const int slot = first + t * TPS;
+                    if (slot >= lo && slot < hi && rec[t] < 0) {
+                        off[t] = (slot - shift) * src_row;
+                        rec[t] = records;
+                    }
+                }
+                ++records;
             }
         }
         if (!owner) continue;   // uniform over the workgroup
 
+        Raw8<F32> raw[STEPS][2];
+#pragma unroll
+        for (int t = 0; t < STEPS; ++t) {
+            raw[t][0].load(src + off[t] + ca * 8 * EB);
+            raw[t][1].load(src + off[t] + cb * 8 * EB);
+        }
+        float x[STEPS][16];
+        auto turn_rows = [&](const StoreSegment& s, int r, bool unpack) __attribute__((always_inline)) {
+            float c[8], sn[8];
+            const bool turns = is_k && s.dst_pos0 != s.src_pos0;   // uniform
+            if (turns) {
+                // lane l evaluates pair l; the others' come through LDS (a wave's accesses are in order)
+                float c1, s1;
+                turn((double)s.dst_pos0 - (double)s.src_pos0, ft.w[lane], c1, s1);
+                asm volatile("" ::: "memory");
+                coef_lds[wave][lane] = c1;
+                coef_lds[wave][kPairs + lane] = s1;
+                __builtin_amdgcn_wave_barrier();
+                asm volatile("" ::: "memory");
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    // HALF: pairs 8 cl ..; INTERLEAVED: 4 pairs of each of the lane's chunks
+                    const int pair = (INTER ? (h ? (half_r + cl) * 4 : cl * 4) : cl * 8 + 4 * h) & (kPairs - 1);
+                    const f32x4 cv = *(const f32x4*)&coef_lds[wave][pair], sv = *(const f32x4*)&coef_lds[wave][kPairs + pair];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        c[4 * h + i] = cv[i];
+                        sn[4 * h + i] = sv[i];
+                    }
+                }
+            }
+            if (unpack) {
+#pragma unroll
+                for (int t = 0; t < STEPS; ++t)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) x[t][i] = raw[t][i >> 3].get(i & 7);
+            }
+            if (!turns) return;
+#pragma unroll
+            for (int t = 0; t < STEPS; ++t) {
+                if (!rope || rec[t] != r) continue;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int ia = INTER ? 2 * i : i, ib = INTER ? 2 * i + 1 : i + 8;
+                    const float u = x[t][ia], v = x[t][ib];
+                    x[t][ia] = fmaf(u, c[i], -(v * sn[i]));
+                    x[t][ib] = fmaf(u, sn[i], v * c[i]);
+                }
+            }
+        };
+        turn_rows(mine, 0, true);
+        // The other records' rows, found once more.
+#pragma unroll 1
+        for (int j0 = seg_i & ~63, r = 1; r < records && j0 < a.n_segs; j0 += 64) {
+            uint64_t hits = __builtin_amdgcn_ballot_w64(j0 + lane > seg_i && touches(j0 + lane));
+#pragma unroll 1
+            for (; hits; hits &= hits - 1, ++r) turn_rows(a.segs[j0 + __builtin_ctzll(hits)], r, false);
+        }
+
         // The largest finite magnitude, and whether the block gets and keeps rows.
         float m = 0.f;
 #pragma unroll
-        for (int t = 0; t < STEPS; ++t)
+        for (int t = 0; t < STEPS; ++t) {
+            float n = 0.f;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) m = fmaxf(m, fabsf(x[t][i]));   // (passes over a NaN)
+            for (int i = 0; i < 16; ++i) n = fmaxf(n, fabsf(x[t][i]));   // (passes over a NaN)
+            m = rec[t] >= 0 ? fmaxf(m, n) : m;
+        }
         if (__builtin_amdgcn_ballot_w64(m == INFINITY) != 0) {
             m = 0.f;
 #pragma unroll
             for (int t = 0; t < STEPS; ++t)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) m = fmaxf(m, fabsf(x[t][i]) < INFINITY ? fabsf(x[t][i]) : 0.f);
+                for (int i = 0; i < 16; ++i)
+                    m = fmaxf(m, rec[t] >= 0 && fabsf(x[t][i]) < INFINITY ? fabsf(x[t][i]) : 0.f);
         }
         bool gets = false, keeps = false;
         bool kept[STEPS];
 #pragma unroll
         for (int t = 0; t < STEPS; ++t) {
-            kept[t] = working && !has[t] && first + t * TPS < min((int64_t)live, block_end);
-            gets |= has[t];
+            kept[t] = working && rec[t] < 0 && first + t * TPS < (int)min((int64_t)live, block_end);
+            gets |= rec[t] >= 0;
             keeps |= kept[t];
         }
         int top = wave_max_u((int)__float_as_uint(m));
@@ -322,7 +341,7 @@ __global__ __launch_bounds__(kWaves * 64) void store_kernel(StoreArgs a, StoreGe
         const float up = __uint_as_float((uint32_t)(254 - min(e, 254)) << 23);   // 2^(127 - e)
 #pragma unroll
         for (int t = 0; t < STEPS; ++t) {
-            if (!has[t]) continue;
+            if (rec[t] < 0) continue;
             uint8_t* const p = rows + (int64_t)(t * TPS) * dst_row;
             u32x2 w[2];
 #pragma unroll
