@@ -24,9 +24,9 @@
 //     it; the owner gathers the rows of all segments that end or begin there, so that
 //     chunks spliced back to back in one call share a block's scale.  Every wave finds
 //     the segments by looking through the records, 64 at a time.
-//   * cos and sin come from fp64 (angle, reduction by pi/2 and Taylor series) and are
-//     rounded to fp32 once: an E4M3 code depends on the rotated value's last bits only
-//     near a rounding boundary, and there the fp32 rotation decides as exactly as it can.
+//   * cos and sin are formed as exactly as fp32 holds them: an E4M3 code depends on the
+//     rotated value's last bits only near a rounding boundary, and there the fp32
+//     rotation decides as exactly as it can.
 #include <math.h>
 
 #include "attn_columns.h"
@@ -55,32 +55,49 @@ struct StoreGeo {
     int rope_c0, rope_nc;  // rotary chunks of 8 channels: first, number
 };
 
-__device__ inline uint32_t pack4(float a, float b, float c, float d) {
-    const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
-    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, lo, true);
+typedef short s16x2 __attribute__((ext_vector_type(2)));
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+
+// Codes of four values divided by a power of two (the conversion applies it: one
+// instruction for two values, like the unscaled one).
+__device__ inline uint32_t pack4(float a, float b, float c, float d, float scale) {
+    s16x2 v = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(s16x2{0, 0}, a, b, scale, false);
+    v = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(v, c, d, scale, true);
+    return __builtin_bit_cast(uint32_t, v);
+}
+__device__ inline uint32_t pack4_bf16(uint32_t lo, uint32_t hi, float scale) {
+    s16x2 v = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(s16x2{0, 0}, __builtin_bit_cast(bf16x2, lo), scale, false);
+    v = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(v, __builtin_bit_cast(bf16x2, hi), scale, true);
+    return __builtin_bit_cast(uint32_t, v);
 }
 __device__ inline float exp2_int(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }   // -126 <= e <= 127
 
-// cos and sin of delta * omega, fp64 throughout and rounded once.  The Taylor series
-// leave out terms below 2^-29.
+// cos and sin of delta * omega to fp32's last bit or nearly: the angle is formed and
+// reduced by pi/2 in fp64, r = rh + rl in two fp32 parts, and the Taylor series are
+// summed in fp32 with their leading terms kept apart from the corrections (errors below
+// 0.8 of half a unit in the last place beside the rounding of the result; terms below
+// 2^-29 left out).  fp64 series would hold 24 more registers in constants.
 __device__ inline void turn(double delta, double omega, float& c, float& s) {
     const double x = delta * omega;
     const double k = rint(x * 0.63661977236758134308);            // 2/pi
     double r = fma(-k, 1.5707963267948966192, x);                // pi/2, leading part
     r = fma(-k, 6.123233995736766036e-17, r);                    // pi/2, trailing part
     const int q = (int)fma(-4.0, floor(k * 0.25), k);            // k mod 4
-    const double z = r * r;
-    double ps = fma(z, 1.0 / 362880.0, -1.0 / 5040.0);           // 1/9!, -1/7!
-    ps = fma(z, ps, 1.0 / 120.0);
-    ps = fma(z, ps, -1.0 / 6.0);
-    const double sr = fma(r * z, ps, r);
-    double pc = fma(z, -1.0 / 3628800.0, 1.0 / 40320.0);         // -1/10!, 1/8!
-    pc = fma(z, pc, -1.0 / 720.0);
-    pc = fma(z, pc, 1.0 / 24.0);
-    pc = fma(z, pc, -0.5);
-    const double cr = fma(z, pc, 1.0);
-    const float sa = (float)((q & 1) ? cr : sr);
-    const float ca = (float)((q & 1) ? sr : cr);
+    const float rh = (float)r, rl = (float)(r - (double)rh);
+    const float z = rh * rh, zl = fmaf(rh, rh, -z) + 2.f * rh * rl, hz = 0.5f * z;
+    // sin r = rh + (rl (1 - z/2) + rh z (-1/3! + z/5! - z^2/7! + z^3/9!))
+    float ps = fmaf(z, 2.75573192e-6f, -1.98412698e-4f);
+    ps = fmaf(z, ps, 8.33333333e-3f);
+    ps = fmaf(z, ps, -0.166666667f);
+    const float sr = rh + fmaf(rh * z, ps, fmaf(-hz, rl, rl));
+    // cos r = (1 - z/2) + (what that rounding lost - zl/2 + z^2 (1/4! - z/6! + z^2/8! - z^3/10!))
+    float pc = fmaf(z, -2.75573192e-7f, 2.48015873e-5f);
+    pc = fmaf(z, pc, -1.38888889e-3f);
+    pc = fmaf(z, pc, 4.16666667e-2f);
+    const float w = 1.f - hz, lost = (1.f - w) - hz;
+    const float cr = w + fmaf(z * z, pc, fmaf(-0.5f, zl, lost));
+    const float sa = (q & 1) ? cr : sr;
+    const float ca = (q & 1) ? sr : cr;
     s = (q & 2) ? -sa : sa;
     c = ((q + 1) & 2) ? -ca : ca;
 }
@@ -109,7 +126,7 @@ __device__ inline uint32_t swap1(uint32_t v) { return (uint32_t)dpp<0xb1>((int)v
 
 // D: head size.  SUBS: waves (of 32 slots) per scale block.  INTER: interleaved pairs.
 template <int D, int SUBS, bool F32, bool INTER>
-__global__ __launch_bounds__(kWaves * 64) void store_kernel(StoreArgs a, StoreGeo g, Freqs ft) {
+__global__ __launch_bounds__(kWaves * 64, D == 64 ? 5 : F32 ? 3 : 4) void store_kernel(StoreArgs a, StoreGeo g, Freqs ft) {
     constexpr int LPT = D / 16;           // lanes per row
     constexpr int TPS = 64 / LPT;         // rows per step
     constexpr int STEPS = kSub / TPS;
@@ -129,7 +146,15 @@ __global__ __launch_bounds__(kWaves * 64) void store_kernel(StoreArgs a, StoreGe
     const int rest = working ? unit / a.n_kv_heads : 0;
     const int tensor = rest % g.tensors, layer = rest / g.tensors;
     const bool is_k = tensor == 0;
+    // whether any unit of this workgroup is of the keys: units u0 .. share a layer and tensor in runs of heads
+    const int u0 = (blockIdx.y * g.parts + part) * (kWaves / SUBS);
+    bool has_keys = false;
+#pragma unroll
+    for (int i = 0; i < kWaves / SUBS; ++i)
+        has_keys = has_keys || (u0 + i < g.units && (u0 + i) / a.n_kv_heads % g.tensors == 0);
 
+    // The first look at the records (below) is under way before this segment's own is here.
+    StoreSegment look = a.segs[min(lane, a.n_segs - 1)];
     const StoreSegment mine = a.segs[seg_i];
     const bool teller = blockIdx.y == 0 && part == 0 && threadIdx.x == 0 && k0 == 0;   // reports what is out of range
     auto flag = [&]() __attribute__((always_inline)) {
@@ -192,124 +217,69 @@ __global__ __launch_bounds__(kWaves * 64) void store_kernel(StoreArgs a, StoreGe
         const int old = working ? (int)*scale_at : 0;
         uint8_t* const rows = dst + at * dst_page + (int64_t)(inside + sub * kSub + row0) * dst_row;
 
-        // Which record fills which slot: those that touch the block, by number (a slot that two
-        // records name goes to the first); one below this segment's owns the block. 
-        auto touches = [&](int j) __attribute__((always_inline)) {
-            const StoreSegment s = a.segs[min(j, a.n_segs - 1)];
-            return j < a.n_segs && s.seq == mine.seq && s.n_tokens > 0 && s.dst_pos0 < block_end &&
-                   (int64_t)s.dst_pos0 + s.n_tokens > slot0;
-        };
-        int64_t off[STEPS];   // of the row in the source, bytes; a row that exists where a lane has none
-        int rec[STEPS];       // its record's place among those that touch the block, -1 none
+        // Which record fills which slot: this segment's own, then the others that touch the block, by
+        // number (a slot that two records name goes to the first); one below this segment's owns the
+        // block.  The own rows are under way while the others are looked for, 64 records at a time.
+        int rec[STEPS];       // the record's place among those that touch the block, -1 none
+        int64_t off[STEPS];   // its row in the source, bytes; a row that exists where a lane has none
 #pragma unroll
         for (int t = 0; t < STEPS; ++t) {
-            off[t] = 0;
             rec[t] = -1;
+            off[t] = 0;
         }
-        int records = 0;
-        bool owner = true;
-#pragma unroll 1
-        for (int j0 = 0; j0 < a.n_segs && owner; j0 += 64) {
-            uint64_t hits = __builtin_amdgcn_ballot_w64(touches(j0 + lane));
-#pragma unroll 1
-            for (; hits; hits &= hits - 1) {
-                const int h = j0 + __builtin_ctzll(hits);
-                owner = h >= seg_i;
-                if (!owner) break;
-                const StoreSegment s = a.segs[h];
-                // the block's slots [lo, hi) that the record fills from rows that exist
-                const int64_t shift = (int64_t)s.dst_pos0 - s.src_slot0;   // slot - source slot
-                const int lo = (int)max(max(slot0, (int64_t)s.dst_pos0), shift);
-                const int hi = (int)min(min(block_end, (int64_t)s.dst_pos0 + s.n_tokens), shift + a.n_src);
+        auto assign = [&](const StoreSegment& s, int place) __attribute__((always_inline)) {
+            // the block's slots [lo, hi) that the record fills from rows that exist
+            const int64_t shift = (int64_t)s.dst_pos0 - s.src_slot0;   // slot - source slot
+            const int lo = (int)max(max(slot0, (int64_t)s.dst_pos0), shift);
+            const int hi = (int)min(min(block_end, (int64_t)s.dst_pos0 + s.n_tokens), shift + a.n_src);
 #pragma unroll
-                for (int t = 0; t < STEPS; ++t) {
-                    const int slot = first + t * TPS;
-                    if (slot >= lo && slot < hi && rec[t] < 0) {
-                        off[t] = (slot - shift) * src_row;
-                        rec[t] = records;
-                    }
+            for (int t = 0; t < STEPS; ++t) {
+                const int slot = first + t * TPS;
+                if (slot >= lo && slot < hi && rec[t] < 0) {
+                    rec[t] = place;
+                    off[t] = (slot - shift) * src_row;
                 }
-                ++records;
             }
-        }
-        if (!owner) continue;   // uniform over the workgroup
-
+        };
         Raw8<F32> raw[STEPS][2];
+        assign(mine, 0);
 #pragma unroll
         for (int t = 0; t < STEPS; ++t) {
             raw[t][0].load(src + off[t] + ca * 8 * EB);
             raw[t][1].load(src + off[t] + cb * 8 * EB);
         }
-        float x[STEPS][16];
-        auto turn_rows = [&](const StoreSegment& s, int r, bool unpack) __attribute__((always_inline)) {
-            float c[8], sn[8];
-            const bool turns = is_k && s.dst_pos0 != s.src_pos0;   // uniform
-            if (turns) {
-                // lane l evaluates pair l; the others' come through LDS (a wave's accesses are in order)
-                float c1, s1;
-                turn((double)s.dst_pos0 - (double)s.src_pos0, ft.w[lane], c1, s1);
-                asm volatile("" ::: "memory");
-                coef_lds[wave][lane] = c1;
-                coef_lds[wave][kPairs + lane] = s1;
-                __builtin_amdgcn_wave_barrier();
-                asm volatile("" ::: "memory");
+        auto hit = [&](const StoreSegment& s, int j) __attribute__((always_inline)) {
+            return j < a.n_segs && j != seg_i && s.seq == mine.seq && s.n_tokens > 0 && s.dst_pos0 < block_end &&
+                   (int64_t)s.dst_pos0 + s.n_tokens > slot0;
+        };
+        auto others = [&](int j0) __attribute__((always_inline)) {   // those among records j0 .. j0 + 63
+            if (a.n_segs > 64) look = a.segs[min(j0 + lane, a.n_segs - 1)];
+            return __builtin_amdgcn_ballot_w64(hit(look, j0 + lane));
+        };
+        int records = 1;
+        bool owner = true, moved = mine.dst_pos0 != mine.src_pos0;
+#pragma unroll 1
+        for (int j0 = 0; j0 < a.n_segs && owner; j0 += 64) {
+#pragma unroll 1
+            for (uint64_t hits = others(j0); hits; hits &= hits - 1) {
+                const int h = j0 + __builtin_ctzll(hits);
+                owner = h > seg_i;
+                if (!owner) break;
+                const StoreSegment s = a.segs[h];
+                assign(s, records);
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    // HALF: pairs 8 cl ..; INTERLEAVED: 4 pairs of each of the lane's chunks
-                    const int pair = (INTER ? (h ? (half_r + cl) * 4 : cl * 4) : cl * 8 + 4 * h) & (kPairs - 1);
-                    const f32x4 cv = *(const f32x4*)&coef_lds[wave][pair], sv = *(const f32x4*)&coef_lds[wave][kPairs + pair];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        c[4 * h + i] = cv[i];
-                        sn[4 * h + i] = sv[i];
+                for (int t = 0; t < STEPS; ++t) {
+                    if (rec[t] == records) {
+                        raw[t][0].load(src + off[t] + ca * 8 * EB);
+                        raw[t][1].load(src + off[t] + cb * 8 * EB);
                     }
                 }
+                ++records;
+                moved = moved || s.dst_pos0 != s.src_pos0;
             }
-            if (unpack) {
-#pragma unroll
-                for (int t = 0; t < STEPS; ++t)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) x[t][i] = raw[t][i >> 3].get(i & 7);
-            }
-            if (!turns) return;
-#pragma unroll
-            for (int t = 0; t < STEPS; ++t) {
-                if (!rope || rec[t] != r) continue;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int ia = INTER ? 2 * i : i, ib = INTER ? 2 * i + 1 : i + 8;
-                    const float u = x[t][ia], v = x[t][ib];
-                    x[t][ia] = fmaf(u, c[i], -(v * sn[i]));
-                    x[t][ib] = fmaf(u, sn[i], v * c[i]);
-                }
-            }
-        };
-        turn_rows(mine, 0, true);
-        // The other records' rows, found once more.
-#pragma unroll 1
-        for (int j0 = seg_i & ~63, r = 1; r < records && j0 < a.n_segs; j0 += 64) {
-            uint64_t hits = __builtin_amdgcn_ballot_w64(j0 + lane > seg_i && touches(j0 + lane));
-#pragma unroll 1
-            for (; hits; hits &= hits - 1, ++r) turn_rows(a.segs[j0 + __builtin_ctzll(hits)], r, false);
         }
+        if (!owner) continue;   // uniform over the workgroup
 
-        // The largest finite magnitude, and whether the block gets and keeps rows.
-        float m = 0.f;
-#pragma unroll
-        for (int t = 0; t < STEPS; ++t) {
-            float n = 0.f;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) n = fmaxf(n, fabsf(x[t][i]));   // (passes over a NaN)
-            m = rec[t] >= 0 ? fmaxf(m, n) : m;
-        }
-        if (__builtin_amdgcn_ballot_w64(m == INFINITY) != 0) {
-            m = 0.f;
-#pragma unroll
-            for (int t = 0; t < STEPS; ++t)
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    m = fmaxf(m, rec[t] >= 0 && fabsf(x[t][i]) < INFINITY ? fabsf(x[t][i]) : 0.f);
-        }
         bool gets = false, keeps = false;
         bool kept[STEPS];
 #pragma unroll
@@ -318,50 +288,157 @@ __global__ __launch_bounds__(kWaves * 64) void store_kernel(StoreArgs a, StoreGe
             gets |= rec[t] >= 0;
             keeps |= kept[t];
         }
-        int top = wave_max_u((int)__float_as_uint(m));
         int any = (__builtin_amdgcn_ballot_w64(gets) != 0 ? 1 : 0) | (__builtin_amdgcn_ballot_w64(keeps) != 0 ? 2 : 0);
-        if constexpr (SUBS > 1) {
-            // (two sets of words: a wave may be one block ahead)
-            if (lane == 0) {
-                top_lds[turn_no][wave] = top;
-                any_lds[turn_no][wave] = any;
-            }
-            __syncthreads();
+        int e = 0;
+
+        // From the rows to their codes.  PACKED: no row turns, and they stay in bf16, which takes half
+        // the instructions; otherwise they become fp32.  (Two copies of the code rather than a choice at
+        // each step, which would hold both forms in registers.)
+        auto quantise = [&](auto packed_tag) __attribute__((always_inline)) {
+            constexpr bool PACKED = decltype(packed_tag)::value;
+            // the fp32 bits of the largest finite magnitude
+            int top;
+            float x[PACKED ? 1 : STEPS][16];
+            if constexpr (PACKED) {
+                auto largest = [&](auto all_tag) __attribute__((always_inline)) {
+                    u16x2 m = {0, 0};
 #pragma unroll
-            for (int w = 0; w < SUBS; ++w) {
-                top = max(top, top_lds[turn_no][wave / SUBS * SUBS + w]);
-                any |= any_lds[turn_no][wave / SUBS * SUBS + w];
+                    for (int t = 0; t < STEPS; ++t)
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            u16x2 v = __builtin_bit_cast(u16x2, rec[t] >= 0 ? raw[t][i >> 2].a[i & 3] & 0x7fff7fffu : 0u);
+                            if (!decltype(all_tag)::value) {
+                                v[0] = v[0] < 0x7f80 ? v[0] : 0;
+                                v[1] = v[1] < 0x7f80 ? v[1] : 0;
+                            }
+                            m = __builtin_elementwise_max(m, v);
+                        }
+                    return max((int)m[0], (int)m[1]);
+                };
+                top = largest(std::true_type{});
+                if (__builtin_amdgcn_ballot_w64(top >= 0x7f80) != 0) top = largest(std::false_type{});
+                top <<= 16;
+            } else {
+#pragma unroll
+                for (int t = 0; t < STEPS; ++t)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) x[t][i] = raw[t][i >> 3].get(i & 7);
+                // Turn the rows of a record, the r-th that touches the block.
+                auto turn_rows = [&](const StoreSegment& s, int r) __attribute__((always_inline)) {
+                    if (!is_k || s.dst_pos0 == s.src_pos0) return;   // uniform
+                    // lane l evaluates pair l; the others' come through LDS (a wave's accesses are in order)
+                    float c1, s1;
+                    turn((double)s.dst_pos0 - (double)s.src_pos0, ft.w[lane], c1, s1);
+                    asm volatile("" ::: "memory");
+                    coef_lds[wave][lane] = c1;
+                    coef_lds[wave][kPairs + lane] = s1;
+                    __builtin_amdgcn_wave_barrier();
+                    asm volatile("" ::: "memory");
+                    float c[8], sn[8];
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        // HALF: pairs 8 cl ..; INTERLEAVED: 4 pairs of each of the lane's chunks
+                        const int pair = (INTER ? (h ? (half_r + cl) * 4 : cl * 4) : cl * 8 + 4 * h) & (kPairs - 1);
+                        const f32x4 cv = *(const f32x4*)&coef_lds[wave][pair];
+                        const f32x4 sv = *(const f32x4*)&coef_lds[wave][kPairs + pair];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            c[4 * h + i] = cv[i];
+                            sn[4 * h + i] = sv[i];
+                        }
+                    }
+#pragma unroll
+                    for (int t = 0; t < STEPS; ++t) {
+                        if (!rope || rec[t] != r) continue;
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const int ia = INTER ? 2 * i : i, ib = INTER ? 2 * i + 1 : i + 8;
+                            const float u = x[t][ia], v = x[t][ib];
+                            x[t][ia] = fmaf(u, c[i], -(v * sn[i]));
+                            x[t][ib] = fmaf(u, sn[i], v * c[i]);
+                        }
+                    }
+                };
+                turn_rows(mine, 0);
+                // The other records' rows, found once more.
+#pragma unroll 1
+                for (int j0 = 0, r = 1; r < records && j0 < a.n_segs; j0 += 64)
+#pragma unroll 1
+                    for (uint64_t hits = others(j0); hits; hits &= hits - 1, ++r)
+                        turn_rows(a.segs[j0 + __builtin_ctzll(hits)], r);
+                float m = 0.f;
+#pragma unroll
+                for (int t = 0; t < STEPS; ++t) {
+                    float n = 0.f;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) n = fmaxf(n, fabsf(x[t][i]));   // (passes over a NaN)
+                    m = rec[t] >= 0 ? fmaxf(m, n) : m;
+                }
+                if (__builtin_amdgcn_ballot_w64(m == INFINITY) != 0) {
+                    m = 0.f;
+#pragma unroll
+                    for (int t = 0; t < STEPS; ++t)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            m = fmaxf(m, rec[t] >= 0 && fabsf(x[t][i]) < INFINITY ? fabsf(x[t][i]) : 0.f);
+                }
+                top = (int)__float_as_uint(m);
             }
+            top = wave_max_u(top);
+            if constexpr (SUBS > 1) {
+                // (two sets of words: a wave may be one block ahead)
+                if (lane == 0) {
+                    top_lds[turn_no][wave] = top;
+                    any_lds[turn_no][wave] = any;
+                }
+                __syncthreads();
+#pragma unroll
+                for (int w = 0; w < SUBS; ++w) {
+                    top = max(top, top_lds[turn_no][wave / SUBS * SUBS + w]);
+                    any |= any_lds[turn_no][wave / SUBS * SUBS + w];
+                }
+            }
+            if (!working || !in_pool || !(any & 1)) return;
+            // 448 = 1.75 * 2^8 is the largest code.
+            const int need = (top >> 23) - 8 + ((top & 0x7fffff) > 0x600000 ? 1 : 0);
+            e = max(need, 1);
+            if (any & 2) e = max(e, old);
+            const float scale = __uint_as_float((uint32_t)min(e, 254) << 23);   // 2^(e - 127)
+#pragma unroll
+            for (int t = 0; t < STEPS; ++t) {
+                if (rec[t] < 0) continue;
+                uint8_t* const p = rows + (int64_t)(t * TPS) * dst_row;
+                u32x2 w[2];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    if constexpr (PACKED) {
+                        const u32x4 y = raw[t][h].a;
+                        w[h] = u32x2{pack4_bf16(y[0], y[1], scale), pack4_bf16(y[2], y[3], scale)};
+                    } else {
+                        const float* y = x[t] + 8 * h;
+                        w[h] = u32x2{pack4(y[0], y[1], y[2], y[3], scale), pack4(y[4], y[5], y[6], y[7], scale)};
+                    }
+                }
+                if (pairs) {
+                    // lanes 2m and 2m + 1 hold neighbouring chunks of either half of the row: one
+                    // takes both of the first half, the other both of the second
+                    const bool odd = lane & 1;
+                    const uint32_t g0 = swap1(odd ? w[0][0] : w[1][0]), g1 = swap1(odd ? w[0][1] : w[1][1]);
+                    const u32x4 v = odd ? u32x4{g0, g1, w[1][0], w[1][1]} : u32x4{w[0][0], w[0][1], g0, g1};
+                    __builtin_nontemporal_store(v, (u32x4*)(p + (odd ? cb - 1 : ca) * 8));
+                } else {
+                    __builtin_nontemporal_store(w[0], (u32x2*)(p + ca * 8));
+                    __builtin_nontemporal_store(w[1], (u32x2*)(p + cb * 8));
+                }
+            }
+        };
+        if constexpr (F32) {
+            quantise(std::false_type{});
+        } else {
+            if (moved && has_keys) quantise(std::false_type{});   // uniform over the workgroup
+            else quantise(std::true_type{});
         }
         if (!working || !in_pool || !(any & 1)) continue;
-        // 448 = 1.75 * 2^8 is the largest code.
-        const int need = (top >> 23) - 8 + ((top & 0x7fffff) > 0x600000 ? 1 : 0);
-        int e = max(need, 1);
-        if (any & 2) e = max(e, old);
-        const float up = __uint_as_float((uint32_t)(254 - min(e, 254)) << 23);   // 2^(127 - e)
-#pragma unroll
-        for (int t = 0; t < STEPS; ++t) {
-            if (rec[t] < 0) continue;
-            uint8_t* const p = rows + (int64_t)(t * TPS) * dst_row;
-            u32x2 w[2];
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const float* y = x[t] + 8 * h;
-                w[h][0] = pack4(y[0] * up, y[1] * up, y[2] * up, y[3] * up);
-                w[h][1] = pack4(y[4] * up, y[5] * up, y[6] * up, y[7] * up);
-            }
-            if (pairs) {
-                // lanes 2m and 2m + 1 hold neighbouring chunks of either half of the row: one
-                // takes both of the first half, the other both of the second
-                const bool odd = lane & 1;
-                const uint32_t g0 = swap1(odd ? w[0][0] : w[1][0]), g1 = swap1(odd ? w[0][1] : w[1][1]);
-                const u32x4 v = odd ? u32x4{g0, g1, w[1][0], w[1][1]} : u32x4{w[0][0], w[0][1], g0, g1};
-                __builtin_nontemporal_store(v, (u32x4*)(p + (odd ? cb - 1 : ca) * 8));
-            } else {
-                __builtin_nontemporal_store(w[0], (u32x2*)(p + ca * 8));
-                __builtin_nontemporal_store(w[1], (u32x2*)(p + cb * 8));
-            }
-        }
         if ((any & 2) && e > old) {
             // 2^(old - e): codes below 2^-18 of the largest one vanish, so no smaller factor is needed
             const float down = exp2_int(max(old - e, -126));
@@ -377,7 +454,7 @@ __global__ __launch_bounds__(kWaves * 64) void store_kernel(StoreArgs a, StoreGe
                     for (int i = 0; i < 2; ++i) {
                         const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[i], false);
                         const auto hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[i], true);
-                        w[i] = pack4(lo[0] * down, lo[1] * down, hi[0] * down, hi[1] * down);
+                        w[i] = pack4(lo[0] * down, lo[1] * down, hi[0] * down, hi[1] * down, 1.0f);
                     }
                     *q = w;
                 }
