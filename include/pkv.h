@@ -398,7 +398,8 @@ typedef struct pkv_segment_quant {
  * they must not write the same slot, and different sequences must not write into the
  * same page.  kv_len is read only: the caller raises it afterwards.
  * layout: dtype of the source, n_tokens its slots; dst_capacity the logical slots of
- * every sequence (at most 2^30); dst strides in bytes; reserved 0.  head_dim 64 or 128;
+ * every sequence (at most 2^30); dst strides in bytes; slot strides (src and dst stride[2])
+ * at most 16 MiB; reserved 0.  head_dim 64 or 128;
  * v_dim head_dim, or 0 without values.  rope_offset a multiple of 8, rope_dim of 16.
  * omega: host fp64 [rope_dim/2] per-pair frequencies as in pkv_reposition_splice_freqs,
  * or NULL for rope_theta^(-2i/rope_dim).  segs: DEVICE array; max_seg_tokens: at least

@@ -652,6 +652,11 @@ PKV_EXPORT pkv_status pkv_reposition_splice_quant(const void* src_k, const void*
             L->dst_v_stride[i] % 16)
             return fail(PKV_ERR_ALIGN, "strides must be multiples of 16 bytes");
     }
+    // The kernel addresses the rows of one block (up to 128 slots) by 32-bit byte offsets.
+    constexpr int64_t kMaxRowBytes = (int64_t)1 << 24;
+    if (L->src_k_stride[2] > kMaxRowBytes / eb || L->src_v_stride[2] > kMaxRowBytes / eb ||
+        L->dst_k_stride[2] > kMaxRowBytes || L->dst_v_stride[2] > kMaxRowBytes)
+        return fail(PKV_ERR_SHAPE, "slot strides exceed 16 MiB");
     if (!aligned16(src_k) || !aligned16(src_v) || !aligned16(k_pages) || !aligned16(v_pages))
         return fail(PKV_ERR_ALIGN, "tensor pointers must be 16-byte aligned");
     pkv::StoreArgs a;

@@ -43,14 +43,14 @@ struct Freqs {
     double w[kPairs];
 };
 
-// Launch geometry: workgroup (x, y) takes units ((y * parts + part) * per_wg ..) of
-// spot x / parts, where a spot is a segment's k-th block and a unit one (layer,
-// tensor, head); the parts of a row of heads are neighbours.
+// Grid: x = (block of the segment, part of the heads), y = segment, z = (layer,
+// tensor).  A workgroup is its waves' worth of heads of one block; with blocks of 32
+// slots and fewer heads than waves, of several consecutive blocks.
 struct StoreGeo {
-    int seg0;              // first segment of this launch
-    int spots_per_seg;     // blocks of the longest segment
+    int spots;             // x extent over the parts: groups of blocks of the longest segment
     int parts;             // workgroups that share the heads of a slot
-    int units;             // layers x tensors x heads
+    int heads;             // heads per workgroup
+    int blocks;            // blocks per workgroup: waves / (waves per block x heads)
     int tensors;           // 2, or 1 without values
     int rope_c0, rope_nc;  // rotary chunks of 8 channels: first, number
 };
@@ -135,38 +135,35 @@ __global__ __launch_bounds__(kWaves * 64, D == 64 ? 5 : F32 ? 3 : 4) void store_
     __shared__ int top_lds[2][kWaves], any_lds[2][kWaves];
     __shared__ __attribute__((aligned(16))) float coef_lds[kWaves][2 * kPairs];   // cos of all pairs, then sin
 
-    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    const int lane = threadIdx.x & 63;
-    const int spot = (int)(blockIdx.x / (uint32_t)g.parts), part = (int)(blockIdx.x - (uint32_t)spot * g.parts);
-    const int seg_i = g.seg0 + spot / g.spots_per_seg, k0 = spot % g.spots_per_seg;
-    const int unit = (blockIdx.y * g.parts + part) * (kWaves / SUBS) + wave / SUBS;
-    const bool working = unit < g.units;   // the others only meet the barriers
-    const int sub = wave % SUBS;
-    const int head = working ? unit % a.n_kv_heads : 0;
-    const int rest = working ? unit / a.n_kv_heads : 0;
-    const int tensor = rest % g.tensors, layer = rest / g.tensors;
-    const bool is_k = tensor == 0;
-    // whether any unit of this workgroup is of the keys: units u0 .. share a layer and tensor in runs of heads
-    const int u0 = (blockIdx.y * g.parts + part) * (kWaves / SUBS);
-    bool has_keys = false;
-#pragma unroll
-    for (int i = 0; i < kWaves / SUBS; ++i)
-        has_keys = has_keys || (u0 + i < g.units && (u0 + i) / a.n_kv_heads % g.tensors == 0);
-
     // The first look at the records (below) is under way before this segment's own is here.
+    const int lane = threadIdx.x & 63;
     StoreSegment look = a.segs[min(lane, a.n_segs - 1)];
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int seg_i = blockIdx.y;
     const StoreSegment mine = a.segs[seg_i];
-    const bool teller = blockIdx.y == 0 && part == 0 && threadIdx.x == 0 && k0 == 0;   // reports what is out of range
+    const int spot = g.parts == 1 ? (int)blockIdx.x : (int)(blockIdx.x / (uint32_t)g.parts);
+    const int part = (int)blockIdx.x - spot * g.parts;
+    const int tensor = g.tensors == 2 ? blockIdx.z & 1 : 0, layer = g.tensors == 2 ? blockIdx.z >> 1 : blockIdx.z;
+    const bool is_k = tensor == 0;
+    const int sub = wave % SUBS, member = wave / SUBS;   // heads fastest
+    const int in_group = g.blocks == 1 ? 0 : member / g.heads;
+    const int head_i = part * g.heads + member - in_group * g.heads;
+    const bool working = head_i < a.n_kv_heads;   // the other waves only meet the barriers
+    const int head = working ? head_i : 0;
+
+    const bool teller = blockIdx.x == 0 && blockIdx.z == 0 && threadIdx.x == 0;   // reports what is out of range
     auto flag = [&]() __attribute__((always_inline)) {
         if (a.err_flag) *a.err_flag = 1;
     };
-    const int64_t end = (int64_t)mine.dst_pos0 + mine.n_tokens;   // one past the last destination slot
     if (mine.n_tokens <= 0) return;
-    if (teller && (mine.seq < 0 || mine.seq >= a.n_seqs || mine.dst_pos0 < 0 || end > a.dst_capacity ||
+    const int64_t past = (int64_t)mine.dst_pos0 + mine.n_tokens;
+    if (teller && (mine.seq < 0 || mine.seq >= a.n_seqs || mine.dst_pos0 < 0 || past > a.dst_capacity ||
                    mine.src_slot0 < 0 || mine.src_slot0 > a.n_src - mine.n_tokens))
         flag();
     if (mine.seq < 0 || mine.seq >= a.n_seqs || a.n_src <= 0) return;
-    const int live = a.kv_len[mine.seq];
+    const int cap = (int)a.dst_capacity;   // at most 2^30: slots and block ends are int32
+    const int end = (int)min(past, (int64_t)cap);
+    const int live = min(a.kv_len[mine.seq], cap);
 
     // This lane's chunks of 8 channels: rotary lanes hold a chunk and its partner.
     const int cl = lane % LPT, row0 = lane / LPT;
@@ -188,66 +185,65 @@ __global__ __launch_bounds__(kWaves * 64, D == 64 ? 5 : F32 ? 3 : 4) void store_
     const bool pairs = !is_k || (g.rope_c0 % 2 == 0 && g.rope_nc % 4 == 0);
     const char* const src = (is_k ? a.src_k : a.src_v) + ((int64_t)layer * (is_k ? a.src_k_stride[0] : a.src_v_stride[0]) +
                                                           (int64_t)head * (is_k ? a.src_k_stride[1] : a.src_v_stride[1])) * EB;
-    const int64_t src_row = (is_k ? a.src_k_stride[2] : a.src_v_stride[2]) * EB;
+    const uint32_t src_row = (uint32_t)((is_k ? a.src_k_stride[2] : a.src_v_stride[2]) * EB);   // at most 16 MiB
     uint8_t* const dst = (is_k ? a.dst_k : a.dst_v) + (int64_t)layer * (is_k ? a.dst_k_stride[0] : a.dst_v_stride[0]) +
                          (int64_t)head * (is_k ? a.dst_k_stride[1] : a.dst_v_stride[1]);
-    const int64_t dst_row = is_k ? a.dst_k_stride[2] : a.dst_v_stride[2];
+    const uint32_t dst_row = (uint32_t)(is_k ? a.dst_k_stride[2] : a.dst_v_stride[2]);
     const int64_t dst_page = is_k ? a.dst_k_page_stride : a.dst_v_page_stride;
     const int32_t* const table =
         (!is_k && a.v_block_table ? a.v_block_table : a.block_table) + (int64_t)mine.seq * a.max_pages;
     uint8_t* const scales = (is_k ? a.k_scale : a.v_scale) + (int64_t)layer * (is_k ? a.k_scale_stride[0] : a.v_scale_stride[0]) +
                             (int64_t)head * (is_k ? a.k_scale_stride[1] : a.v_scale_stride[1]);
 
-    // The segment's blocks k0, k0 + spots_per_seg, .. (one, unless a segment is longer than the stated bound).
+    // The segment's blocks, a grid's worth apart (one, unless a segment is longer than the stated bound).
+    const int b0 = max(mine.dst_pos0, 0) / BT + spot * g.blocks + in_group, b_end = (end + BT - 1) / BT;
     int turn_no = 0;
 #pragma unroll 1
-    for (int64_t b = max((int64_t)mine.dst_pos0, (int64_t)0) / BT + k0; b * BT < min(end, a.dst_capacity);
-         b += g.spots_per_seg, turn_no ^= 1) {
-        const int64_t slot0 = b * BT;                       // the block's first slot
-        const int first = (int)slot0 + sub * kSub + row0;   // this lane's slots: first, + TPS, ..
-        const int64_t block_end = min(slot0 + BT, a.dst_capacity);
-        const int entry = (int)(slot0 >> a.page_shift);
-        const int page = table[entry];
-        const bool in_pool = (int64_t)page >= 0 && (int64_t)page < a.n_pages;
-        if (working && !in_pool && sub == 0 && lane == 0) flag();
+    for (int b = b0; b < b_end; b += g.spots * g.blocks, turn_no ^= 1) {
+        const int slot0 = b * BT;                     // the block's first slot
+        const int first = slot0 + sub * kSub + row0;  // this lane's slots: first, + TPS, ..
+        const int block_end = min(slot0 + BT, cap);
+        const int page = table[slot0 >> a.page_shift];
+        const bool in_pool = page >= 0 && page < a.n_pages;
         const int64_t at = (int64_t)(in_pool ? page : 0);
-        const int inside = (int)(slot0 & ((1 << a.page_shift) - 1));
+        const int inside = slot0 & ((1 << a.page_shift) - 1);
         uint8_t* const scale_at = scales + at * (is_k ? a.k_scale_stride[2] : a.v_scale_stride[2]) +
                                   (inside / BT) * (is_k ? a.k_scale_stride[3] : a.v_scale_stride[3]);
-        const int old = working ? (int)*scale_at : 0;
-        uint8_t* const rows = dst + at * dst_page + (int64_t)(inside + sub * kSub + row0) * dst_row;
+        uint8_t* const rows = dst + at * dst_page + (int64_t)(inside + sub * kSub) * dst_row;
 
         // Which record fills which slot: this segment's own, then the others that touch the block, by
         // number (a slot that two records name goes to the first); one below this segment's owns the
         // block.  The own rows are under way while the others are looked for, 64 records at a time.
-        int rec[STEPS];       // the record's place among those that touch the block, -1 none
-        int64_t off[STEPS];   // its row in the source, bytes; a row that exists where a lane has none
+        int rec[STEPS];   // the record's place among those that touch the block, -1 none
 #pragma unroll
-        for (int t = 0; t < STEPS; ++t) {
-            rec[t] = -1;
-            off[t] = 0;
-        }
-        auto assign = [&](const StoreSegment& s, int place) __attribute__((always_inline)) {
+        for (int t = 0; t < STEPS; ++t) rec[t] = -1;
+        // Take the slots of a record, as its `place`-th; returns the address of its first row in the block
+        // (a row that exists, where it has none) and sets *lo to that row's slot.
+        auto assign = [&](const StoreSegment& s, int place, int* lo_slot) __attribute__((always_inline)) {
             // the block's slots [lo, hi) that the record fills from rows that exist
             const int64_t shift = (int64_t)s.dst_pos0 - s.src_slot0;   // slot - source slot
-            const int lo = (int)max(max(slot0, (int64_t)s.dst_pos0), shift);
-            const int hi = (int)min(min(block_end, (int64_t)s.dst_pos0 + s.n_tokens), shift + a.n_src);
+            const int lo = (int)min(max(max((int64_t)slot0, (int64_t)s.dst_pos0), shift), (int64_t)block_end);
+            const int hi = (int)max(min(min((int64_t)block_end, (int64_t)s.dst_pos0 + s.n_tokens), shift + a.n_src), (int64_t)slot0);
 #pragma unroll
             for (int t = 0; t < STEPS; ++t) {
                 const int slot = first + t * TPS;
-                if (slot >= lo && slot < hi && rec[t] < 0) {
-                    rec[t] = place;
-                    off[t] = (slot - shift) * src_row;
-                }
+                if (slot >= lo && slot < hi && rec[t] < 0) rec[t] = place;
             }
+            *lo_slot = lo;
+            return src + (lo < hi ? (uint64_t)(lo - shift) * src_row : 0);
         };
         Raw8<F32> raw[STEPS][2];
-        assign(mine, 0);
+        {
+            int lo;
+            const char* const p = assign(mine, 0, &lo);
 #pragma unroll
-        for (int t = 0; t < STEPS; ++t) {
-            raw[t][0].load(src + off[t] + ca * 8 * EB);
-            raw[t][1].load(src + off[t] + cb * 8 * EB);
+            for (int t = 0; t < STEPS; ++t) {
+                const uint32_t off = rec[t] == 0 ? (uint32_t)(first + t * TPS - lo) * src_row : 0u;
+                raw[t][0].load(p + (off + ca * 8 * EB));
+                raw[t][1].load(p + (off + cb * 8 * EB));
+            }
         }
+        const int old = (int)*scale_at;
         auto hit = [&](const StoreSegment& s, int j) __attribute__((always_inline)) {
             return j < a.n_segs && j != seg_i && s.seq == mine.seq && s.n_tokens > 0 && s.dst_pos0 < block_end &&
                    (int64_t)s.dst_pos0 + s.n_tokens > slot0;
@@ -266,12 +262,14 @@ __global__ __launch_bounds__(kWaves * 64, D == 64 ? 5 : F32 ? 3 : 4) void store_
                 owner = h > seg_i;
                 if (!owner) break;
                 const StoreSegment s = a.segs[h];
-                assign(s, records);
+                int lo;
+                const char* const p = assign(s, records, &lo);
 #pragma unroll
                 for (int t = 0; t < STEPS; ++t) {
                     if (rec[t] == records) {
-                        raw[t][0].load(src + off[t] + ca * 8 * EB);
-                        raw[t][1].load(src + off[t] + cb * 8 * EB);
+                        const uint32_t off = (uint32_t)(first + t * TPS - lo) * src_row;
+                        raw[t][0].load(p + (off + ca * 8 * EB));
+                        raw[t][1].load(p + (off + cb * 8 * EB));
                     }
                 }
                 ++records;
@@ -284,7 +282,7 @@ __global__ __launch_bounds__(kWaves * 64, D == 64 ? 5 : F32 ? 3 : 4) void store_
         bool kept[STEPS];
 #pragma unroll
         for (int t = 0; t < STEPS; ++t) {
-            kept[t] = working && rec[t] < 0 && first + t * TPS < (int)min((int64_t)live, block_end);
+            kept[t] = working && rec[t] < 0 && first + t * TPS < min(live, block_end);
             gets |= rec[t] >= 0;
             keeps |= kept[t];
         }
@@ -407,7 +405,7 @@ __global__ __launch_bounds__(kWaves * 64, D == 64 ? 5 : F32 ? 3 : 4) void store_
 #pragma unroll
             for (int t = 0; t < STEPS; ++t) {
                 if (rec[t] < 0) continue;
-                uint8_t* const p = rows + (int64_t)(t * TPS) * dst_row;
+                uint8_t* const p = rows + (row0 + t * TPS) * dst_row;
                 u32x2 w[2];
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
@@ -435,9 +433,10 @@ __global__ __launch_bounds__(kWaves * 64, D == 64 ? 5 : F32 ? 3 : 4) void store_
         if constexpr (F32) {
             quantise(std::false_type{});
         } else {
-            if (moved && has_keys) quantise(std::false_type{});   // uniform over the workgroup
+            if (moved && is_k) quantise(std::false_type{});   // uniform over the workgroup
             else quantise(std::true_type{});
         }
+        if (working && !in_pool && sub == 0 && lane == 0) flag();
         if (!working || !in_pool || !(any & 1)) continue;
         if ((any & 2) && e > old) {
             // 2^(old - e): codes below 2^-18 of the largest one vanish, so no smaller factor is needed
@@ -445,7 +444,7 @@ __global__ __launch_bounds__(kWaves * 64, D == 64 ? 5 : F32 ? 3 : 4) void store_
 #pragma unroll
             for (int t = 0; t < STEPS; ++t) {
                 if (!kept[t]) continue;
-                uint8_t* const p = rows + (int64_t)(t * TPS) * dst_row;
+                uint8_t* const p = rows + (row0 + t * TPS) * dst_row;
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     u32x2* const q = (u32x2*)(p + (h ? cb : ca) * 8);
@@ -480,35 +479,38 @@ void launch_geo(const StoreArgs& a, const StoreGeo& g, const Freqs& f, dim3 grid
 
 namespace {
 
-// Grid of a call: per segment (x) and over the units (y).
-struct StoreGrid {
-    int64_t per_seg, y;
-};
-StoreGrid make_geo(const StoreArgs& a, StoreGeo& g) {
+dim3 make_geo(const StoreArgs& a, StoreGeo& g, bool& fits) {
     const int bt = a.block_tokens, per_wg = kWaves / (bt / kSub);
+    g.parts = (a.n_kv_heads + per_wg - 1) / per_wg;
+    // (the waves of a workgroup that meet at a barrier take one block together)
+    g.heads = per_wg;
+    if (bt == kSub && a.n_kv_heads < per_wg) g.heads = a.n_kv_heads == 3 ? 4 : a.n_kv_heads;
+    g.blocks = bt == kSub ? per_wg / g.heads : 1;
     const int64_t longest = a.max_seg_tokens < a.dst_capacity ? a.max_seg_tokens : a.dst_capacity;
-    g.spots_per_seg = (int)((longest + bt - 2) / bt + 1);   // blocks that so many slots can touch
+    const int64_t blocks = (longest + bt - 2) / bt + 1;   // that so many slots can touch
+    g.spots = (int)((blocks + g.blocks - 1) / g.blocks);
     g.tensors = a.src_v ? 2 : 1;
-    const int64_t units = (int64_t)a.n_layers * g.tensors * a.n_kv_heads;
-    g.units = units < 0x7fffffff ? (int)units : 0x7fffffff;
-    g.parts = a.n_kv_heads > per_wg ? (a.n_kv_heads + per_wg - 1) / per_wg : 1;
     g.rope_c0 = a.rope_offset / 8;
     g.rope_nc = a.rope_dim / 8;
-    const int64_t groups = (units + per_wg - 1) / per_wg;
-    return {(int64_t)g.spots_per_seg * g.parts, (groups + g.parts - 1) / g.parts};
+    const int64_t x = (int64_t)g.spots * g.parts, z = (int64_t)a.n_layers * g.tensors;
+    fits = x <= kMaxGridX && z <= 65535;
+    return dim3((unsigned)x, (unsigned)a.n_segs, (unsigned)z);
 }
 
 }  // namespace
 
 bool store_fits(const StoreArgs& a) {
     StoreGeo g;
-    const StoreGrid n = make_geo(a, g);
-    return n.y <= 65535 && n.per_seg <= kMaxGridX;
+    bool fits;
+    make_geo(a, g, fits);
+    return fits;
 }
 
 hipError_t launch_store(const StoreArgs& a, hipStream_t stream) {
     StoreGeo g;
-    const StoreGrid size = make_geo(a, g);
+    bool fits;
+    const dim3 grid = make_geo(a, g, fits);
+    if (!fits) return hipErrorInvalidValue;
     const int subs = a.block_tokens / kSub;
     Freqs f;
     if (a.omega) {
@@ -516,24 +518,16 @@ hipError_t launch_store(const StoreArgs& a, hipStream_t stream) {
     } else {
         for (int i = 0; i < kPairs; ++i) f.w[i] = i < a.rope_dim / 2 ? pow(a.theta, -2.0 * i / a.rope_dim) : 0.0;
     }
-    const int64_t at_once = kMaxGridX / size.per_seg;   // segments per launch
-    for (int64_t s = 0; s < a.n_segs; s += at_once) {
-        const int64_t n = a.n_segs - s < at_once ? a.n_segs - s : at_once;
-        g.seg0 = (int)s;
-        const dim3 grid((unsigned)(n * size.per_seg), (unsigned)size.y);
-        if (a.head_dim == 64) {
-            if (subs == 1) launch_geo<64, 1>(a, g, f, grid, stream);
-            else if (subs == 2) launch_geo<64, 2>(a, g, f, grid, stream);
-            else launch_geo<64, 4>(a, g, f, grid, stream);
-        } else {
-            if (subs == 1) launch_geo<128, 1>(a, g, f, grid, stream);
-            else if (subs == 2) launch_geo<128, 2>(a, g, f, grid, stream);
-            else launch_geo<128, 4>(a, g, f, grid, stream);
-        }
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
+    if (a.head_dim == 64) {
+        if (subs == 1) launch_geo<64, 1>(a, g, f, grid, stream);
+        else if (subs == 2) launch_geo<64, 2>(a, g, f, grid, stream);
+        else launch_geo<64, 4>(a, g, f, grid, stream);
+    } else {
+        if (subs == 1) launch_geo<128, 1>(a, g, f, grid, stream);
+        else if (subs == 2) launch_geo<128, 2>(a, g, f, grid, stream);
+        else launch_geo<128, 4>(a, g, f, grid, stream);
     }
-    return hipSuccess;
+    return hipGetLastError();
 }
 
 }  // namespace pkv
