@@ -43,6 +43,7 @@ def compile_flags():
 FILE_FLAGS = {
     "attn_mla_bf16.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
     "attn_gqa_rows.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+    "attn_gqa_rows_q8.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
     "attn_mla_rows.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
 }
 

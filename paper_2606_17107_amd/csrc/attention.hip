@@ -11,8 +11,9 @@ namespace pkv {
 hipError_t launch_attn_gqa_bf16(const AttnArgs& a, const Plan& p, const BlockScales* scales, dim3 grid,
                                 hipStream_t stream);
 hipError_t launch_attn_mla_bf16(const AttnArgs& a, const Plan& p, dim3 grid, hipStream_t stream);
-hipError_t launch_attn_gqa_rows(const AttnArgs& a, const ColPlan& p, const BlockScales* scales, dim3 grid,
-                                hipStream_t stream);
+hipError_t launch_attn_gqa_rows(const AttnArgs& a, const ColPlan& p, dim3 grid, hipStream_t stream);
+hipError_t launch_attn_gqa_rows_q8(const AttnArgs& a, const ColPlan& p, const BlockScales& scales, dim3 grid,
+                                   hipStream_t stream);
 hipError_t launch_attn_mla_rows(const AttnArgs& a, const ColPlan& p, dim3 grid, hipStream_t stream);
 
 namespace {
@@ -765,7 +766,8 @@ hipError_t launch_columns(const AttnArgs& a, const BlockScales* scales, hipStrea
     if (cols > 0x7fffffff) return hipErrorInvalidValue;
     const dim3 grid((unsigned)cols);
     const hipError_t e = a.variant == 1 ? launch_attn_mla_rows(a, p, grid, stream)
-                                        : launch_attn_gqa_rows(a, p, scales, grid, stream);
+                         : scales       ? launch_attn_gqa_rows_q8(a, p, *scales, grid, stream)
+                                        : launch_attn_gqa_rows(a, p, grid, stream);
     if (e != hipSuccess || p.columns == 0) return e;
     return launch_combine(a, true, stream);
 }

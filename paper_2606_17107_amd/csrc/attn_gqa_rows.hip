@@ -21,39 +21,31 @@
 
 #include "attn_columns.h"
 #include "attn_gqa_tile.h"
-#include "attn_gqa_tile_q8.h"
 
 namespace pkv {
 namespace {
 
 constexpr int kRowWaves = 4;
-constexpr int kRowStagesQ8 = 4;   // LDS stages of a wave over an 8-bit cache (2 of twice the bytes in bf16)
 
 __device__ inline int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
-template <int D, bool PAGED, bool Q8>
-__global__ __launch_bounds__(kRowWaves * 64, 2) void attn_gqa_rows_kernel(AttnArgs a, ColPlan p, ScaleArg<Q8> sa) {
-    static_assert(PAGED || !Q8, "a cache held in 8 bits is paged");
-    using Elem = std::conditional_t<Q8, uint8_t, uint16_t>;
+template <int D, bool PAGED>
+__global__ __launch_bounds__(kRowWaves * 64, 2) void attn_gqa_rows_kernel(AttnArgs a, ColPlan p) {
     constexpr int NW = kRowWaves;
-    constexpr int NS = Q8 ? kRowStagesQ8 : 2;   // LDS stages of a wave
     constexpr int BN = kColTile;           // keys per tile
-    constexpr int EB = sizeof(Elem);       // bytes per element of the cache
-    constexpr int CH = D * EB / 16;        // 16-byte chunks per row
+    constexpr int CH = D / 8;              // 16-byte chunks per row
     constexpr int KBLK = BN * CH / 64;     // LDS-DMA loads per K (or V) tile
     constexpr int KPB = 64 / CH;           // keys per LDS-DMA load
-    constexpr int KP = D == 128 ? (Q8 ? 2 : 4) : 1;   // LDS-DMA loads after which the K swizzle repeats
-    constexpr int VP = D == 128 && Q8 ? 2 : 1;        // ... the V swizzle
+    constexpr int KP = D == 128 ? 4 : 1;   // LDS-DMA loads after which the K swizzle repeats
     constexpr int KS = D / 16;             // MFMA k-steps over channels
     constexpr int DB = D / 32;             // 32-channel output blocks
     constexpr int TE = BN * D;             // elements of one K or V tile
     constexpr int ROWS = 32;               // rows per workgroup
-    static_assert((NS & (NS - 1)) == 0, "a power of two");
-    static_assert(2 * NS * KBLK + KBLK < 64, "loads in flight within the vmcnt range");
-    static_assert(ROWS * D * 4 <= 2 * NS * TE * EB, "a wave's O^T fits its own stages");
+    static_assert(6 * KBLK < 64, "loads in flight within the vmcnt range");
+    static_assert(ROWS * D * 4 <= 4 * TE * 2, "a wave's O^T fits its own stages");
 
-    // Per wave: K stages, then V stages; after the loop, its O^T.
-    __shared__ __attribute__((aligned(16))) Elem stage_lds[NW * 2 * NS * TE];
+    // Per wave: K stages 0 and 1, V stages 0 and 1; after the loop, its O^T.
+    __shared__ __attribute__((aligned(16))) uint16_t stage_lds[NW * 4 * TE];
     __shared__ float row_max_lds[NW][ROWS], row_sum_lds[NW][ROWS];
 
     const uint32_t column = col_decode(p);
@@ -63,15 +55,14 @@ __global__ __launch_bounds__(kRowWaves * 64, 2) void attn_gqa_rows_kernel(AttnAr
     const int j = lane & 31;
     const int hl = lane >> 5;
     const int lkey = lane / CH, phys = lane % CH;
-    Elem* const my_lds = stage_lds + wave * 2 * NS * TE;
-    auto kst = [&](int st) __attribute__((always_inline)) -> Elem* { return my_lds + st * TE; };
-    auto vst = [&](int st) __attribute__((always_inline)) -> Elem* { return my_lds + (NS + st) * TE; };
+    uint16_t* const my_lds = stage_lds + wave * 4 * TE;
+    auto kst = [&](int st) __attribute__((always_inline)) -> uint16_t* { return my_lds + st * TE; };
+    auto vst = [&](int st) __attribute__((always_inline)) -> uint16_t* { return my_lds + (2 + st) * TE; };
 
     // Per-lane LDS element offsets of the MFMA operands within a stage, as in
     // the many-row kernel.
-    int kofs[Q8 ? KS / 2 : KS], vofs[DB];
-    if constexpr (Q8) gqa_operand_offsets_q8<D>(lane, kofs, vofs);
-    else gqa_operand_offsets<D>(lane, kofs, vofs);
+    int kofs[KS], vofs[DB];
+    gqa_operand_offsets<D>(lane, kofs, vofs);
     const float sc2 = a.scale * kLog2e;
 
     // Touch the tensors that the sequence bounds lead to, so that their address
@@ -124,7 +115,7 @@ __global__ __launch_bounds__(kRowWaves * 64, 2) void attn_gqa_rows_kernel(AttnAr
                                    (int64_t)(si.q0 + qi) * a.q_stride[1] + (int64_t)head * a.q_stride[2];
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks)
-                qf[ks] = __builtin_bit_cast(bf16x8, *(const u32x4*)(qrow + (Q8 ? q8_channel(ks, hl) : ks * 16 + hl * 8)));
+                qf[ks] = __builtin_bit_cast(bf16x8, *(const u32x4*)(qrow + ks * 16 + hl * 8));
         }
         int row_start, row_end;
         visible_range(qpos, si.kvl, a.window, row_start, row_end);   // (0, 0) for rows past M
@@ -141,33 +132,26 @@ __global__ __launch_bounds__(kRowWaves * 64, 2) void attn_gqa_rows_kernel(AttnAr
         const int n_tiles = t_end > t_begin ? (t_end - t_begin + NW - 1) / NW : 0;
         auto key_of = [&](int i) __attribute__((always_inline)) { return lo + (t_begin + i * NW) * BN; };
 
-        const char* const kbase = (const char*)((const Elem*)a.k + (int64_t)layer * a.k_stride[0] +
+        const char* const kbase = (const char*)((const uint16_t*)a.k + (int64_t)layer * a.k_stride[0] +
                                                 (int64_t)kvh * a.k_stride[1] + si.base * a.k_stride[2]);
-        const char* const vbase = (const char*)((const Elem*)a.v + (int64_t)layer * a.v_stride[0] +
+        const char* const vbase = (const char*)((const uint16_t*)a.v + (int64_t)layer * a.v_stride[0] +
                                                 (int64_t)kvh * a.v_stride[1] + si.base * a.v_stride[2]);
-        const int64_t krow = a.k_stride[2] * EB, vrow = a.v_stride[2] * EB;   // bytes between keys
+        const int64_t krow = a.k_stride[2] * 2, vrow = a.v_stride[2] * 2;   // bytes between keys
         PageWindow kw, vw;
         if constexpr (PAGED) {
             kw.init(a.block_table, a, sg.seq, key_of(0) >> a.page_shift);
             if (a.v_block_table) vw.init(a.v_block_table, a, sg.seq, key_of(0) >> a.page_shift);
         }
-        // In 8 bits: the exponents of this wave's next tiles' scales.
-        ScaleWindow scale_win;
-        if constexpr (Q8) scale_win.load(a, sa, sg.seq, layer, kvh, 0, n_tiles, key_of);
         // LDS-DMA of one tile of one tensor.  Lane l of load b fills LDS chunk
         // slot 64 b + l: key KPB b + l / CH, physical chunk l % CH, holding logical
         // chunk phys ^ swizzle(key).  The K swizzle repeats every KP loads, the
-        // V swizzle every VP.  A tile that runs past the last visible key
+        // V swizzle every load.  A tile that runs past the last visible key
         // re-reads that key for the missing rows (masked later).
         uint32_t kchunk[KP];
 #pragma unroll
-        for (int b = 0; b < KP; ++b)
-            kchunk[b] = (uint32_t)(phys ^ (Q8 ? swz_k8<D>(b * KPB + lkey) : swz_k<D>(b * KPB + lkey))) * 16u;
-        uint32_t vchunk[VP];
-#pragma unroll
-        for (int b = 0; b < VP; ++b)
-            vchunk[b] = (uint32_t)(phys ^ (Q8 ? swz_v8<D>(b * KPB + lkey) : swz_v<D>(lkey))) * 16u;
-        auto issue = [&](const char* tile, int64_t row_bytes, int t0, Elem* dst, auto v_tag) __attribute__((always_inline)) {
+        for (int b = 0; b < KP; ++b) kchunk[b] = (uint32_t)(phys ^ swz_k<D>(b * KPB + lkey)) * 16u;
+        const uint32_t vchunk = (uint32_t)(phys ^ swz_v<D>(lkey)) * 16u;
+        auto issue = [&](const char* tile, int64_t row_bytes, int t0, uint16_t* dst, auto v_tag) __attribute__((always_inline)) {
             constexpr bool V = decltype(v_tag)::value;
             const uint32_t lds0 = lds_addr_of(dst);
             if (t0 + BN <= hi) {
@@ -175,7 +159,7 @@ __global__ __launch_bounds__(kRowWaves * 64, 2) void attn_gqa_rows_kernel(AttnAr
                 uint64_t at = uniform_u64((uint64_t)(uintptr_t)tile);
 #pragma unroll
                 for (int b = 0; b < KBLK; ++b) {
-                    lds_dma16(lds0 + b * 1024, (const void*)at, lane_off + (V ? vchunk[b % VP] : kchunk[b % KP]));
+                    lds_dma16(lds0 + b * 1024, (const void*)at, lane_off + (V ? vchunk : kchunk[b % KP]));
                     at += (uint64_t)(KPB * row_bytes);
                     asm volatile("" : "+s"(at));   // step by step: KBLK hoisted offsets would spill scalar registers
                 }
@@ -185,35 +169,36 @@ __global__ __launch_bounds__(kRowWaves * 64, 2) void attn_gqa_rows_kernel(AttnAr
 #pragma unroll
                 for (int b = 0; b < KBLK; ++b)
                     lds_dma16(lds0 + b * 1024, tile, (uint32_t)(min(b * KPB + key0, hi - 1 - t0) * row_bytes) +
-                                                        (V ? vchunk[b % VP] : kchunk[b % KP]));
+                                                        (V ? vchunk : kchunk[b % KP]));
             }
         };
         auto issue_k = [&](int i) __attribute__((always_inline)) {
             const int t0 = key_of(i);
             const char* tile;
-            if constexpr (PAGED) tile = kbase + kw.offset(a, t0, a.k_page_stride * EB, krow);
+            if constexpr (PAGED) tile = kbase + kw.offset(a, t0, a.k_page_stride * 2, krow);
             else tile = kbase + (int64_t)t0 * krow;
-            issue(tile, krow, t0, kst(i & (NS - 1)), std::false_type{});
+            issue(tile, krow, t0, kst(i & 1), std::false_type{});
         };
         auto issue_v = [&](int i) __attribute__((always_inline)) {
             const int t0 = key_of(i);
             const char* tile;
             if constexpr (PAGED) {
-                const int64_t off = a.v_block_table ? vw.offset(a, t0, a.v_page_stride * EB, vrow)
-                                                    : kw.offset(a, t0, a.v_page_stride * EB, vrow);
+                const int64_t off = a.v_block_table ? vw.offset(a, t0, a.v_page_stride * 2, vrow)
+                                                    : kw.offset(a, t0, a.v_page_stride * 2, vrow);
                 tile = vbase + off;
             } else {
                 tile = vbase + (int64_t)t0 * vrow;
             }
-            issue(tile, vrow, t0, vst(i & (NS - 1)), std::true_type{});
+            issue(tile, vrow, t0, vst(i & 1), std::true_type{});
         };
-        static_for<0, NS>([&](auto i_tag) {
-            constexpr int i = decltype(i_tag)::value;
-            if (n_tiles > i) {
-                issue_k(i);
-                issue_v(i);
-            }
-        });
+        if (n_tiles > 0) {
+            issue_k(0);
+            issue_v(0);
+        }
+        if (n_tiles > 1) {
+            issue_k(1);
+            issue_v(1);
+        }
 
         f32x16 o[DB];
 #pragma unroll
@@ -227,22 +212,12 @@ __global__ __launch_bounds__(kRowWaves * 64, 2) void attn_gqa_rows_kernel(AttnAr
         // One tile: S^T = K Q^T, online softmax with a lazily moved reference
         // maximum (probabilities stay below 2^kLazy), O^T += V^T P^T.
         constexpr float kLazy = 8.0f;
-        auto scores = [&](const Elem* ks_src, uint32_t es) __attribute__((always_inline)) {
+        auto scores = [&](const uint16_t* ks_src) __attribute__((always_inline)) {
             f32x16 s = f32x16{};
-            if constexpr (Q8) {
-                const float scale = q8_k_scale(es);
 #pragma unroll
-                for (int c = 0; c < KS / 2; ++c) {   // one read holds the codes of two k-steps
-                    const u32x4 w = *(const u32x4*)(ks_src + kofs[c]);
-                    s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(q8_to_bf16(w[0], w[1], scale), qf[2 * c], s, 0, 0, 0);
-                    s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(q8_to_bf16(w[2], w[3], scale), qf[2 * c + 1], s, 0, 0, 0);
-                }
-            } else {
-#pragma unroll
-                for (int ks = 0; ks < KS; ++ks) {
-                    const bf16x8 kf = __builtin_bit_cast(bf16x8, *(const u32x4*)(ks_src + kofs[ks]));
-                    s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[ks], s, 0, 0, 0);
-                }
+            for (int ks = 0; ks < KS; ++ks) {
+                const bf16x8 kf = __builtin_bit_cast(bf16x8, *(const u32x4*)(ks_src + kofs[ks]));
+                s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[ks], s, 0, 0, 0);
             }
             return s;
         };
@@ -300,107 +275,38 @@ __global__ __launch_bounds__(kRowWaves * 64, 2) void attn_gqa_rows_kernel(AttnAr
                 lsum = __builtin_amdgcn_fdot2_f32_bf16((bf16x2){pb[e >> 3][e & 7], pb[e >> 3][(e & 7) + 1]}, ones, lsum, false);
             l_run += lsum;
         };
-        auto add_values = [&](const Elem* vs_src, uint32_t es, const bf16x8 (&pb)[2]) __attribute__((always_inline)) {
+        auto add_values = [&](const uint16_t* vs_src, const bf16x8 (&pb)[2]) __attribute__((always_inline)) {
 #pragma unroll
             for (int st = 0; st < 2; ++st)
 #pragma unroll
-                for (int db = 0; db < DB; ++db) {
-                    bf16x8 vf;
-                    if constexpr (Q8) {
-                        const u32x2 w = q8_v_read(vs_src + vofs[db] + st * 16 * D);
-                        vf = q8_to_bf16(w[0], w[1], q8_v_scale(es));
-                    } else {
-                        vf = gqa_v_operand<D>(vs_src + vofs[db] + st * 16 * D);
-                    }
-                    o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pb[st], o[db], 0, 0, 0);
-                }
+                for (int db = 0; db < DB; ++db)
+                    o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(gqa_v_operand<D>(vs_src + vofs[db] + st * 16 * D),
+                                                                    pb[st], o[db], 0, 0, 0);
         };
-        // In 8 bits, for a tile with keys that some row does not see: true if it has NaN
-        // codes, which then reach only the rows that see their key.
-        auto add_nan_values = [&](const Elem* vs_src, uint32_t es, int t0, const bf16x8 (&pb)[2]) __attribute__((always_inline)) {
-            if constexpr (Q8) {
-                u32x2 w[2 * DB];
-                uint32_t nans = 0;
-#pragma unroll
-                for (int q = 0; q < 2 * DB; ++q) {
-                    w[q] = q8_v_read(vs_src + vofs[q % DB] + (q / DB) * 16 * D);
-                    nans |= q8_nan_bytes(w[q][0]) | q8_nan_bytes(w[q][1]);
-                }
-                if (__builtin_amdgcn_ballot_w64(nans != 0) == 0) return false;
-#pragma unroll
-                for (int st = 0; st < 2; ++st) {
-                    f32x8 seen;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const int key = t0 + st * 16 + (e >> 2) * 8 + hl * 4 + (e & 3);
-                        seen[e] = key < row_end && key >= row_start ? 1.0f : 0.0f;
-                    }
-                    const bf16x8 sees = __builtin_convertvector(seen, bf16x8);
-#pragma unroll
-                    for (int db = 0; db < DB; ++db) {
-                        bf16x8 vf, nf;
-                        q8_split_nan(w[st * DB + db], q8_v_scale(es), vf, nf);
-                        o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pb[st], o[db], 0, 0, 0);
-                        const f32x16 n = __builtin_amdgcn_mfma_f32_32x32x16_bf16(nf, sees, f32x16{}, 0, 0, 0);
-#pragma unroll
-                        for (int r = 0; r < 16; ++r) o[db][r] = n[r] > 0.f ? __builtin_nanf("") : o[db][r];
-                    }
-                }
-                return true;
-            }
-            return false;
-        };
-        // Loads retire in order: K(i), V(i), K(i+1), V(i+1), .., then K(i+NS) once
-        // the scores of tile i have been read, V(i+NS) once its values have.  Wait
-        // until `tiles` whole tiles and `more` loads beyond them are in flight.
-        auto wait_tiles = [&](int tiles, auto more_tag) __attribute__((always_inline)) {
-            constexpr int MORE = decltype(more_tag)::value;
-            static_for<0, NS>([&](auto k_tag) {
-                constexpr int K = decltype(k_tag)::value;
-                if (tiles == K) wait_vmcnt<K * 2 * KBLK + MORE>();
-            });
-        };
+        // Loads retire in order: K(i), V(i), K(i+1), V(i+1), then K(i+2) once
+        // the scores of tile i have been read, V(i+2) once its values have.
         auto tile = [&](int i, int st) __attribute__((always_inline)) {
             const int t0 = key_of(i);
-            const bool more = i + 1 < n_tiles, refill = i + NS < n_tiles;
-            uint32_t es = 0;
-            if constexpr (Q8) {
-                if (!scale_win.holds(i, i)) scale_win.load(a, sa, sg.seq, layer, kvh, i, n_tiles, key_of);
-                es = scale_win.at(i);
-            }
-            if constexpr (NS == 2) {
-                if (more) wait_vmcnt<3 * KBLK>();
-                else wait_vmcnt<KBLK>();
-            } else {
-                wait_tiles(min(NS - 1, n_tiles - 1 - i), std::integral_constant<int, KBLK>{});
-            }
+            const bool more = i + 1 < n_tiles, more2 = i + 2 < n_tiles;
+            if (more) wait_vmcnt<3 * KBLK>();
+            else wait_vmcnt<KBLK>();
             asm volatile("" ::: "memory");
-            f32x16 s = scores(kst(st), es);
+            f32x16 s = scores(kst(st));
             lds_reads_done();
-            if (refill) issue_k(i + NS);
+            if (more2) issue_k(i + 2);
             bf16x8 pb[2];
-            [[maybe_unused]] const bool masked = t0 + BN > e_min || t0 < s_max;
             if (t0 + BN > e_min || t0 < s_max) softmax(t0, s, pb, std::true_type{});
             else softmax(t0, s, pb, std::false_type{});
-            if constexpr (NS == 2) {
-                if (refill) wait_vmcnt<3 * KBLK>();
-                else if (more) wait_vmcnt<2 * KBLK>();
-                else wait_vmcnt<0>();
-            } else {
-                if (refill) wait_vmcnt<(NS - 1) * 2 * KBLK + KBLK>();
-                else wait_tiles(n_tiles - 1 - i, std::integral_constant<int, 0>{});
-            }
+            if (more2) wait_vmcnt<3 * KBLK>();
+            else if (more) wait_vmcnt<2 * KBLK>();
+            else wait_vmcnt<0>();
             asm volatile("" ::: "memory");
-            if constexpr (Q8) {
-                if (!(masked && add_nan_values(vst(st), es, t0, pb))) add_values(vst(st), es, pb);
-            } else {
-                add_values(vst(st), es, pb);
-            }
+            add_values(vst(st), pb);
             lds_reads_done();
-            if (refill) issue_v(i + NS);
+            if (more2) issue_v(i + 2);
         };
 #pragma unroll 1
-        for (int i = 0; i < n_tiles; ++i) tile(i, i & (NS - 1));
+        for (int i = 0; i < n_tiles; ++i) tile(i, i & 1);
 
         // Merge the four waves: O^T to this wave's stages (row-major fp32,
         // 16-byte chunks XOR-swizzled by row), maxima and sums beside.
@@ -418,30 +324,25 @@ __global__ __launch_bounds__(kRowWaves * 64, 2) void attn_gqa_rows_kernel(AttnAr
             row_sum_lds[wave][j] = l_tot;
         }
         __syncthreads();
-        col_merge_rows<NW, ROWS, D>(a, p, sg, si, layer, kvh * p.G, p.G, M, (const float*)stage_lds, 2 * NS * TE * EB / 4,
+        col_merge_rows<NW, ROWS, D>(a, p, sg, si, layer, kvh * p.G, p.G, M, (const float*)stage_lds, 2 * TE,
                                     &row_max_lds[0][0], &row_sum_lds[0][0]);
         __syncthreads();   // the stages are free for the next item
     }
 }
 
 template <int D>
-hipError_t launch_d(const AttnArgs& a, const ColPlan& p, const BlockScales* scales, dim3 grid, hipStream_t stream) {
-    const ScaleArg<false> none;
-    if (scales)
-        hipLaunchKernelGGL((attn_gqa_rows_kernel<D, true, true>), grid, dim3(kRowWaves * 64), 0, stream, a, p,
-                           ScaleArg<true>{*scales});
-    else if (a.block_table)
-        hipLaunchKernelGGL((attn_gqa_rows_kernel<D, true, false>), grid, dim3(kRowWaves * 64), 0, stream, a, p, none);
+hipError_t launch_d(const AttnArgs& a, const ColPlan& p, dim3 grid, hipStream_t stream) {
+    if (a.block_table)
+        hipLaunchKernelGGL((attn_gqa_rows_kernel<D, true>), grid, dim3(kRowWaves * 64), 0, stream, a, p);
     else
-        hipLaunchKernelGGL((attn_gqa_rows_kernel<D, false, false>), grid, dim3(kRowWaves * 64), 0, stream, a, p, none);
+        hipLaunchKernelGGL((attn_gqa_rows_kernel<D, false>), grid, dim3(kRowWaves * 64), 0, stream, a, p);
     return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_attn_gqa_rows(const AttnArgs& a, const ColPlan& p, const BlockScales* scales, dim3 grid,
-                                hipStream_t stream) {
-    return a.head_dim == 64 ? launch_d<64>(a, p, scales, grid, stream) : launch_d<128>(a, p, scales, grid, stream);
+hipError_t launch_attn_gqa_rows(const AttnArgs& a, const ColPlan& p, dim3 grid, hipStream_t stream) {
+    return a.head_dim == 64 ? launch_d<64>(a, p, grid, stream) : launch_d<128>(a, p, grid, stream);
 }
 
 }  // namespace pkv
