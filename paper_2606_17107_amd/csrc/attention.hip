@@ -761,7 +761,7 @@ hipError_t launch_columns(const AttnArgs& a, const BlockScales* scales, hipStrea
     // (set-up, first loads and merge: about 7 us), in tiles of one workgroup at head
     // size 128; the tiles of head size 64 take half as long, with the same counts.
     p.min_tiles = a.variant == 1 ? 4 : 8;
-    p.item_cost = a.variant == 1 ? 4 : 12;
+    p.item_cost = a.variant == 1 ? 4 : a.dtype == 2 ? 24 : 12;
     const int64_t cols = p.columns ? p.columns : (col_items(a) + kXcds - 1) / kXcds * kXcds;
     if (cols > 0x7fffffff) return hipErrorInvalidValue;
     const dim3 grid((unsigned)cols);
