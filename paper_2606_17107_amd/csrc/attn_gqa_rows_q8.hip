@@ -2,10 +2,10 @@
 // generation and short suffixes (paper Sec. 5 "Linear-time TTFT"; Sec. 4 erratum).
 //
 // The work is shared out as in attn_gqa_rows.hip: workgroups take equal runs of the
-// tile axis (attn_columns.h), the four waves of a workgroup every fourth tile, each
+// tile axis (attn_columns.h), the waves of a workgroup take its tiles in turn, each
 // through LDS stages of its own without a barrier, and are merged at the end.  What
-// differs is the tile loop.  A tile of codes is half the bytes of a bf16 one, and one
-// wave a SIMD has half the time for it, which the steps of a tile one after another
+// differs is the tile loop.  A tile of codes is half the bytes of a bf16 one, and a
+// wave has half the time for it, which the steps of a tile one after another
 // (scores, maximum, probabilities, values) exceed.  So, as in the many-row kernel, the
 // score MFMAs of the next tile are interleaved with the probabilities of this one, and
 // this one's value MFMAs with the maxima of the next one's scores; codes are turned
@@ -18,15 +18,50 @@
 namespace pkv {
 namespace {
 
-constexpr int kWaves = 4;
+// Waves of a workgroup (one a CU) and LDS stages of a wave.  Head size 128: one wave a
+// SIMD, which needs 290 registers, and deep staging.  Head size 64: two waves a SIMD hide
+// each other's latencies (16 caches of 8448..12544 slots, 2 KV heads: 29.7 us a call with
+// four waves of 8 stages, 27.6 with eight of 4, 25.5 with eight of 2).
+template <int D>
+constexpr int row_waves() { return D == 128 ? 4 : 8; }
+template <int D>
+constexpr int row_stages() { return D == 128 ? 4 : 2; }
 constexpr int kAhead = 3;   // LDS operand reads issued this many operands ahead of their MFMA
 
 __device__ inline int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
+// What the wave's next 64 tiles need of the tables, tile first + l in lane l: the pages of
+// K and V (clamped into the pool) and the exponents of their scales, K's in the low byte
+// and V's in the next.  Loading it stalls the loop for two dependent loads, once in
+// about 60 tiles.
+struct TileWindow {
+    int first;
+    int k_page, v_page, exps;
+
+    template <typename F>
+    __device__ __forceinline__ void load(const AttnArgs& a, const BlockScales& s, int seq, int layer, int kvh, int from,
+                                         int n_tiles, F key_of) {
+        first = from;
+        k_page = v_page = exps = 0;
+        if (n_tiles <= 0) return;
+        const int key = key_of(min(from + (int)__lane_id(), n_tiles - 1));   // (below the slots that the table covers)
+        const int64_t entry = (int64_t)seq * a.max_pages + (key >> a.page_shift);
+        const int block = (key & ((1 << a.page_shift) - 1)) >> s.block_shift;
+        const int top = (int)(a.n_pages - 1);
+        k_page = min(max(a.block_table[entry], 0), top);
+        v_page = a.v_block_table ? min(max(a.v_block_table[entry], 0), top) : k_page;
+        const uint8_t* const k = s.k + layer * s.k_stride[0] + kvh * s.k_stride[1];
+        const uint8_t* const v = s.v + layer * s.v_stride[0] + kvh * s.v_stride[1];
+        exps = k[k_page * s.k_stride[2] + block * s.k_stride[3]] | (v[v_page * s.v_stride[2] + block * s.v_stride[3]] << 8);
+    }
+    __device__ __forceinline__ bool holds(int i) const { return i < first + 64; }   // (tiles are visited in order)
+    __device__ __forceinline__ int of(int reg, int i) const { return __builtin_amdgcn_readlane(reg, (i - first) & 63); }
+};
+
 template <int D>
-__global__ __launch_bounds__(kWaves * 64, 1) void attn_gqa_rows_q8_kernel(AttnArgs a, ColPlan p, BlockScales sa) {
-    constexpr int NW = kWaves;
-    constexpr int NS = D == 128 ? 4 : 8;   // LDS stages of a wave: 32 KB of codes
+__global__ __launch_bounds__(row_waves<D>() * 64, D == 128 ? 1 : 2) void attn_gqa_rows_q8_kernel(AttnArgs a, ColPlan p, BlockScales sa) {
+    constexpr int NW = row_waves<D>();
+    constexpr int NS = row_stages<D>();
     constexpr int BN = kColTile;           // keys per tile
     constexpr int CH = D / 16;             // 16-byte chunks per row
     constexpr int KBLK = BN * CH / 64;     // LDS-DMA loads per K (or V) tile
@@ -127,12 +162,9 @@ __global__ __launch_bounds__(kWaves * 64, 1) void attn_gqa_rows_q8_kernel(AttnAr
         const char* const kbase = (const char*)a.k + (int64_t)layer * a.k_stride[0] + (int64_t)kvh * a.k_stride[1];
         const char* const vbase = (const char*)a.v + (int64_t)layer * a.v_stride[0] + (int64_t)kvh * a.v_stride[1];
         const int64_t krow = a.k_stride[2], vrow = a.v_stride[2];   // bytes between keys
-        PageWindow kw, vw;
-        kw.init(a.block_table, a, sg.seq, key_of(0) >> a.page_shift);
-        if (a.v_block_table) vw.init(a.v_block_table, a, sg.seq, key_of(0) >> a.page_shift);
-        // The exponents of this wave's next tiles' scales.
-        ScaleWindow scale_win;
-        scale_win.load(a, sa, sg.seq, layer, kvh, 0, n_tiles, key_of);
+        TileWindow win;
+        win.load(a, sa, sg.seq, layer, kvh, 0, n_tiles, key_of);
+        const int page_mask = (1 << a.page_shift) - 1;
 
         // LDS-DMA of one tile of one tensor.  Lane l of load b fills LDS chunk
         // slot 64 b + l: key KPB b + l / CH, physical chunk l % CH, holding logical
@@ -167,13 +199,11 @@ __global__ __launch_bounds__(kWaves * 64, 1) void attn_gqa_rows_q8_kernel(AttnAr
         };
         auto issue_k = [&](int i) __attribute__((always_inline)) {
             const int t0 = key_of(i);
-            issue(kbase + kw.offset(a, t0, a.k_page_stride, krow), krow, t0, kst(i), std::false_type{});
+            issue(kbase + win.of(win.k_page, i) * a.k_page_stride + (t0 & page_mask) * krow, krow, t0, kst(i), std::false_type{});
         };
         auto issue_v = [&](int i) __attribute__((always_inline)) {
             const int t0 = key_of(i);
-            const int64_t off = a.v_block_table ? vw.offset(a, t0, a.v_page_stride, vrow)
-                                                : kw.offset(a, t0, a.v_page_stride, vrow);
-            issue(vbase + off, vrow, t0, vst(i), std::true_type{});
+            issue(vbase + win.of(win.v_page, i) * a.v_page_stride + (t0 & page_mask) * vrow, vrow, t0, vst(i), std::true_type{});
         };
 #pragma unroll 1
         for (int i = 0; i < min(NS, n_tiles); ++i) {
@@ -367,54 +397,58 @@ __global__ __launch_bounds__(kWaves * 64, 1) void attn_gqa_rows_q8_kernel(AttnAr
             asm volatile("" ::: "memory");
         };
         uint32_t es_cur = 0;   // exponents of the tile whose scores are held
-        auto values = [&](int i, const bf16x8 (&pb)[2], const f32x16& nxt, auto nxt_tag) __attribute__((always_inline)) {
-            constexpr bool NXT = decltype(nxt_tag)::value;
-            const int t0 = key_of(i);
-            float mx;
-            if (masked(t0) && nan_codes(vst(i))) {
-                add_nan_values(vst(i), es_cur, t0, pb);
-                mx = -INFINITY;
-                if (NXT) {
+        auto all_probabilities = [&](const f32x16& s, bf16x8 (&pb)[2]) __attribute__((always_inline)) {
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) mx = fmaxf(mx, nxt[r]);
-                }
-            } else {
-                mx = seg2(vst(i), es_cur, pb, nxt, nxt_tag);
+            for (int h = 0; h < 2; ++h) {
+                f32x8 pv8;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) pv8[e] = probability(s[h * 8 + e]);
+                pb[h] = __builtin_convertvector(pv8, bf16x8);
             }
-            lds_reads_done();
+        };
+        auto maximum = [&](const f32x16& s) __attribute__((always_inline)) {
+            float mx = s[0];
+#pragma unroll
+            for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
             return mx;
         };
-        // Tile i's probabilities and values, and the scores of tile i + 1.
+        // Tile i's probabilities and values, and the scores of tile i + 1; tile i has no hidden key.
         auto step = [&](int i, f32x16& cur, f32x16& nxt) __attribute__((always_inline)) {
             wait_step(n_tiles - 1 - i);
-            if (!scale_win.holds(i + 1, i + 1)) scale_win.load(a, sa, sg.seq, layer, kvh, i + 1, n_tiles, key_of);
-            const uint32_t es = scale_win.at(i + 1);
+            const uint32_t es = win.of(win.exps, i + 1);
             bf16x8 pb[2];
             seg1(kst(i + 1), es, cur, nxt, pb, std::true_type{});
             lds_reads_done();
             if (i + 1 + NS < n_tiles) issue_k(i + 1 + NS);
             if (masked(key_of(i + 1))) hide(key_of(i + 1), nxt);
-            const float mx = values(i, pb, nxt, std::true_type{});
+            const float mx = seg2(vst(i), es_cur, pb, nxt, std::true_type{});
+            lds_reads_done();
             if (i + NS < n_tiles) issue_v(i + NS);
             es_cur = es;
             move_max(both(mx));
         };
-        auto drain = [&](int i, f32x16& cur) __attribute__((always_inline)) {
-            wait_step(0);
+        // The same for any tile, the last one too, without overlap.
+        auto plain = [&](int i, f32x16& cur) __attribute__((always_inline)) {
+            wait_step(n_tiles - 1 - i);
             bf16x8 pb[2];
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                f32x8 pv8;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) pv8[e] = probability(cur[h * 8 + e]);
-                pb[h] = __builtin_convertvector(pv8, bf16x8);
-            }
-            values(i, pb, cur, std::false_type{});
+            all_probabilities(cur, pb);
+            if (masked(key_of(i)) && nan_codes(vst(i))) add_nan_values(vst(i), es_cur, key_of(i), pb);
+            else seg2(vst(i), es_cur, pb, cur, std::false_type{});
+            lds_reads_done();
+            if (i + 1 >= n_tiles) return;
+            es_cur = win.of(win.exps, i + 1);
+            bf16x8 none[2];
+            seg1(kst(i + 1), es_cur, cur, cur, none, std::false_type{});
+            lds_reads_done();
+            if (i + 1 + NS < n_tiles) issue_k(i + 1 + NS);
+            if (i + NS < n_tiles) issue_v(i + NS);
+            if (masked(key_of(i + 1))) hide(key_of(i + 1), cur);
+            move_max(both(maximum(cur)));
         };
         if (n_tiles > 0) {
             f32x16 s_a, s_b;
             bf16x8 none[2];
-            es_cur = scale_win.at(0);
+            es_cur = win.of(win.exps, 0);
             if (n_tiles >= NS) wait_vmcnt<(2 * NS - 1) * KBLK>();
             else static_for<1, NS>([&](auto k_tag) {
                 constexpr int K = decltype(k_tag)::value;
@@ -425,25 +459,21 @@ __global__ __launch_bounds__(kWaves * 64, 1) void attn_gqa_rows_q8_kernel(AttnAr
             lds_reads_done();
             if (NS < n_tiles) issue_k(NS);
             if (masked(key_of(0))) hide(key_of(0), s_a);
-            float mx = -INFINITY;
-#pragma unroll
-            for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s_a[r]);
-            move_max(both(mx));
-            int i = 0;
+            move_max(both(maximum(s_a)));
+            // Tiles with hidden keys come first (a window's start) and last.
 #pragma unroll 1
-            for (; i + 2 < n_tiles; i += 2) {
-                step(i, s_a, s_b);
-                step(i + 1, s_b, s_a);
+            for (int i = 0; i < n_tiles; ++i) {
+                if (!win.holds(i + 1 + NS)) win.load(a, sa, sg.seq, layer, kvh, i, n_tiles, key_of);
+                if (i + 1 < n_tiles && !masked(key_of(i))) {
+                    step(i, s_a, s_b);
+                    s_a = s_b;
+                } else {
+                    plain(i, s_a);
+                }
             }
-            if (i + 1 < n_tiles) {
-                step(i, s_a, s_b);
-                s_a = s_b;
-                ++i;
-            }
-            drain(i, s_a);
         }
 
-        // Merge the four waves: O^T to this wave's stages (row-major fp32,
+        // Merge the waves: O^T to this wave's stages (row-major fp32,
         // 16-byte chunks XOR-swizzled by row), maxima and sums beside.
         constexpr int OC = D / 4;   // 16-byte fp32 chunks per row
         float* const my_o = (float*)my_lds;
@@ -469,9 +499,10 @@ __global__ __launch_bounds__(kWaves * 64, 1) void attn_gqa_rows_q8_kernel(AttnAr
 
 hipError_t launch_attn_gqa_rows_q8(const AttnArgs& a, const ColPlan& p, const BlockScales& scales, dim3 grid,
                                    hipStream_t stream) {
-    const dim3 block(kWaves * 64);
-    if (a.head_dim == 64) hipLaunchKernelGGL((attn_gqa_rows_q8_kernel<64>), grid, block, 0, stream, a, p, scales);
-    else hipLaunchKernelGGL((attn_gqa_rows_q8_kernel<128>), grid, block, 0, stream, a, p, scales);
+    if (a.head_dim == 64)
+        hipLaunchKernelGGL((attn_gqa_rows_q8_kernel<64>), grid, dim3(row_waves<64>() * 64), 0, stream, a, p, scales);
+    else
+        hipLaunchKernelGGL((attn_gqa_rows_q8_kernel<128>), grid, dim3(row_waves<128>() * 64), 0, stream, a, p, scales);
     return hipGetLastError();
 }
 
