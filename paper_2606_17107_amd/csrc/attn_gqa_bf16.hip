@@ -18,8 +18,14 @@
 //   * V stays row-major ([key][channel]) in LDS; the transposed A operand of
 //     the PV product comes from ds_read_b64_tr_b16, with the keys of each
 //     16-key step ordered as the P^T accumulator holds them.
-//   * A cache held in 8 bits (Q8, paged): the same schedule over tiles of codes,
-//     which become bf16 at the operand registers (attn_gqa_tile_q8.h).
+//   * A cache held in 8 bits (Q8, paged): tiles in LDS are bf16 tiles like any
+//     other.  A wave loads its share of a tile's codes into registers two tiles
+//     before they go to their stage, and converts and writes them among the MFMAs
+//     of segment 2.  1024 queries of 28 heads over 50176 slots: 786 us (938 TF/s),
+//     as long as over the bf16 cache; 904 us with codes in LDS that every wave
+//     converts at its operand reads (four times the conversions), 926 us with all
+//     of a step's conversions before its MFMAs, conditions around its loads (the
+//     compiler then waits for the newest) and LDS writes two to a bank.
 #include <type_traits>
 
 #include "attn_gqa_tile.h"
@@ -44,7 +50,6 @@ enum { kFull, kFew, kOrdered };
 template <int D, bool PAGED, int FORM, bool Q8>
 __global__ __launch_bounds__(kWaves * 64, 2) void attn_gqa_bf16_kernel(AttnArgs a, Plan p, ScaleArg<Q8> sa) {
     static_assert(PAGED || !Q8, "a cache held in 8 bits is paged");
-    using Elem = std::conditional_t<Q8, uint8_t, uint16_t>;
     // The arguments of the set-up are asked for together: left alone, their loads sink
     // to their uses, one scalar round trip after another (64 queries x 4 heads over
     // 8256 keys, 8 kv heads: 30.0 us a call, 29.6 with this).
@@ -52,8 +57,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_gqa_bf16_kernel(AttnArgs 
                  "s"(a.q_pos), "s"(a.kv_len), "s"(a.cu_q), "s"(a.kv_base), "s"(a.cache_slots), "s"(a.total_q),
                  "s"(a.max_kv_len), "s"(a.window), "s"(a.n_kv_heads), "s"(a.n_layers));
     constexpr int QB = kQB, NW = kWaves, NS = kStages;
-    constexpr int EB = sizeof(Elem);       // bytes per element of the cache
-    constexpr int CH = D * EB / 16;        // 16-byte chunks per row
+    constexpr int CH = D / 8;              // 16-byte chunks per row
     constexpr int BN = 32;                 // keys per tile
     constexpr int NKB = BN / 32;           // 32-key blocks per tile
     constexpr int KBLK = BN * CH / 64;     // 64-lane LDS-DMA blocks per K (or V) tile
@@ -68,10 +72,11 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_gqa_bf16_kernel(AttnArgs 
     // compile-time constants after unrolling, so one address register per
     // operand serves every stage through the 16-bit immediate offset of the
     // LDS read (K stages within 48 KB of the block, V stages of the V half).
-    __shared__ __attribute__((aligned(16))) Elem stage_lds[2 * NS * TE];
+    __shared__ __attribute__((aligned(16))) uint16_t stage_lds[2 * NS * TE];
     __shared__ int red[NW], red_min[NW], red_start[NW], red_smax[NW];
-    auto kst = [&](int st) __attribute__((always_inline)) -> Elem* { return stage_lds + st * TE; };
-    auto vst = [&](int st) __attribute__((always_inline)) -> Elem* { return stage_lds + (NS + st) * TE; };
+    __shared__ int nan_lds[1];   // 8 bits: NaN codes were left out of a tile that not every row sees whole
+    auto kst = [&](int st) __attribute__((always_inline)) -> uint16_t* { return stage_lds + st * TE; };
+    auto vst = [&](int st) __attribute__((always_inline)) -> uint16_t* { return stage_lds + (NS + st) * TE; };
 
     int group, rb;
     if (!decode(p, group, rb)) return;
@@ -88,7 +93,8 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_gqa_bf16_kernel(AttnArgs 
     if (m0 >= M) return;
 
     const int tid = threadIdx.x;
-    const int wave = tid >> 6;
+    int wave = tid >> 6;
+    if constexpr (Q8) wave = __builtin_amdgcn_readfirstlane(wave);   // scalar addresses and branches
     const int lane = tid & 63;
     const int j = lane & 31;
     const int hl = lane >> 5;
@@ -124,7 +130,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_gqa_bf16_kernel(AttnArgs 
         for (int ks = 0; ks < KS; ++ks) v[ks] = u32x4{0u, 0u, 0u, 0u};
         if (FORM == kFull || row_ok[qb]) {
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) v[ks] = *(const u32x4*)(qrow + (Q8 ? q8_channel(ks, hl) : ks * 16 + hl * 8));
+            for (int ks = 0; ks < KS; ++ks) v[ks] = *(const u32x4*)(qrow + ks * 16 + hl * 8);
         }
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) qf[qb][ks] = __builtin_bit_cast(bf16x8, v[ks]);
@@ -146,6 +152,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_gqa_bf16_kernel(AttnArgs 
     const int wmax = wave_max_i(rmax);
     const int wsmin = wave_min_i(smin);
     const int wsmax = wave_max_i(smax);   // tiles below this need the window mask
+    if constexpr (Q8) nan_lds[0] = 0;
     if (lane == 0) {
         red[wave] = wmax;
         red_min[wave] = wmin;
@@ -172,6 +179,8 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_gqa_bf16_kernel(AttnArgs 
     const int loop_end = min(hi, k_begin + run);
     const int n_tiles = loop_end > k_begin ? (loop_end - k_begin + BN - 1) / BN : 0;
 
+    using Elem = std::conditional_t<Q8, uint8_t, uint16_t>;   // of the cache
+    constexpr int EB = sizeof(Elem);
     const Elem* kbase = (const Elem*)a.k + (int64_t)layer * a.k_stride[0] +
                         (int64_t)kvh * a.k_stride[1] + si.base * a.k_stride[2];
     const Elem* vbase = (const Elem*)a.v + (int64_t)layer * a.v_stride[0] +
@@ -193,8 +202,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_gqa_bf16_kernel(AttnArgs 
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
         const int key = dma_key(i);
-        const int logical = (lane % CH) ^ (wave_v ? (Q8 ? swz_v8<D>(key) : swz_v<D>(key))
-                                                  : (Q8 ? swz_k8<D>(key) : swz_k<D>(key)));
+        const int logical = (lane % CH) ^ (wave_v ? swz_v<D>(key) : swz_k<D>(key));
         src_off[i] = (uint32_t)(key * trow + logical * 16);
     }
     // Stage the tile starting at key t0.  A tile that runs past the last
@@ -203,16 +211,16 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_gqa_bf16_kernel(AttnArgs 
     // size, so each tile lies in one page.
     PageWindow pw;
     // Waves that move V blocks read V's own block table when there is one.
-    if constexpr (PAGED)
+    if constexpr (PAGED && !Q8)
         pw.init(wave_v && a.v_block_table ? a.v_block_table : a.block_table, a, seq, k_begin >> a.page_shift);
     const int64_t tpage = (wave_v ? a.v_page_stride : a.k_page_stride) * EB;   // bytes between pages
-    auto issue = [&](int t0, Elem* ks_dst, Elem* vs_dst) __attribute__((always_inline)) {
+    auto issue = [&](int t0, uint16_t* ks_dst, uint16_t* vs_dst) __attribute__((always_inline)) {
         const char* tile;
         if constexpr (PAGED)
             tile = tens + pw.offset(a, t0, tpage, trow);
         else
             tile = tens + (int64_t)t0 * trow;
-        const uint32_t lds0 = lds_addr_of((wave_v ? vs_dst : ks_dst) + blk0 * 64 * (16 / EB));
+        const uint32_t lds0 = lds_addr_of((wave_v ? vs_dst : ks_dst) + blk0 * 64 * 8);
         if (t0 + BN <= loop_end) {
 #pragma unroll
             for (int i = 0; i < PER; ++i) lds_dma16(lds0 + i * 1024, tile, src_off[i]);
@@ -225,30 +233,13 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_gqa_bf16_kernel(AttnArgs 
         }
     };
 
-    // An operand as it is read from LDS (k_read, v_read) and as it enters the MFMA
-    // (k_value, v_value): the same in bf16; in 8 bits one read holds the codes of two
-    // k-steps, and es has the exponents of the tile's scales.
-    constexpr int KR = Q8 ? KS / 2 : KS;   // K reads per tile
-    constexpr int KQ = KS / KR;            // k-steps of one
-    int kofs[KR], vofs[DB];
-    if constexpr (Q8) gqa_operand_offsets_q8<D>(lane, kofs, vofs);
-    else gqa_operand_offsets<D>(lane, kofs, vofs);
-    auto k_read = [&](const Elem* ks_src, int kr, int kb) __attribute__((always_inline)) {
-        const u32x4 w = *(const u32x4*)(ks_src + kofs[kr] + kb * 32 * D);
-        if constexpr (Q8) return w;
-        else return __builtin_bit_cast(bf16x8, w);
+    int kofs[KS], vofs[DB];
+    gqa_operand_offsets<D>(lane, kofs, vofs);
+    auto k_operand = [&](const uint16_t* ks_src, int ks, int kb) __attribute__((always_inline)) {
+        return __builtin_bit_cast(bf16x8, *(const u32x4*)(ks_src + kofs[ks] + kb * 32 * D));
     };
-    auto k_value = [&](const auto& w, int ks, uint32_t es) __attribute__((always_inline)) {
-        if constexpr (Q8) return q8_to_bf16(w[(ks & 1) * 2], w[(ks & 1) * 2 + 1], q8_k_scale(es));
-        else return w;
-    };
-    auto v_read = [&](const Elem* vs_src, int st, int db) __attribute__((always_inline)) {
-        if constexpr (Q8) return q8_v_read(vs_src + vofs[db] + st * 16 * D);
-        else return gqa_v_operand<D>(vs_src + vofs[db] + st * 16 * D);
-    };
-    auto v_value = [&](const auto& w, uint32_t es) __attribute__((always_inline)) {
-        if constexpr (Q8) return q8_to_bf16(w[0], w[1], q8_v_scale(es));
-        else return w;
+    auto v_operand = [&](const uint16_t* vs_src, int st, int db) __attribute__((always_inline)) {
+        return gqa_v_operand<D>(vs_src + vofs[db] + st * 16 * D);
     };
 
     f32x16 o[DB][QB];
@@ -267,7 +258,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_gqa_bf16_kernel(AttnArgs 
     const float sc2 = a.scale * kLog2e;
 
     // Raw scores S^T = K Q^T of the tile held in K stage ks_src.
-    auto qk = [&](const Elem* ks_src, uint32_t es, f32x16 (&s)[NKB][QB]) __attribute__((always_inline)) {
+    auto qk = [&](const uint16_t* ks_src, f32x16 (&s)[NKB][QB]) __attribute__((always_inline)) {
 #pragma unroll
         for (int kb = 0; kb < NKB; ++kb)
 #pragma unroll
@@ -276,14 +267,14 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_gqa_bf16_kernel(AttnArgs 
         for (int ks = 0; ks < KS; ++ks) {
 #pragma unroll
             for (int kb = 0; kb < NKB; ++kb) {
-                const bf16x8 kf = k_value(k_read(ks_src, ks / KQ, kb), ks, es);
+                const bf16x8 kf = k_operand(ks_src, ks, kb);
 #pragma unroll
                 for (int qb = 0; qb < QB; ++qb)
                     s[kb][qb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[qb][ks], s[kb][qb], 0, 0, 0);
             }
         }
         // Keep the K-operand reads one or two MFMAs ahead instead of all at once.
-        if constexpr (!Q8) sched_reads_mfma<NKB * KS, 1, QB>();
+        sched_reads_mfma<NKB * KS, 1, QB>();
     };
 
     // Softmax, part 1 (branchy, before the overlapped region): mask the raw
@@ -369,7 +360,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_gqa_bf16_kernel(AttnArgs 
     };
 
     // O^T += V^T P^T for the tile held in V stage vs_src.
-    auto pv = [&](const Elem* vs_src, uint32_t es, const bf16x8 (&pb)[QB][2 * NKB]) __attribute__((always_inline)) {
+    auto pv = [&](const uint16_t* vs_src, const bf16x8 (&pb)[QB][2 * NKB]) __attribute__((always_inline)) {
         // Lane group g (16 lanes) reads channels 32db + 16(g&1) .. +15 for
         // keys {16st + 8b + 4(g>>1) + 0..3}, b = 0, 1: the key order of the
         // P^T accumulator rows.
@@ -377,46 +368,13 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_gqa_bf16_kernel(AttnArgs 
         for (int st = 0; st < 2 * NKB; ++st) {
 #pragma unroll
             for (int db = 0; db < DB; ++db) {
-                const bf16x8 vf = v_value(v_read(vs_src, st, db), es);
+                const bf16x8 vf = v_operand(vs_src, st, db);
 #pragma unroll
                 for (int qb = 0; qb < QB; ++qb)
                     o[db][qb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pb[qb][st], o[db][qb], 0, 0, 0);
             }
         }
-        if constexpr (!Q8) sched_reads_mfma<2 * NKB * DB, 2, QB>();
-    };
-    // The same in 8 bits for a tile that has NaN codes and keys that some row does not
-    // see: a NaN reaches only the rows that see its key.
-    auto nan_codes = [&](const auto* vs_src) __attribute__((always_inline)) {
-        uint32_t nans = 0;
-#pragma unroll
-        for (int q = 0; q < 2 * DB; ++q) {
-            const auto w = v_read(vs_src, q / DB, q % DB);
-            nans |= q8_nan_bytes(w[0]) | q8_nan_bytes(w[1]);
-        }
-        return __builtin_amdgcn_ballot_w64(nans != 0) != 0;
-    };
-    auto pv_nan = [&](const auto* vs_src, uint32_t es, int t0, const bf16x8 (&pb)[QB][2 * NKB]) __attribute__((always_inline)) {
-        static_assert(QB == 1 && NKB == 1, "one row block and key block");
-#pragma unroll
-        for (int st = 0; st < 2; ++st) {
-            f32x8 seen;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int key = t0 + st * 16 + (e >> 2) * 8 + hl * 4 + (e & 3);
-                seen[e] = key < row_end[0] && key >= row_start[0] ? 1.0f : 0.0f;
-            }
-            const bf16x8 sees = __builtin_convertvector(seen, bf16x8);
-#pragma unroll
-            for (int db = 0; db < DB; ++db) {
-                bf16x8 vf, nf;
-                q8_split_nan(v_read(vs_src, st, db), q8_v_scale(es), vf, nf);
-                o[db][0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pb[0][st], o[db][0], 0, 0, 0);
-                const f32x16 n = __builtin_amdgcn_mfma_f32_32x32x16_bf16(nf, sees, f32x16{}, 0, 0, 0);
-#pragma unroll
-                for (int r = 0; r < 16; ++r) o[db][0][r] = n[r] > 0.f ? __builtin_nanf("") : o[db][0][r];
-            }
-        }
+        sched_reads_mfma<2 * NKB * DB, 2, QB>();
     };
 
     // Processing order.  The pipelined schedule takes the F tiles that need
@@ -431,22 +389,6 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_gqa_bf16_kernel(AttnArgs 
         const int t = i < F ? i + n_lead : (i < F + n_lead ? i - F : i);
         return k_begin + t * BN;
     };
-
-    // In 8 bits: the exponents of the tiles' scales, for the tiles from `first` on.
-    ScaleWindow scale_win;
-    auto load_scales = [&](int first) __attribute__((always_inline)) {
-        if constexpr (Q8) scale_win.load(a, sa, seq, layer, kvh, first, n_tiles, key_of);
-    };
-    auto more_scales = [&](int first, int last) __attribute__((always_inline)) {   // tiles first .. last are next
-        if constexpr (Q8) {
-            if (!scale_win.holds(first, last)) load_scales(first);
-        }
-    };
-    auto exponents = [&](int i) __attribute__((always_inline)) -> uint32_t {
-        if constexpr (Q8) return scale_win.at(i);
-        else return 0u;
-    };
-    load_scales(0);
 
     // Tiles are staged through NS LDS stages: tile i lives in stage i % NS
     // and is issued NS-1 tiles ahead of its use.  Wait until at most
@@ -463,39 +405,104 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_gqa_bf16_kernel(AttnArgs 
     };
     auto lds_reads_done = []() __attribute__((always_inline)) { __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (0 << 8) | (3 << 14)); };
 
+    // In 8 bits: tile i's codes, this wave's share of them, in register set i % 2 from two steps before
+    // they go to the tile's stage: PER pieces of 64 lanes of 8 codes, which become the lanes' 16-byte
+    // chunks of the bf16 tile.  Consecutive lanes write consecutive chunks, at D = 64 of odd keys the other
+    // half of the row first, so that the 8 lanes of an LDS cycle cover its banks.  Tiles past the last one
+    // repeat it: without conditions around loads and conversions the compiler waits for just the set it
+    // needs.  Keys past the last visible one are read (their page is whole) and masked.
+    const int blk8 = (wave * PER - (wave_v ? KBLK : 0)) / 2;   // of KBLK / 2 blocks of 64 lanes of 16 codes
+    u32x2 codes[2][PER];
+    int lds8[PER];       // bytes from the stage's K tile
+    uint32_t off8[PER];  // bytes from the tile's first key
+    CodeWindow win;
+    if constexpr (Q8) {
+#pragma unroll
+        for (int n = 0; n < PER; ++n) {
+            const int slot = (blk8 + n / 2) * 64 + lane, key = slot / (CH / 2);
+            const int c = slot % (CH / 2) + ((n ^ (D == 64 ? key : 0)) & 1) * (CH / 2);
+            off8[n] = (uint32_t)(key * trow + c * 8);
+            lds8[n] = ((wave_v ? NS * TE : 0) + key * D + ((c ^ (wave_v ? swz_v<D>(key) : swz_k<D>(key))) << 3)) * 2;
+        }
+        win.init(a, sa, wave_v, seq, layer, kvh);
+        win.load(a, 0, n_tiles, key_of);
+    }
+    auto load_codes = [&](int i, u32x2 (&set)[PER]) __attribute__((always_inline)) {
+        i = min(i, n_tiles - 1);
+        const char* const tile = tens + win.page(i) * tpage + (key_of(i) & ((1 << a.page_shift) - 1)) * trow;
+#pragma unroll
+        for (int n = 0; n < PER; ++n) set[n] = *(const u32x2*)(tile + off8[n]);
+    };
+    auto put_codes = [&](u32x2 piece, float scale, char* dst) __attribute__((always_inline)) {
+        *(bf16x8*)dst = q8_to_bf16(piece[0], piece[1], scale);
+    };
+    // A tile with keys that some row does not see must not bring NaN values (0 * NaN): they are left out
+    // here and come back, to the rows that see them, at the end.
+    auto hides = [&](int t0) __attribute__((always_inline)) { return t0 + BN > e_min || t0 < s_max; };
+    auto leave_out_nan = [&](int i, u32x2 (&set)[PER]) __attribute__((always_inline)) {
+        if (wave_v && hides(key_of(i))) {
+            uint32_t nans = 0;
+#pragma unroll
+            for (int n = 0; n < PER; ++n) nans |= q8_nan_bytes(set[n][0]) | q8_nan_bytes(set[n][1]);
+            if (__builtin_amdgcn_ballot_w64(nans != 0) != 0) {
+                nan_lds[0] = 1;
+#pragma unroll
+                for (int n = 0; n < PER; ++n)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) set[n][e] &= ~((q8_nan_bytes(set[n][e]) >> 7) * 0xffu);
+            }
+        }
+    };
+    auto stage_codes = [&](int i, u32x2 (&set)[PER], uint16_t* ks_dst) __attribute__((always_inline)) {
+        i = min(i, n_tiles - 1);
+        leave_out_nan(i, set);
+        const float scale = win.scale(i);
+#pragma unroll
+        for (int n = 0; n < PER; ++n) put_codes(set[n], scale, (char*)ks_dst + lds8[n]);
+    };
+    // Fill the stage that tile i - 1 left (behind the barrier that opens step i): with tile i + NS - 1.
+    auto refill = [&](int i, auto stage_tag) __attribute__((always_inline)) {
+        constexpr int S = (decltype(stage_tag)::value + NS - 1) % NS;   // stage of tile i + NS - 1
+        const int ahead = i + NS - 1;
+        if constexpr (Q8) {
+            stage_codes(ahead, codes[S & 1], kst(S));
+            load_codes(ahead + 2, codes[S & 1]);
+        } else {
+            if (ahead < n_tiles) issue(key_of(ahead), kst(S), vst(S));
+        }
+    };
+    // Before the NS steps from i on, which stage tiles up to i + 2 NS - 2 and load two more.
+    auto more_tiles = [&](int i) __attribute__((always_inline)) {
+        if constexpr (Q8) {
+            if (i + 2 * NS >= win.last && win.last < n_tiles) win.load(a, i, n_tiles, key_of);
+        }
+    };
+
     // One tile in plain order: wait for it, then QK^T, softmax and PV back to
     // back.  The barrier that publishes tile i also proves every wave finished
     // tile i-1, so tile i-1's stage is refilled with tile i+NS-1 right after.
     auto plain_tile = [&](int i, auto stage_tag) __attribute__((always_inline)) {
         constexpr int S = decltype(stage_tag)::value;
-        wait_outstanding(min(i + NS - 2, n_tiles - 1) - i);
+        if constexpr (!Q8) wait_outstanding(min(i + NS - 2, n_tiles - 1) - i);
         lds_reads_done();
         bare_barrier();
-        const int ahead = i + NS - 1;
-        if (ahead < n_tiles) issue(key_of(ahead), kst((S + NS - 1) % NS), vst((S + NS - 1) % NS));
+        refill(i, stage_tag);
         f32x16 sc[NKB][QB];
-        const int t0 = key_of(i);
-        const uint32_t es = exponents(i);
-        qk(kst(S), es, sc);
+        qk(kst(S), sc);
         bf16x8 pb[QB][2 * NKB];
+        const int t0 = key_of(i);
         if (t0 + BN > wmin || t0 < wsmax) {
             row_max(t0, sc, std::true_type{});
             probs(t0, sc, pb, std::true_type{});
-            if constexpr (Q8) {
-                if (nan_codes(vst(S))) {
-                    pv_nan(vst(S), es, t0, pb);
-                    return;
-                }
-            }
         } else {
             row_max(t0, sc, std::false_type{});
             probs(t0, sc, pb, std::false_type{});
         }
-        pv(vst(S), es, pb);
+        pv(vst(S), pb);
     };
     auto plain_from = [&](int first) __attribute__((always_inline)) {
         for (int t = first - first % NS; t < n_tiles; t += NS) {
-            more_scales(t, t + NS - 1);
+            more_tiles(t);
             static_for<0, NS>([&](auto s_tag) {
                 const int i = t + decltype(s_tag)::value;
                 if (i >= first && i < n_tiles) plain_tile(i, s_tag);
@@ -503,9 +510,24 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_gqa_bf16_kernel(AttnArgs 
         }
     };
 
+    if constexpr (Q8) {
+        static_assert(NS == 4, "tiles 0 .. 2 are staged, 3 and 4 in registers");
+        if (n_tiles > 0) {
+            u32x2 first[3][PER];
 #pragma unroll
-    for (int s = 0; s < NS - 1; ++s)
-        if (s < n_tiles) issue(key_of(s), kst(s), vst(s));
+            for (int s = 0; s < 3; ++s) load_codes(s, first[s]);
+            load_codes(3, codes[1]);
+            asm volatile("" ::: "memory");   // in this order, which the loop's waits count on
+            load_codes(4, codes[0]);
+#pragma unroll
+            for (int s = 0; s < 3; ++s)
+                if (s < n_tiles) stage_codes(s, first[s], kst(s));
+        }
+    } else {
+#pragma unroll
+        for (int s = 0; s < NS - 1; ++s)
+            if (s < n_tiles) issue(key_of(s), kst(s), vst(s));
+    }
 
     {
         // Intra-wave software pipeline over the leading tiles that need no
@@ -535,23 +557,19 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_gqa_bf16_kernel(AttnArgs 
         // Written as fenced groups of one K operand's MFMAs, their share of
         // the VALU work and the operand read kAhead steps ahead, so
         // the LDS reads stay in flight across MFMAs.
-        // (In 8 bits an operand is converted one group ahead of its MFMAs.)
-        auto seg1 = [&](const Elem* ks_src, uint32_t es, int kbn, f32x16 (&cur)[QB], f32x16 (&nxt)[QB],
+        auto seg1 = [&](const uint16_t* ks_src, int kbn, f32x16 (&cur)[QB], f32x16 (&nxt)[QB],
                         bf16x8 (&pb)[QB][2]) __attribute__((always_inline)) {
-            constexpr int A = kAhead < KR ? kAhead : KR;
+            constexpr int A = kAhead < KS ? kAhead : KS;
             constexpr int PER_K = 16 / KS;   // probabilities per k-step and row block
-            decltype(k_read(ks_src, 0, kbn)) kop[KR];
+            bf16x8 kop[KS];
 #pragma unroll
-            for (int q = 0; q < A; ++q) kop[q] = k_read(ks_src, q, kbn);
+            for (int q = 0; q < A; ++q) kop[q] = k_operand(ks_src, q, kbn);
             __builtin_amdgcn_sched_barrier(0);
-            bf16x8 kf;
-            if constexpr (Q8) kf = k_value(kop[0], 0, es);
 #pragma unroll
             for (int q = 0; q < KS; ++q) {
 #pragma unroll
                 for (int qb = 0; qb < QB; ++qb) {
-                    if constexpr (!Q8) kf = kop[q];
-                    nxt[qb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[qb][q], q == 0 ? f32x16{} : nxt[qb],
+                    nxt[qb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kop[q], qf[qb][q], q == 0 ? f32x16{} : nxt[qb],
                                                                      0, 0, 0);
                     const float neg_m = -m_run[qb];
 #pragma unroll
@@ -567,10 +585,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_gqa_bf16_kernel(AttnArgs 
                         }
                     }
                 }
-                if (q % KQ == KQ - 1 && q / KQ + A < KR) kop[q / KQ + A] = k_read(ks_src, q / KQ + A, kbn);
-                if constexpr (Q8) {
-                    if (q + 1 < KS) kf = k_value(kop[(q + 1) / KQ], q + 1, es);
-                }
+                if (q + A < KS) kop[q + A] = k_operand(ks_src, q + A, kbn);
                 __builtin_amdgcn_sched_barrier(0);
             }
         };
@@ -578,18 +593,17 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_gqa_bf16_kernel(AttnArgs 
         // Segment 2: O^T += V^T P^T for key block kbc of the V stage; the row
         // maxima of nxt (over both lanes of a row, into mx) and the row sums
         // of pb alongside, in fenced groups as in segment 1.
-        auto seg2 = [&](const Elem* vs_src, uint32_t es, int kbc, const bf16x8 (&pb)[QB][2], const f32x16 (&nxt)[QB],
-                        float (&mx)[QB]) __attribute__((always_inline)) {
+        // more(q): further work to put beside operand q's MFMAs.
+        auto seg2 = [&](const uint16_t* vs_src, int kbc, const bf16x8 (&pb)[QB][2], const f32x16 (&nxt)[QB],
+                        float (&mx)[QB], auto more) __attribute__((always_inline)) {
             constexpr int NQ = 2 * DB;                 // V operands: two 16-key steps x DB channel blocks
             constexpr int A = kAhead < NQ ? kAhead : NQ;
             constexpr int PER_M = 16 / NQ;             // maxima per operand and row block
             constexpr int PER_D = 8 / NQ > 0 ? 8 / NQ : 1;   // sum steps per operand and row block
-            decltype(v_read(vs_src, 0, 0)) vop[NQ];
+            bf16x8 vop[NQ];
 #pragma unroll
-            for (int q = 0; q < A; ++q) vop[q] = v_read(vs_src, 2 * kbc + q / DB, q % DB);
+            for (int q = 0; q < A; ++q) vop[q] = v_operand(vs_src, 2 * kbc + q / DB, q % DB);
             __builtin_amdgcn_sched_barrier(0);
-            bf16x8 vf;
-            if constexpr (Q8) vf = v_value(vop[0], es);
             float m0[QB], m1[QB], l0[QB], l1[QB];
 #pragma unroll
             for (int qb = 0; qb < QB; ++qb) {
@@ -603,8 +617,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_gqa_bf16_kernel(AttnArgs 
                 const int h = q / DB, db = q % DB;
 #pragma unroll
                 for (int qb = 0; qb < QB; ++qb) {
-                    if constexpr (!Q8) vf = vop[q];
-                    o[db][qb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pb[qb][h], o[db][qb], 0, 0, 0);
+                    o[db][qb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vop[q], pb[qb][h], o[db][qb], 0, 0, 0);
 #pragma unroll
                     for (int r = q * PER_M; r < (q + 1) * PER_M; r += 2) {
                         m0[qb] = fmaxf(m0[qb], nxt[qb][r]);
@@ -618,9 +631,12 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_gqa_bf16_kernel(AttnArgs 
                         else l0[qb] = __builtin_amdgcn_fdot2_f32_bf16((bf16x2){pp[e], pp[e + 1]}, ones, l0[qb], false);
                     }
                 }
-                if (q + A < NQ) vop[q + A] = v_read(vs_src, 2 * kbc + (q + A) / DB, (q + A) % DB);
-                if constexpr (Q8) {
-                    if (q + 1 < NQ) vf = v_value(vop[q + 1], es);
+                if (q + A < NQ) vop[q + A] = v_operand(vs_src, 2 * kbc + (q + A) / DB, (q + A) % DB);
+                more(q);
+                if constexpr (Q8) {   // here, not behind the last MFMA
+#pragma unroll
+                    for (int qb = 0; qb < QB; ++qb)
+                        if (q & 1) asm volatile("" : "+v"(m0[qb]), "+v"(m1[qb]), "+v"(l0[qb]), "+v"(l1[qb]));
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
@@ -653,28 +669,41 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_gqa_bf16_kernel(AttnArgs 
 
         // One step: scores of the next tile from ks_next, the current tile's
         // probabilities and PV from vs_cur.
-        auto half_step = [&](const Elem* ks_next, uint32_t es_next, int kbn, const Elem* vs_cur, uint32_t es_cur, int kbc,
-                             f32x16 (&cur)[QB], f32x16 (&nxt)[QB]) __attribute__((always_inline)) {
+        auto half_step = [&](const uint16_t* ks_next, int kbn, const uint16_t* vs_cur, int kbc, f32x16 (&cur)[QB],
+                             f32x16 (&nxt)[QB], auto more) __attribute__((always_inline)) {
             bf16x8 pb[QB][2];
             float mx[QB];
-            seg1(ks_next, es_next, kbn, cur, nxt, pb);
+            seg1(ks_next, kbn, cur, nxt, pb);
             __builtin_amdgcn_s_setprio(1);
-            seg2(vs_cur, es_cur, kbc, pb, nxt, mx);
+            seg2(vs_cur, kbc, pb, nxt, mx, more);
             __builtin_amdgcn_s_setprio(0);
             move_max(mx);
         };
 
-        uint32_t es_cur = 0;   // exponents of the tile whose scores are held
         auto iteration = [&](int i, auto u_tag, f32x16 (&cur)[QB], f32x16 (&nxt)[QB]) __attribute__((always_inline)) {
             constexpr int U = decltype(u_tag)::value;
-            wait_outstanding(min(i + NS - 2, n_tiles - 1) - (i + 1));   // tile i+1 has landed
+            if constexpr (!Q8) wait_outstanding(min(i + NS - 2, n_tiles - 1) - (i + 1));   // tile i+1 has landed
             lds_reads_done();
             bare_barrier();
-            if (i + NS - 1 < n_tiles)
-                issue(key_of(i + NS - 1), kst((U + NS - 1) % NS), vst((U + NS - 1) % NS));
-            const uint32_t es = es_cur;
-            es_cur = exponents(i + 1);
-            half_step(kst((U + 1) % NS), es_cur, 0, vst(U), es, 0, cur, nxt);
+            if constexpr (Q8) {
+                // As refill, with the conversions among the MFMAs of segment 2.
+                constexpr int S = (U + NS - 1) % NS, EVERY = 2 * DB / PER;
+                const int ahead = min(i + NS - 1, n_tiles - 1);
+                u32x2(&set)[PER] = codes[S & 1];
+                u32x2 later[PER];
+                leave_out_nan(ahead, set);
+                const float scale = win.scale(ahead);
+                char* const dst = (char*)kst(S);
+                load_codes(i + NS + 1, later);
+                half_step(kst((U + 1) % NS), 0, vst(U), 0, cur, nxt, [&](int q) __attribute__((always_inline)) {
+                    if (q % EVERY == 0) put_codes(set[q / EVERY], scale, dst + lds8[q / EVERY]);
+                });
+#pragma unroll
+                for (int n = 0; n < PER; ++n) set[n] = later[n];
+            } else {
+                refill(i, u_tag);
+                half_step(kst((U + 1) % NS), 0, vst(U), 0, cur, nxt, [](int) {});
+            }
         };
 
         // Last pipelined tile: probabilities and PV without overlap; issues
@@ -683,8 +712,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_gqa_bf16_kernel(AttnArgs 
             constexpr int U = decltype(u_tag)::value;
             lds_reads_done();
             bare_barrier();
-            if (i + NS - 1 < n_tiles)
-                issue(key_of(i + NS - 1), kst((U + NS - 1) % NS), vst((U + NS - 1) % NS));
+            refill(i, u_tag);
             bf16x8 pb[QB][2];
 #pragma unroll
             for (int qb = 0; qb < QB; ++qb) {
@@ -708,25 +736,25 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_gqa_bf16_kernel(AttnArgs 
             for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int db = 0; db < DB; ++db) {
-                    const bf16x8 vf = v_value(v_read(vst(U), h, db), es_cur);
+                    const bf16x8 vf = v_operand(vst(U), h, db);
 #pragma unroll
                     for (int qb = 0; qb < QB; ++qb)
                         o[db][qb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pb[qb][h], o[db][qb], 0, 0, 0);
                 }
         };
 
-        if (F >= 2) {
+        int done = 0;   // tiles behind the pipelined loop
+        if (F >= (Q8 ? NS + 1 : 2)) {
             f32x16 sA[QB], sB[QB];
-            wait_outstanding(min(NS - 2, n_tiles - 1));
+            if constexpr (!Q8) wait_outstanding(min(NS - 2, n_tiles - 1));
             lds_reads_done();
             bare_barrier();
-            es_cur = exponents(0);
             // scores of tile 0 and their maxima
 #pragma unroll
             for (int qb = 0; qb < QB; ++qb) sA[qb] = f32x16{};
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
-                const bf16x8 kf = k_value(k_read(kst(0), ks / KQ, 0), ks, es_cur);
+                const bf16x8 kf = k_operand(kst(0), ks, 0);
 #pragma unroll
                 for (int qb = 0; qb < QB; ++qb)
                     sA[qb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[qb][ks], sA[qb], 0, 0, 0);
@@ -744,27 +772,87 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_gqa_bf16_kernel(AttnArgs 
                 }
                 move_max(mx);
             }
-            for (int t = 0; t + 1 < F; t += NS) {
-                more_scales(t, t + NS);
+            if constexpr (Q8) {
+                int t = 0;
+                // Whole rounds of the stages, without a condition inside; up to NS - 1 tiles are left to plain
+                // order.
+                for (; t + NS < F; t += NS) {
+                    more_tiles(t);
+                    static_for<0, NS / 2>([&](auto h_tag) {
+                        constexpr int u = decltype(h_tag)::value * 2;
+                        iteration(t + u, std::integral_constant<int, u>{}, sA, sB);
+                        iteration(t + u + 1, std::integral_constant<int, u + 1>{}, sB, sA);
+                    });
+                }
+                drain(t, std::integral_constant<int, 0>{}, sA);
+                done = t + 1;
+            } else {
+                for (int t = 0; t + 1 < F; t += NS) {
+                    static_for<0, NS>([&](auto u_tag) {
+                        constexpr int u = decltype(u_tag)::value;
+                        const int i = t + u;
+                        if (i + 1 < F) {
+                            if constexpr (u % 2 == 0) iteration(i, u_tag, sA, sB);
+                            else iteration(i, u_tag, sB, sA);
+                        }
+                    });
+                }
+                const int last = F - 1;
                 static_for<0, NS>([&](auto u_tag) {
                     constexpr int u = decltype(u_tag)::value;
-                    const int i = t + u;
-                    if (i + 1 < F) {
-                        if constexpr (u % 2 == 0) iteration(i, u_tag, sA, sB);
-                        else iteration(i, u_tag, sB, sA);
+                    if (last % NS == u) {
+                        if constexpr (u % 2 == 0) drain(last, u_tag, sA);
+                        else drain(last, u_tag, sB);
                     }
                 });
+                done = F;
             }
-            const int last = F - 1;
-            static_for<0, NS>([&](auto u_tag) {
-                constexpr int u = decltype(u_tag)::value;
-                if (last % NS == u) {
-                    if constexpr (u % 2 == 0) drain(last, u_tag, sA);
-                    else drain(last, u_tag, sB);
-                }
-            });
         }
-        plain_from(F >= 2 ? F : 0);
+        plain_from(done);
+    }
+
+    if constexpr (Q8) {
+        // NaN values of tiles that not every row sees whole: a product of where they are with the keys'
+        // visibility, over those tiles once more.
+        asm volatile("" ::: "memory");
+        lds_reads_done();
+        bare_barrier();
+        if (nan_lds[0] != 0) {   // uniform
+            static_assert(QB == 1 && NKB == 1, "one row block and key block");
+#pragma unroll 1
+            for (int i = 0; i < n_tiles; ++i) {
+                const int t0 = key_of(i);
+                if (!hides(t0)) continue;
+                if (wave_v) {
+                    win.load(a, i, n_tiles, key_of);
+                    u32x2 set[PER];
+                    load_codes(i, set);
+#pragma unroll
+                    for (int n = 0; n < PER; ++n)
+                        put_codes(u32x2{(q8_nan_bytes(set[n][0]) >> 7) * 0x38u, (q8_nan_bytes(set[n][1]) >> 7) * 0x38u}, 1.0f,
+                                  (char*)kst(0) + lds8[n]);   // 1.0 where NaN is
+                }
+                __syncthreads();
+#pragma unroll 1
+                for (int st = 0; st < 2; ++st) {
+                    f32x8 seen;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const int key = t0 + st * 16 + (e >> 2) * 8 + hl * 4 + (e & 3);
+                        seen[e] = key < row_end[0] && key >= row_start[0] ? 1.0f : 0.0f;
+                    }
+                    const bf16x8 sees = __builtin_convertvector(seen, bf16x8);
+#pragma unroll
+                    for (int db = 0; db < DB; ++db) {
+                        const f32x16 n = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_operand(vst(0), st, db), sees, f32x16{}, 0, 0, 0);
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) o[db][0][r] = n[r] > 0.f ? __builtin_nanf("") : o[db][0][r];
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                }
+                __syncthreads();
+            }
+        }
     }
 
     // Finish each row: the two lanes of a column hold disjoint partial sums.

@@ -58,6 +58,9 @@ struct TileWindow {
     __device__ __forceinline__ int of(int reg, int i) const { return __builtin_amdgcn_readlane(reg, (i - first) & 63); }
 };
 
+__device__ __forceinline__ float q8_k_scale(uint32_t e) { return __uint_as_float((e & 0xffu) << 23); }
+__device__ __forceinline__ float q8_v_scale(uint32_t e) { return __uint_as_float((e >> 8) << 23); }
+
 template <int D>
 __global__ __launch_bounds__(row_waves<D>() * 64, D == 128 ? 1 : 2) void attn_gqa_rows_q8_kernel(AttnArgs a, ColPlan p, BlockScales sa) {
     constexpr int NW = row_waves<D>();

@@ -1,13 +1,13 @@
-// The GQA attention kernels over a cache held in 8 bits: the LDS layout of the
-// 32-key E4M3 tiles, the MFMA operand reads and the blocks' scales.
+// The GQA attention kernels over a cache held in 8 bits: conversion, the few-row
+// kernel's LDS layout of the 32-key E4M3 tiles and its MFMA operand reads, and the
+// scales of the many-row kernel's tiles.
 //
-// A tile stays in its codes from HBM to the operand registers and is turned into
-// bf16 there, two codes an instruction (v_cvt_scalef32_pk_bf16_fp8, at the rate
-// of an FMA), with the block's scale, a power of two, applied by the same
-// instruction: a code times its scale is exactly a bf16 number, so everything
-// behind the operands is the bf16 kernels' arithmetic over the dequantised cache.
-// Converting once a workgroup instead (bf16 tiles in LDS) would move 2.5 times the
-// LDS bytes, which the bf16 kernels are near the limit of.
+// Codes become bf16 two an instruction (v_cvt_scalef32_pk_bf16_fp8, at the rate of
+// an FMA), with the block's scale, a power of two, applied by the same instruction:
+// a code times its scale is exactly a bf16 number, so everything behind the
+// conversion is the bf16 kernels' arithmetic over the dequantised cache.  In the
+// few-row kernel one wave reads a tile and converts it at its operand reads; the
+// many-row kernel's four waves share a tile and convert it once, on its way to LDS.
 #pragma once
 
 #include "attn_common.h"
@@ -83,53 +83,60 @@ struct ScaleArg {};
 template <>
 struct ScaleArg<true> : BlockScales {};
 
-// The scales of up to 256 tiles in the order in which the loop visits them, K's
-// exponent in the low byte and V's in the next, in four registers of 64 lanes (as
-// PageWindow).  Loading it again stalls the loop for two dependent loads, once in
-// 256 tiles.
-struct ScaleWindow {
-    int first, last;        // tiles first .. last - 1
-    int e0, e1, e2, e3;
+// What a wave that stages one tensor's tiles needs of the tables for the next 128 of them,
+// in the order in which the loop visits them: pages (clamped into the pool) and scales, two
+// registers of 64 lanes each.  Loading it again stalls the loop for two dependent loads,
+// once in about 120 tiles.
+struct CodeWindow {
+    const int32_t* row;      // the sequence's row of the tensor's block table
+    const uint8_t* scales;   // of the layer and head
+    int64_t page_stride, block_stride;   // of the scales
+    int block_shift, top;
+    int first, last;         // tiles first .. last - 1
+    int p0, p1;
+    float s0, s1;
 
-    // key_of(i): first key of tile i < n_tiles.  Table entries are clamped into the pool.
+    __device__ __forceinline__ void init(const AttnArgs& a, const BlockScales& s, bool of_v, int seq, int layer, int kvh) {
+        row = (of_v && a.v_block_table ? a.v_block_table : a.block_table) + (int64_t)seq * a.max_pages;
+        const int64_t* const stride = of_v ? s.v_stride : s.k_stride;
+        scales = (of_v ? s.v : s.k) + layer * stride[0] + kvh * stride[1];
+        page_stride = stride[2];
+        block_stride = stride[3];
+        block_shift = s.block_shift;
+        top = (int)(a.n_pages - 1);
+    }
+    // key_of(i): first key of tile i < n_tiles.
     template <typename F>
-    __device__ __forceinline__ void load(const AttnArgs& a, const BlockScales& s, int seq, int layer, int kvh, int from,
-                                         int n_tiles, F key_of) {
-        const int32_t* const k_row = a.block_table + (int64_t)seq * a.max_pages;
-        const int32_t* const v_row = a.v_block_table ? a.v_block_table + (int64_t)seq * a.max_pages : k_row;
-        const uint8_t* const k = s.k + layer * s.k_stride[0] + kvh * s.k_stride[1];
-        const uint8_t* const v = s.v + layer * s.v_stride[0] + kvh * s.v_stride[1];
-        auto lookup = [&](int i) __attribute__((always_inline)) {
-            const int key = key_of(min(i, n_tiles - 1));   // (below the slots that the table covers)
-            const int entry = key >> a.page_shift;
-            const int block = (key & ((1 << a.page_shift) - 1)) >> s.block_shift;
-            const int top = (int)(a.n_pages - 1);
-            const int kp = min(max(k_row[entry], 0), top), vp = min(max(v_row[entry], 0), top);
-            return k[kp * s.k_stride[2] + block * s.k_stride[3]] | (v[vp * s.v_stride[2] + block * s.v_stride[3]] << 8);
-        };
+    __device__ __forceinline__ void load(const AttnArgs& a, int from, int n_tiles, F key_of) {
         first = from;
         last = from + 64;
-        e0 = e1 = e2 = e3 = 0;
+        p0 = p1 = 0;
+        s0 = s1 = 0.f;
         if (n_tiles <= 0) return;
+        auto lookup = [&](int i, int& page, float& scale) __attribute__((always_inline)) {
+            const int key = key_of(min(i, n_tiles - 1));   // (below the slots that the table covers)
+            page = min(max(row[key >> a.page_shift], 0), top);
+            const int block = (key & ((1 << a.page_shift) - 1)) >> block_shift;
+            scale = __uint_as_float((uint32_t)scales[page * page_stride + block * block_stride] << 23);
+        };
         const int i = from + (int)__lane_id();
-        e0 = lookup(i);
+        lookup(i, p0, s0);
         if (n_tiles > last) {
-            last = from + 256;
-            e1 = lookup(i + 64);
-            e2 = lookup(i + 128);
-            e3 = lookup(i + 192);
+            last = from + 128;
+            lookup(i + 64, p1, s1);
         }
     }
-    __device__ __forceinline__ bool holds(int lo, int hi) const { return lo >= first && hi < last; }
-    // Both exponents of tile i (one that the window holds), in a scalar register.
-    __device__ __forceinline__ uint32_t at(int i) const {
-        const int r = (i - first) >> 6, l = (i - first) & 63;
-        const int x0 = __builtin_amdgcn_readlane(e0, l), x1 = __builtin_amdgcn_readlane(e1, l);
-        const int x2 = __builtin_amdgcn_readlane(e2, l), x3 = __builtin_amdgcn_readlane(e3, l);
-        return (uint32_t)(r == 0 ? x0 : r == 1 ? x1 : r == 2 ? x2 : x3);
+    // Of tile i, which the window holds.
+    __device__ __forceinline__ int64_t page(int i) const {
+        const int l = (i - first) & 63;
+        const int x0 = __builtin_amdgcn_readlane(p0, l), x1 = __builtin_amdgcn_readlane(p1, l);
+        return i - first < 64 ? x0 : x1;
+    }
+    __device__ __forceinline__ float scale(int i) const {
+        const int l = (i - first) & 63;
+        const int x0 = __builtin_amdgcn_readlane(__float_as_int(s0), l), x1 = __builtin_amdgcn_readlane(__float_as_int(s1), l);
+        return __int_as_float(i - first < 64 ? x0 : x1);
     }
 };
-__device__ __forceinline__ float q8_k_scale(uint32_t e) { return __uint_as_float((e & 0xffu) << 23); }
-__device__ __forceinline__ float q8_v_scale(uint32_t e) { return __uint_as_float((e >> 8) << 23); }
 
 }  // namespace pkv
