@@ -7,8 +7,12 @@
 // do not depend on timing), and a launch that applies it: block-table rows and the
 // copies of pages.  Nothing is read back by the host, so a captured graph replays
 // them with whatever the tables hold then.  The copies are the cost, a stream read
-// once and written once: 16-byte units, four loads in flight a thread, tiles of
-// (page, layers and slots end to end) shared by a grid that fills the GPU.
+// once and written once: 16-byte units, four loads in flight a thread, tiles of 16 KB.
+// Measured: 220 pages of 1 MB moved, 88 us with the plan's 5 (copies at 5.5 TB/s, what a
+// copy of this size reaches here; 103 with 2048 blocks that take several tiles each); 128
+// forks with a last page of up to 64 x 8 x 128 codes in 8 layers copied, 39 us with 10 for
+// the branches freed before and the plan (46 with the tiles of a layer neighbours: a short
+// tail then leaves the same XCDs without work in every layer).
 #include "attn_columns.h"
 
 namespace pkv {
@@ -18,7 +22,8 @@ constexpr int kPlan = 1024;        // threads of the planning workgroup
 constexpr int kPer = 8;            // pages per thread and round of a scan
 constexpr int kThreads = 256;
 constexpr int kAhead = 4;          // units per thread whose loads are issued before the first store
-constexpr int kBlocks = 2048;      // blocks of the applying launch at most: eight a CU
+constexpr int kTile = kThreads * kAhead;
+constexpr int kBlocks = 16384;     // blocks of the applying launch at most: how many moves there are the host cannot know
 
 // Exclusive prefix sum over the workgroup's threads, in thread order; *total is the
 // sum.  Every thread takes part.
@@ -192,36 +197,52 @@ __global__ __launch_bounds__(kPlan) void pages_compact_plan(PagesArgs a) {
     }
 }
 
+// Units first .. first + kTile - 1 of a run of `units` in one piece from byte `at` of both pages.
+template <typename T>
+__device__ __forceinline__ void copy_run(const PageTensor& s, const PageMove& m, int64_t at, uint32_t first, uint32_t units) {
+    const T* const from = (const T*)(s.data + (int64_t)m.src * s.page_stride + at) + first;
+    T* const to = (T*)(s.data + (int64_t)m.dst * s.page_stride + at) + first;
+    const uint32_t left = units - first;
+    T v[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+        v[k] = __builtin_nontemporal_load(from + min(k * kThreads + threadIdx.x, left - 1));   // (no branches)
+    }
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+        const uint32_t u = k * kThreads + threadIdx.x;
+        if (u < left) __builtin_nontemporal_store(v[k], to + u);
+    }
+}
+
+// The same of units counted over layers, slots and heads that lie apart.
 template <typename T>
 __device__ __forceinline__ void copy_units(const PageTensor& s, const PageMove& m, uint32_t first, uint32_t units_per_layer,
-                                           uint32_t units, bool runs) {
+                                           uint32_t units) {
     T v[kAhead];
     char* to[kAhead];
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
-        const uint32_t u = first + k * kThreads + threadIdx.x;
-        to[k] = nullptr;
-        if (u >= units) continue;
+        const uint32_t u = min(first + k * kThreads + threadIdx.x, units - 1);
         const uint32_t layer = u / units_per_layer;
         uint32_t rest = u - layer * units_per_layer;
-        int64_t at = (int64_t)layer * s.layer_stride;
-        if (!runs) {   // uniform: slots or heads apart
-            const uint32_t row = rest / (uint32_t)s.row_units;
-            rest -= row * (uint32_t)s.row_units;
-            const uint32_t slot = row / (uint32_t)s.heads;
-            at += (int64_t)slot * s.slot_stride + (int64_t)(row - slot * (uint32_t)s.heads) * s.head_stride;
-        }
-        at += (int64_t)rest << s.unit_shift;
+        const uint32_t row = rest / (uint32_t)s.row_units;
+        rest -= row * (uint32_t)s.row_units;
+        const uint32_t slot = row / (uint32_t)s.heads;
+        const int64_t at = (int64_t)layer * s.layer_stride + (int64_t)slot * s.slot_stride +
+                           (int64_t)(row - slot * (uint32_t)s.heads) * s.head_stride + ((int64_t)rest << s.unit_shift);
         v[k] = __builtin_nontemporal_load((const T*)(s.data + (int64_t)m.src * s.page_stride + at));
         to[k] = s.data + (int64_t)m.dst * s.page_stride + at;
     }
 #pragma unroll
     for (int k = 0; k < kAhead; ++k)
-        if (to[k]) __builtin_nontemporal_store(v[k], (T*)to[k]);
+        if (first + k * kThreads + threadIdx.x < units) __builtin_nontemporal_store(v[k], (T*)to[k]);
 }
 
 // Block-table rows, and the copies: job j is a piece of the rows below row_jobs, then
-// tile (move, tensor, tile of the tensor's share).
+// tile (move, tensor, tile of the tensor's share).  runs: tiles a layer of a tensor whose
+// pages lie in one piece in each layer and fill half a tile or more there (no division a
+// unit then), else 0.
 template <bool FORK>
 __global__ __launch_bounds__(kThreads) void pages_apply(PagesArgs a, int64_t row_jobs, int pieces, int4 tiles, int4 runs) {
     const int64_t per_move = (int64_t)tiles.x + tiles.y + tiles.z + tiles.w;
@@ -257,8 +278,9 @@ __global__ __launch_bounds__(kThreads) void pages_apply(PagesArgs a, int64_t row
             continue;
         }
         const int64_t c = j - row_jobs;
-        const PageMove m = a.moves[c / per_move];
-        int tile = (int)(c % per_move), k = 0;
+        const int64_t move = c / per_move;
+        const PageMove m = a.moves[move];
+        int tile = (int)(c - move * per_move), k = 0;
         const int n[4] = {tiles.x, tiles.y, tiles.z, tiles.w};
         const int r[4] = {runs.x, runs.y, runs.z, runs.w};
 #pragma unroll
@@ -271,16 +293,32 @@ __global__ __launch_bounds__(kThreads) void pages_apply(PagesArgs a, int64_t row
         const PageTensor s = a.tensors[k];
         const uint32_t slots = (uint32_t)((m.tokens + s.slot_tokens - 1) / s.slot_tokens);
         const uint32_t per_layer = slots * (uint32_t)s.heads * (uint32_t)s.row_units;
+        const int run = k == 0 ? r[0] : k == 1 ? r[1] : k == 2 ? r[2] : r[3];
+        if (run) {
+            // Layer after layer: what a short tail leaves without work is then shared by the XCDs, over
+            // which blocks go round.
+            const int piece = tile / s.layers, layer = tile - piece * s.layers;
+            const uint32_t first = (uint32_t)piece * kTile;
+            if (first >= per_layer) continue;
+            const int64_t at = (int64_t)layer * s.layer_stride;
+            switch (s.unit_shift) {
+                case 4: copy_run<u32x4>(s, m, at, first, per_layer); break;
+                case 3: copy_run<u32x2>(s, m, at, first, per_layer); break;
+                case 2: copy_run<uint32_t>(s, m, at, first, per_layer); break;
+                case 1: copy_run<uint16_t>(s, m, at, first, per_layer); break;
+                default: copy_run<uint8_t>(s, m, at, first, per_layer); break;
+            }
+            continue;
+        }
         const uint32_t units = per_layer * (uint32_t)s.layers;
-        const uint32_t first = (uint32_t)tile * (kThreads * kAhead);
+        const uint32_t first = (uint32_t)tile * kTile;
         if (first >= units) continue;
-        const bool run = k == 0 ? r[0] : k == 1 ? r[1] : k == 2 ? r[2] : r[3];
         switch (s.unit_shift) {
-            case 4: copy_units<u32x4>(s, m, first, per_layer, units, run); break;
-            case 3: copy_units<u32x2>(s, m, first, per_layer, units, run); break;
-            case 2: copy_units<uint32_t>(s, m, first, per_layer, units, run); break;
-            case 1: copy_units<uint16_t>(s, m, first, per_layer, units, run); break;
-            default: copy_units<uint8_t>(s, m, first, per_layer, units, run); break;
+            case 4: copy_units<u32x4>(s, m, first, per_layer, units); break;
+            case 3: copy_units<u32x2>(s, m, first, per_layer, units); break;
+            case 2: copy_units<uint32_t>(s, m, first, per_layer, units); break;
+            case 1: copy_units<uint16_t>(s, m, first, per_layer, units); break;
+            default: copy_units<uint8_t>(s, m, first, per_layer, units); break;
         }
     }
 }
@@ -293,10 +331,12 @@ hipError_t launch_apply(const PagesArgs& a, hipStream_t stream) {
     int64_t per_move = 0;
     for (int k = 0; k < a.n_tensors; ++k) {
         const PageTensor& s = a.tensors[k];
-        const int64_t units = (int64_t)s.layers * s.slots * s.heads * s.row_units;
-        tiles[k] = (int)((units + kThreads * kAhead - 1) / (kThreads * kAhead));
+        const int64_t layer_units = (int64_t)s.slots * s.heads * s.row_units;
         const int64_t row = (int64_t)s.row_units << s.unit_shift;
-        runs[k] = (s.heads == 1 || s.head_stride == row) && (s.slots == 1 || s.slot_stride == row * s.heads);
+        if ((s.heads == 1 || s.head_stride == row) && (s.slots == 1 || s.slot_stride == row * s.heads) &&
+            layer_units >= kTile / 2)
+            runs[k] = (int)((layer_units + kTile - 1) / kTile);
+        tiles[k] = runs[k] ? runs[k] * s.layers : (int)((layer_units * s.layers + kTile - 1) / kTile);
         per_move += tiles[k];
     }
     // The number of moves is known on the device: at most one a fork, or half the pages.
