@@ -351,38 +351,27 @@ __global__ __launch_bounds__(row_waves<D>() * 64, D == 128 ? 1 : 2) void attn_gq
             l_run += l0 + l1;
             return fmaxf(m0, m1);
         };
-        // Whether V stage vs_src holds NaN codes; the values of a masked tile that does: a NaN reaches only the
-        // rows that see its key.
-        auto nan_codes = [&](const uint8_t* vs_src) __attribute__((always_inline)) {
+        // A masked tile must not bring NaN values (0 * NaN): its NaN codes are cleared in V stage vs_src, and
+        // come back, to the rows that see them, at the end of the item.
+        bool left_out = false;
+        auto leave_out_nan = [&](uint8_t* vs_src) __attribute__((always_inline)) {
+            u32x4 w[TE / 1024];
             uint32_t nans = 0;
 #pragma unroll
-            for (int q = 0; q < 2 * DB; ++q) {
-                const u32x2 w = q8_v_read(vs_src + vofs[q % DB] + (q / DB) * 16 * D);
-                nans |= q8_nan_bytes(w[0]) | q8_nan_bytes(w[1]);
+            for (int n = 0; n < TE / 1024; ++n) {
+                w[n] = *(const u32x4*)(vs_src + (n * 64 + lane) * 16);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) nans |= q8_nan_bytes(w[n][e]);
             }
-            return __builtin_amdgcn_ballot_w64(nans != 0) != 0;
-        };
-        auto add_nan_values = [&](const uint8_t* vs_src, uint32_t es, int t0, const bf16x8 (&pb)[2]) __attribute__((always_inline)) {
+            if (__builtin_amdgcn_ballot_w64(nans != 0) == 0) return;
+            left_out = true;
 #pragma unroll
-            for (int st = 0; st < 2; ++st) {
-                f32x8 seen;
+            for (int n = 0; n < TE / 1024; ++n) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int key = t0 + st * 16 + (e >> 2) * 8 + hl * 4 + (e & 3);
-                    seen[e] = key < row_end && key >= row_start ? 1.0f : 0.0f;
-                    l_run += (float)pb[st][e];
-                }
-                const bf16x8 sees = __builtin_convertvector(seen, bf16x8);
-#pragma unroll
-                for (int db = 0; db < DB; ++db) {
-                    bf16x8 vf, nf;
-                    q8_split_nan(q8_v_read(vs_src + vofs[db] + st * 16 * D), q8_v_scale(es), vf, nf);
-                    o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pb[st], o[db], 0, 0, 0);
-                    const f32x16 n = __builtin_amdgcn_mfma_f32_32x32x16_bf16(nf, sees, f32x16{}, 0, 0, 0);
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) o[db][r] = n[r] > 0.f ? __builtin_nanf("") : o[db][r];
-                }
+                for (int e = 0; e < 4; ++e) w[n][e] &= ~((q8_nan_bytes(w[n][e]) >> 7) * 0xffu);
+                *(u32x4*)(vs_src + (n * 64 + lane) * 16) = w[n];
             }
+            asm volatile("" ::: "memory");
         };
 
         // Loads retire in order: K(0), V(0), .., K(NS-1), V(NS-1), K(NS) once tile 0's scores are read, then
@@ -435,8 +424,8 @@ __global__ __launch_bounds__(row_waves<D>() * 64, D == 128 ? 1 : 2) void attn_gq
             wait_step(n_tiles - 1 - i);
             bf16x8 pb[2];
             all_probabilities(cur, pb);
-            if (masked(key_of(i)) && nan_codes(vst(i))) add_nan_values(vst(i), es_cur, key_of(i), pb);
-            else seg2(vst(i), es_cur, pb, cur, std::false_type{});
+            if (masked(key_of(i))) leave_out_nan(vst(i));
+            seg2(vst(i), es_cur, pb, cur, std::false_type{});
             lds_reads_done();
             if (i + 1 >= n_tiles) return;
             es_cur = win.of(win.exps, i + 1);
@@ -472,6 +461,37 @@ __global__ __launch_bounds__(row_waves<D>() * 64, D == 128 ? 1 : 2) void attn_gq
                     s_a = s_b;
                 } else {
                     plain(i, s_a);
+                }
+            }
+            if (left_out) {   // where the NaN values are times the keys' visibility, over the masked tiles once more
+#pragma unroll 1
+                for (int i = 0; i < n_tiles; ++i) {
+                    const int t0 = key_of(i);
+                    if (!masked(t0)) continue;
+                    win.load(a, sa, sg.seq, layer, kvh, i, n_tiles, key_of);
+                    issue_v(i);
+                    wait_vmcnt<0>();
+                    asm volatile("" ::: "memory");
+#pragma unroll 1
+                    for (int st = 0; st < 2; ++st) {
+                        f32x8 seen;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            const int key = t0 + st * 16 + (e >> 2) * 8 + hl * 4 + (e & 3);
+                            seen[e] = key < row_end && key >= row_start ? 1.0f : 0.0f;
+                        }
+                        const bf16x8 sees = __builtin_convertvector(seen, bf16x8);
+#pragma unroll
+                        for (int db = 0; db < DB; ++db) {
+                            const u32x2 w = q8_v_read(vst(i) + vofs[db] + st * 16 * D);
+                            const bf16x8 nan = q8_to_bf16((q8_nan_bytes(w[0]) >> 7) * 0x38u, (q8_nan_bytes(w[1]) >> 7) * 0x38u, 1.0f);
+                            const f32x16 n = __builtin_amdgcn_mfma_f32_32x32x16_bf16(nan, sees, f32x16{}, 0, 0, 0);
+#pragma unroll
+                            for (int r = 0; r < 16; ++r) o[db][r] = n[r] > 0.f ? __builtin_nanf("") : o[db][r];
+                            __builtin_amdgcn_sched_barrier(0);
+                        }
+                    }
+                    lds_reads_done();
                 }
             }
         }

@@ -68,14 +68,6 @@ __device__ __forceinline__ u32x2 q8_v_read(const uint8_t* base) {
 __device__ __forceinline__ uint32_t q8_nan_bytes(uint32_t w) {
     return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
 }
-// Values of 8 keys of one channel in a tile with masked keys: a NaN code weighs
-// nothing in `value` and 1 in `nan`, for a product with the keys' visibility that
-// tells which rows see it (0 * NaN would reach the rows that do not).
-__device__ __forceinline__ void q8_split_nan(u32x2 w, float scale, bf16x8& value, bf16x8& nan) {
-    const uint32_t m0 = (q8_nan_bytes(w[0]) >> 7) * 0xffu, m1 = (q8_nan_bytes(w[1]) >> 7) * 0xffu;
-    value = q8_to_bf16(w[0] & ~m0, w[1] & ~m1, scale);
-    nan = q8_to_bf16(m0 & 0x38383838u, m1 & 0x38383838u, 1.0f);   // 0x38: 1.0
-}
 
 // Kernel argument: empty where the cache is not in 8 bits.
 template <bool Q8>
