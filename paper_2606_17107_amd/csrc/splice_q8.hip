@@ -75,8 +75,9 @@ __device__ inline float exp2_int(int e) { return __uint_as_float((uint32_t)(e + 
 // cos and sin of delta * omega to fp32's last bit or nearly: the angle is formed and
 // reduced by pi/2 in fp64, r = rh + rl in two fp32 parts, and the Taylor series are
 // summed in fp32 with their leading terms kept apart from the corrections (errors below
-// 0.8 of half a unit in the last place beside the rounding of the result; terms below
-// 2^-29 left out).  fp64 series would hold 24 more registers in constants.
+// 0.09 of a unit in the last place beside the rounding of the result, which is the nearest
+// number for all but 0.3% of the sines and 0.6% of the cosines; terms below 2^-29 left out).
+// fp64 series would hold 24 more registers in constants.
 __device__ inline void turn(double delta, double omega, float& c, float& s) {
     const double x = delta * omega;
     const double k = rint(x * 0.63661977236758134308);            // 2/pi
@@ -84,18 +85,22 @@ __device__ inline void turn(double delta, double omega, float& c, float& s) {
     r = fma(-k, 6.123233995736766036e-17, r);                    // pi/2, trailing part
     const int q = (int)fma(-4.0, floor(k * 0.25), k);            // k mod 4
     const float rh = (float)r, rl = (float)(r - (double)rh);
-    const float z = rh * rh, zl = fmaf(rh, rh, -z) + 2.f * rh * rl, hz = 0.5f * z;
-    // sin r = rh + (rl (1 - z/2) + rh z (-1/3! + z/5! - z^2/7! + z^3/9!))
+    const float z = rh * rh, ze = fmaf(rh, rh, -z), hz = 0.5f * z;   // rh^2 = z + ze
+    // sin r = rh - rh^3/3! + (rh^3 (z/5! - z^2/7! + z^3/9!) + rl (1 - z/2))
+    const float cube = rh * z, cube_e = fmaf(rh, ze, fmaf(rh, z, -cube));
+    constexpr float k3 = -0.166666671633720398f, k3_e = 4.96705373e-9f;   // -1/3! = k3 + k3_e
+    const float third = cube * k3, third_e = fmaf(cube_e, k3, fmaf(cube, k3, -third));
     float ps = fmaf(z, 2.75573192e-6f, -1.98412698e-4f);
     ps = fmaf(z, ps, 8.33333333e-3f);
-    ps = fmaf(z, ps, -0.166666667f);
-    const float sr = rh + fmaf(rh * z, ps, fmaf(-hz, rl, rl));
-    // cos r = (1 - z/2) + (what that rounding lost - zl/2 + z^2 (1/4! - z/6! + z^2/8! - z^3/10!))
+    ps = fmaf(z, ps, k3_e);
+    const float lead = rh + third, lead_e = (rh - lead) + third;
+    const float sr = lead + (lead_e + fmaf(cube, ps, third_e + fmaf(-hz, rl, rl)));
+    // cos r = (1 - z/2) + (what that rounding lost - (ze + 2 rh rl)/2 + z^2 (1/4! - z/6! + z^2/8! - z^3/10!))
     float pc = fmaf(z, -2.75573192e-7f, 2.48015873e-5f);
     pc = fmaf(z, pc, -1.38888889e-3f);
     pc = fmaf(z, pc, 4.16666667e-2f);
     const float w = 1.f - hz, lost = (1.f - w) - hz;
-    const float cr = w + fmaf(z * z, pc, fmaf(-0.5f, zl, lost));
+    const float cr = w + fmaf(z * z, pc, fmaf(-0.5f, ze + 2.f * rh * rl, lost));
     const float sa = (q & 1) ? cr : sr;
     const float ca = (q & 1) ? sr : cr;
     s = (q & 2) ? -sa : sa;
@@ -350,10 +355,15 @@ __global__ __launch_bounds__(kWaves * 64, D == 64 ? 5 : F32 ? 3 : 4) void store_
                         if (!rope || rec[t] != r) continue;
 #pragma unroll
                         for (int i = 0; i < 8; ++i) {
+                            // Rounded as the formula stands, products and sum: which of two codes a value
+                            // beside a rounding boundary gets is then the same as in a plain fp32 program.
+                            // (An FMA for one product errs as often, on other values; 16 contexts of 4052
+                            // tokens in 4 layers: 180 us, 198 as it is.)
+#pragma clang fp contract(off)
                             const int ia = INTER ? 2 * i : i, ib = INTER ? 2 * i + 1 : i + 8;
                             const float u = x[t][ia], v = x[t][ib];
-                            x[t][ia] = fmaf(u, c[i], -(v * sn[i]));
-                            x[t][ib] = fmaf(u, sn[i], v * c[i]);
+                            x[t][ia] = u * c[i] - v * sn[i];
+                            x[t][ib] = u * sn[i] + v * c[i];
                         }
                     }
                 };
