@@ -204,7 +204,7 @@ __global__ __launch_bounds__(kWaves * 64, D == 64 ? 5 : F32 ? 3 : 4) void store_
     const int b0 = max(mine.dst_pos0, 0) / BT + spot * g.blocks + in_group, b_end = (end + BT - 1) / BT;
     int turn_no = 0;
 #pragma unroll 1
-    for (int b = b0; b < b_end; b += g.spots * g.blocks, turn_no ^= 1) {
+    for (int b = b0; b < b_end; b += g.spots * g.blocks) {
         const int slot0 = b * BT;                     // the block's first slot
         const int first = slot0 + sub * kSub + row0;  // this lane's slots: first, + TPS, ..
         const int block_end = min(slot0 + BT, cap);
@@ -446,6 +446,7 @@ __global__ __launch_bounds__(kWaves * 64, D == 64 ? 5 : F32 ? 3 : 4) void store_
             if (moved && is_k) quantise(std::false_type{});   // uniform over the workgroup
             else quantise(std::true_type{});
         }
+        turn_no ^= 1;   // (a skipped block has no barrier)
         if (working && !in_pool && sub == 0 && lane == 0) flag();
         if (!working || !in_pool || !(any & 1)) continue;
         if ((any & 2) && e > old) {

@@ -96,6 +96,26 @@ def test_fork(kind, page, out_of_place):
     assert int(flag.item()) == 0
 
 
+@pytest.mark.parametrize("row,dtype", [(67, torch.uint8), (5, torch.int16), (64, torch.int32)])
+def test_fork_tails_of_many_tiles(row, dtype):
+    """Pages that lie in one piece in each layer and take many tiles there, in units of 1, 2 and 16 bytes; last pages of
+    one slot, of one short of a page, and between."""
+    rng = np.random.default_rng(row)
+    page, L, H = 1024, 3, 3
+    table, ref, lens = random_pool(rng, 8, 2, page, 12, [page + 1, page + 511, 2 * page - 1, page, 0, 0, 0, 0])
+    forks = [(0, 4, page + 1), (1, 5, page + 511), (2, 6, 2 * page - 1), (3, 7, 300)]
+    size = torch.empty(0, dtype=dtype).element_size()
+    ts = [torch.from_numpy(rng.integers(0, 256, (L, len(ref), page, H, row, size)).astype(np.uint8)).cuda().view(dtype)[..., 0]]
+    before = [as_bytes(t) for t in ts]
+    want_ref, want, copies, bad = R.fork(ref, table, table, forks, page, True)
+    assert not bad and len(copies) == 4
+    g_ref, g = cuda(ref), cuda(table)
+    pkv.pages_fork(ts, g_ref, g, page, pkv.make_forks([dict(parent=a, child=b, n_tokens=n) for a, b, n in forks], "cuda"), 4)
+    torch.cuda.synchronize()
+    np.testing.assert_array_equal(g.cpu().numpy(), want)
+    check_tensors(ts, before, copies, page)
+
+
 def test_fork_many():
     """More records than one round of the plan, over more pages than one round of its scan."""
     rng = np.random.default_rng(1)

@@ -85,6 +85,16 @@ def test_splice_nothing_to_do():
     assert pkv.pkv_reposition_splice_quant(**keys) == 0
 
 
+@needs_no_gpu
+def test_splice_slots_too_far_apart():
+    """The rows of a block are addressed by 32-bit offsets: slots lie at most 16 MiB apart."""
+    far, eb = 1 << 24, 2
+    for name, most in (("src_k", far // eb), ("src_v", far // eb), ("dst_k", far), ("dst_v", far)):
+        args = lambda step: splice_args(n_segs=0, **{"L__%s_stride" % name: pkv._i64x3(0, 0, step)})   # noqa: E731
+        assert pkv.pkv_reposition_splice_quant(**args(most + 16)) == 2 and b"16 MiB" in pkv.pkv_last_error().encode()
+        assert b"16 MiB" not in (pkv.pkv_reposition_splice_quant(**args(most)), pkv.pkv_last_error().encode())[1]
+
+
 # ---- attention ------------------------------------------------------------------
 
 def attention_args(**kw):
