@@ -647,7 +647,7 @@ bool col_route(const AttnArgs& a) {
     if (rows < 1 || rows > (a.variant == 1 ? kRowsMla : kRowsGqa) || !col_long_enough(a, rows))
         return false;
     // axis positions and workgroup ids are 32-bit
-    return col_items(a) * ((int64_t)a.max_kv_len / kColTile + 16) < 0x7fffffff;
+    return col_items(a) * ((int64_t)a.max_kv_len / kColTile + (a.dtype == 2 ? 32 : 16)) < 0x7fffffff;
 }
 
 }  // namespace
@@ -674,6 +674,10 @@ int attention_splits(const AttnArgs& a) {
     // sustain about 1.0 PFLOP/s (GQA) and 1.1 PFLOP/s (MLA), a workgroup's
     // fixed cost is about 20 us, the combine streams at about 5 TB/s.  At
     // least 512 keys per split, at most 32 splits.
+    // Over a cache held in 8 bits up to 8 splits may be as short as 128 keys while each
+    // workgroup has a CU of its own (8 KV heads of 4: 40 queries over 1000 keys 31.5 us a
+    // call in 1 split, 17.8 in 7; 64 over 2048 25.8 in 4, 22.6 in 8; beyond, 16 sequences
+    // of 40 over 1000 33.0 in 1, 38.3 in 2).
     const Plan p = make_plan(a, 1);
     const int64_t wgs = (int64_t)p.n_groups * p.rbs;   // workgroups per split
     const int64_t kv = seen_keys(a);
@@ -694,7 +698,7 @@ int attention_splits(const AttnArgs& a) {
     int best = 1;
     double best_t = 1e30;
     for (int s = 1; s <= 32; ++s) {
-        if (s > 1 && kv / s < 512) break;
+        if (s > 1 && kv / s < (a.dtype == 2 && s <= 8 && wgs * s <= kCUs ? 128 : 512)) break;
         const double rounds = (double)((wgs * s + slots - 1) / slots);
         const double t = rounds * (20e-6 + (wg_flops / s) / slot_rate) + (s > 1 ? s * comb_bytes / 5e12 + 5e-6 : 0.0);
         if (t < best_t * (1.0 - 1e-9)) {
@@ -760,6 +764,9 @@ hipError_t launch_columns(const AttnArgs& a, const BlockScales* scales, hipStrea
     // Measured costs of a column's shortest useful run and of starting an item
     // (set-up, first loads and merge: about 7 us), in tiles of one workgroup at head
     // size 128; the tiles of head size 64 take half as long, with the same counts.
+    // (A tile of codes takes half as long and starting an item does not: 16 caches of
+    // 8448..12544 slots, 4 KV heads of 128, 49 us a call with 12 tiles, 46.5 with 24; 64
+    // of 1000..5000, 8 KV heads, 94 and 92; 5 of 300..20000, 29.9 and 28.3.)
     p.min_tiles = a.variant == 1 ? 4 : 8;
     p.item_cost = a.variant == 1 ? 4 : a.dtype == 2 ? 24 : 12;
     const int64_t cols = p.columns ? p.columns : (col_items(a) + kXcds - 1) / kXcds * kXcds;
