@@ -18,14 +18,14 @@
 namespace pkv {
 namespace {
 
-// Waves of a workgroup (one a CU) and LDS stages of a wave.  Head size 128: one wave a
-// SIMD, which needs 290 registers, and deep staging.  Head size 64: two waves a SIMD hide
-// each other's latencies (16 caches of 8448..12544 slots, 2 KV heads: 29.7 us a call with
-// four waves of 8 stages, 27.6 with eight of 4, 25.5 with eight of 2).
-template <int D>
-constexpr int row_waves() { return D == 128 ? 4 : 8; }
-template <int D>
-constexpr int row_stages() { return D == 128 ? 4 : 2; }
+// Waves of a workgroup (one a CU) and LDS stages of a wave: two waves a SIMD hide each
+// other's latencies, and the loads in flight are the same as with half the waves and twice
+// the stages (32 heads over 4 KV heads of 128, 16 caches of 8448..12544 slots: 45.2 us a
+// call with four waves of 4 stages, 43.6 with these; 8 KV heads, one cache of 32768: 25.6
+// and 25.0; 2 KV heads of 64: 29.7 with four waves of 8, 27.6 with eight of 4, 25.2 with
+// these).
+constexpr int kRowWaves = 8;
+constexpr int kRowStages = 2;
 constexpr int kAhead = 3;   // LDS operand reads issued this many operands ahead of their MFMA
 
 __device__ inline int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
@@ -62,9 +62,9 @@ __device__ __forceinline__ float q8_k_scale(uint32_t e) { return __uint_as_float
 __device__ __forceinline__ float q8_v_scale(uint32_t e) { return __uint_as_float((e >> 8) << 23); }
 
 template <int D>
-__global__ __launch_bounds__(row_waves<D>() * 64, D == 128 ? 1 : 2) void attn_gqa_rows_q8_kernel(AttnArgs a, ColPlan p, BlockScales sa) {
-    constexpr int NW = row_waves<D>();
-    constexpr int NS = row_stages<D>();
+__global__ __launch_bounds__(kRowWaves * 64, 2) void attn_gqa_rows_q8_kernel(AttnArgs a, ColPlan p, BlockScales sa) {
+    constexpr int NW = kRowWaves;
+    constexpr int NS = kRowStages;
     constexpr int BN = kColTile;           // keys per tile
     constexpr int CH = D / 16;             // 16-byte chunks per row
     constexpr int KBLK = BN * CH / 64;     // LDS-DMA loads per K (or V) tile
@@ -455,13 +455,24 @@ __global__ __launch_bounds__(row_waves<D>() * 64, D == 128 ? 1 : 2) void attn_gq
             // Tiles with hidden keys come first (a window's start) and last.
 #pragma unroll 1
             for (int i = 0; i < n_tiles; ++i) {
-                if (!win.holds(i + 1 + NS)) win.load(a, sa, sg.seq, layer, kvh, i, n_tiles, key_of);
-                if (i + 1 < n_tiles && !masked(key_of(i))) {
+                auto more_tiles = [&]() __attribute__((always_inline)) {
+                    if (!win.holds(i + 1 + NS)) win.load(a, sa, sg.seq, layer, kvh, i, n_tiles, key_of);
+                };
+                // A loop of their own, two steps a round: where the two kinds of step meet, and where the
+                // scores change places, whole tiles of registers would be moved.
+#pragma unroll 1
+                for (; i + 1 < n_tiles && !masked(key_of(i)); ++i) {
+                    more_tiles();
                     step(i, s_a, s_b);
-                    s_a = s_b;
-                } else {
-                    plain(i, s_a);
+                    if (!(++i + 1 < n_tiles && !masked(key_of(i)))) {
+                        s_a = s_b;
+                        break;
+                    }
+                    more_tiles();
+                    step(i, s_b, s_a);
                 }
+                more_tiles();
+                plain(i, s_a);
             }
             if (left_out) {   // where the NaN values are times the keys' visibility, over the masked tiles once more
 #pragma unroll 1
@@ -523,9 +534,9 @@ __global__ __launch_bounds__(row_waves<D>() * 64, D == 128 ? 1 : 2) void attn_gq
 hipError_t launch_attn_gqa_rows_q8(const AttnArgs& a, const ColPlan& p, const BlockScales& scales, dim3 grid,
                                    hipStream_t stream) {
     if (a.head_dim == 64)
-        hipLaunchKernelGGL((attn_gqa_rows_q8_kernel<64>), grid, dim3(row_waves<64>() * 64), 0, stream, a, p, scales);
+        hipLaunchKernelGGL((attn_gqa_rows_q8_kernel<64>), grid, dim3(kRowWaves * 64), 0, stream, a, p, scales);
     else
-        hipLaunchKernelGGL((attn_gqa_rows_q8_kernel<128>), grid, dim3(row_waves<128>() * 64), 0, stream, a, p, scales);
+        hipLaunchKernelGGL((attn_gqa_rows_q8_kernel<128>), grid, dim3(kRowWaves * 64), 0, stream, a, p, scales);
     return hipGetLastError();
 }
 
