@@ -615,10 +615,19 @@ int64_t col_items(const AttnArgs& a) { return (int64_t)a.n_layers * a.n_kv_heads
 // 24.4 / 46.0; 64 MLA sequences of which one has 512 keys, the others 32: 21.6 / 18.8,
 // so several are cut a little earlier than one).  Head size 64 has two workgroups a
 // CU, but columns use one: whole items up to twice the length when they outnumber
-// the slots.
+// the slots.  Over a cache held in 8 bits a whole item takes half as long, a merge as
+// long as ever (32 heads over 8 KV heads of 128, one query; whole / cut: 4 sequences,
+// 1024 keys 13.5 / 15.3 us, 1280 14.7 / 14.8, 1536 16.1 / 15.1; 16 heads of 64, 4
+// sequences, 1280 keys 12.2 / 14.2, 1800 14.3 / 14.3), and items that take one round and
+// half the CUs or more stay whole the longer, as cut ones have less to gain (16
+// sequences, 2048 keys 20.4 / 24.4, 100..2048 keys 19.9 / 20.6).
 bool col_whole(const AttnArgs& a) {
     const int64_t items = col_items(a);
-    const int64_t cut = a.variant == 1       ? (a.n_seqs == 1 ? 640 : 512)
+    const bool one_round = items <= kCUs && 2 * items >= kCUs;
+    const int64_t cut = a.dtype == 2         ? (one_round || (a.head_dim == 64 && items > 2 * kCUs) ? 2048
+                                                : a.head_dim == 64 && items <= kCUs                 ? 1536
+                                                                                                    : 1280)
+                        : a.variant == 1     ? (a.n_seqs == 1 ? 640 : 512)
                         : a.head_dim == 128  ? 832
                         : items > 2 * kCUs   ? 2048
                                              : 1024;
