@@ -773,9 +773,9 @@ hipError_t launch_columns(const AttnArgs& a, const BlockScales* scales, hipStrea
     // Measured costs of a column's shortest useful run and of starting an item
     // (set-up, first loads and merge: about 7 us), in tiles of one workgroup at head
     // size 128; the tiles of head size 64 take half as long, with the same counts.
-    // (A tile of codes takes half as long and starting an item does not: 16 caches of
-    // 8448..12544 slots, 4 KV heads of 128, 49 us a call with 12 tiles, 46.5 with 24; 64
-    // of 1000..5000, 8 KV heads, 94 and 92; 5 of 300..20000, 29.9 and 28.3.)
+    // (A tile of codes takes half as long and starting an item does not: with 12 / 24
+    // tiles 5 caches of 300..20000 slots, 8 KV heads of 128, take 27.1 / 25.9 us a call,
+    // 16 of 8448..12544 with 4 KV heads 44.1 / 43.5, with 2 KV heads of 64 26.4 / 25.2.)
     p.min_tiles = a.variant == 1 ? 4 : 8;
     p.item_cost = a.variant == 1 ? 4 : a.dtype == 2 ? 24 : 12;
     const int64_t cols = p.columns ? p.columns : (col_items(a) + kXcds - 1) / kXcds * kXcds;
