@@ -358,7 +358,7 @@ __global__ __launch_bounds__(kWaves * 64, D == 64 ? 5 : F32 ? 3 : 4) void store_
                             // Rounded as the formula stands, products and sum: which of two codes a value
                             // beside a rounding boundary gets is then the same as in a plain fp32 program.
                             // (An FMA for one product errs as often, on other values; 16 contexts of 4052
-                            // tokens in 4 layers: 180 us, 198 as it is.)
+                            // tokens in 4 layers: 180 us, 184 as it is.)
 #pragma clang fp contract(off)
                             const int ia = INTER ? 2 * i : i, ib = INTER ? 2 * i + 1 : i + 8;
                             const float u = x[t][ia], v = x[t][ib];
