@@ -128,7 +128,7 @@ ATTENTION_REFUSALS = [
     (dict(d__kv_base=BASE), 2), (dict(d__cache_slots=257), 2), (dict(d__max_kv_len=(1 << 30) + 1), 2),
     (dict(s__block_tokens=48), 2), (dict(s__block_tokens=128), 2), (dict(s__reserved=7), 2), (dict(pg__page_size=100), 2),
     (dict(s__v_stride=pkv._i64x4(-1, 1, 4, 4)), 2), (dict(d__k_stride=pkv._i64x3(655360, 128, (1 << 26) + 16)), 2),
-    (dict(d__k_stride=pkv._i64x3(655360, 128, 520)), 3), (dict(d__q_stride=pkv._i64x3(3072, 1024, 132)), 3),
+    (dict(d__k_stride=pkv._i64x3(655360, 128, 520)), 3), (dict(d__q_stride=pkv._i64x3(4096, 1024, 132)), 3),
     (dict(q=BASE + GB + 2), 3), (dict(k_pages=BASE + 2 * GB + 8), 3), (dict(pg__page_stride_k=100), 3),
     (dict(out=BASE + GB), 4), (dict(out=BASE + 3 * GB + 4096), 4), (dict(out=BASE + 11 * GB), 4), (dict(out=BASE + 10 * GB - 64), 4),
     (dict(d__n_splits=2), 1), (dict(d__n_splits=2, workspace=BASE + 12 * GB, workspace_bytes=16), 2),
