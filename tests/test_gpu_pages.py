@@ -271,3 +271,22 @@ def test_graph_of_free_fork_compact():
                 t[:, p] = t[:, int(old)].clone()
         g.copy_(cuda(table))
         g_ref.copy_(cuda(ref))
+
+
+def test_offsets_past_32_bits():
+    """Pages at the end of a pool of more than 4 GiB: a fork's copy and a compaction's moves."""
+    P, page, H, d = 70000, 64, 8, 128
+    pool = torch.empty((1, P, page, H, d), dtype=torch.uint8, device="cuda")
+    rng = np.random.default_rng(60)
+    body = torch.from_numpy(rng.integers(0, 256, (page, H, d)).astype(np.uint8)).cuda()
+    pool[0, P - 1], pool[0, P - 2], pool[0, 0] = body, 0, 0
+    ref = torch.ones(P, dtype=torch.int32, device="cuda")
+    ref[P - 2] = 0
+    table = torch.tensor([[P - 1, -1], [-1, -1]], dtype=torch.int32, device="cuda")
+    pkv.pages_fork([pool], ref, table, page, pkv.make_forks([dict(parent=0, child=1, n_tokens=41)], "cuda"), 1)
+    assert table.tolist() == [[P - 1, -1], [P - 2, -1]] and int(ref[P - 2]) == 1
+    assert torch.equal(pool[0, P - 2, :41], body[:41]) and not pool[0, P - 2, 41:].any()
+    ref[0] = 0
+    used = pkv.pages_compact([pool], ref, table, page)[-1]
+    assert table.tolist() == [[0, -1], [P - 2, -1]] and int(ref[P - 1]) == 0 and int(ref[0]) == 1 and int(used) == P - 1
+    assert torch.equal(pool[0, 0], body)

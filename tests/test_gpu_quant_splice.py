@@ -241,3 +241,29 @@ def test_side_stream_and_graph():
         call(want)
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, want)), i
+
+
+def test_offsets_past_32_bits():
+    """Pages at the end of pools of more than 4 GiB, and source slots as far in, get the bytes that small pools get."""
+    H, d, page, block, far = 8, 128, 64, 32, 70000
+    g = synth.Draws(50, "cpu")
+    rows = [g.normal((1, H, 100, d), torch.bfloat16).cuda() for _ in "kv"]
+    seg = lambda slot: pkv.make_segments_quant([dict(src_slot0=slot, seq=0, n_tokens=90, src_pos0=3, dst_pos0=20)], "cuda")   # noqa: E731
+    kv_len = torch.tensor([20], dtype=torch.int32, device="cuda")
+    results = []
+    for P, slots, first in ((2, 100, 5), (far, 2100000, 2099900)):
+        src = [torch.empty((1, slots, H, d), dtype=torch.bfloat16, device="cuda").permute(0, 2, 1, 3) for _ in "k"]
+        pools = [torch.empty((1, P, page, H, d), dtype=torch.uint8, device="cuda") for _ in "kv"]
+        scales = [torch.full((1, P, page // block, H), 120, dtype=torch.uint8, device="cuda") for _ in "kv"]
+        for t in pools:
+            t[:, P - 2:] = 0x38
+        src[0][:, :, first:first + 90] = rows[0][:, :, :90]
+        table = torch.tensor([[P - 1, P - 2]], dtype=torch.int32, device="cuda")
+        pkv.reposition_splice_quant(src[0], src[0], pools[0], pools[1], scales[0], scales[1], seg(first), 1, 90, kv_len, table, 1e4,
+                                    d, dst_capacity=2 * page)
+        torch.cuda.synchronize()
+        results.append([t[:, P - 2:].cpu() for t in pools + scales])
+        del src, pools, scales
+        torch.cuda.empty_cache()
+    for a, b in zip(*results):
+        assert torch.equal(a, b)
