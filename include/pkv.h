@@ -384,9 +384,9 @@ typedef struct pkv_segment_quant {
 
 /* Reposition + splice into a paged cache held in 8 bits (Sec. 5; Sec. 8: the cache
  * keeps per-token KV, so the operation carries over).  The source is bf16 or fp32 as
- * in pkv_reposition_splice_batched; rows are turned by delta with the arithmetic of
- * that call (coefficients in fp64 rounded to fp32) and quantised without an
- * intermediate rounding.  For a block that gets rows x_t, with `kept` the block's
+ * in pkv_reposition_splice_batched; rows are turned by delta in fp32, with
+ * coefficients of fp64 angles to 0.6 units in the last place, and quantised without
+ * an intermediate rounding.  For a block that gets rows x_t, with `kept` the block's
  * other slots below kv_len[seq] (the slots in use before the call):
  *     need = the smallest e >= 1 with max |x_t| <= 448 * 2^(e - 127)
  *     e    = need if nothing is kept, else max(need, the block's old e)

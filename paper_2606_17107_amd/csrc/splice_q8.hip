@@ -27,6 +27,11 @@
 //   * cos and sin are formed as exactly as fp32 holds them: an E4M3 code depends on the
 //     rotated value's last bits only near a rounding boundary, and there the fp32
 //     rotation decides as exactly as it can.
+//   * Measured (8 KV heads of 128): 4096 tokens into 32 layers 138 us a call, 808 MB at 5.9
+//     TB/s, what a copy of such rows reaches; 277 when every row was loaded once for the
+//     maximum and once for the codes.  16 contexts of 4052 tokens in 4 layers, whose source
+//     stays in the L2s, 184 us for 531 MB written: vector instructions take 72% of the
+//     cycles.  One token in each of 64 contexts 7 us, 5 in the kernel: a chain of loads.
 #include <math.h>
 
 #include "attn_columns.h"
