@@ -354,12 +354,12 @@ pkv_status pkv_suffix_attention_noalloc(const void* q, const void* k_cache, cons
 /* A paged cache of E4M3 codes (1 sign, 4 exponent, 3 fraction bits, bias 7, finite
  * up to 448, 0x7f and 0xff NaN, no infinities) with one scale byte e per block of
  * block_tokens slots, KV head, layer and tensor: a code of value c stands for
- * c * 2^(e - 127), exactly a bf16 number.  Pools and block tables are those of
- * pkv_paged_cache with one byte per element; the scale of (layer l, kv head h, page
- * P, block b of the page) is at l*stride[0] + h*stride[1] + P*stride[2] +
- * b*stride[3].  The library writes e in [1, 254]; over a block with e of 0 or 255 a
- * result is undefined.  Values go through paging->v_block_table when it is set, their
- * scales too. */
+ * c * 2^(e - 127).  Pools and block tables are those of pkv_paged_cache with one byte
+ * per element; the scale of (layer l, kv head h, page P, block b of the page) is at
+ * l*stride[0] + h*stride[1] + P*stride[2] + b*stride[3].  The library writes e in
+ * [1, 246], under which every finite code is finite in bf16; over a block with another
+ * e a result is undefined.  Values go through paging->v_block_table when it is set,
+ * their scales too. */
 typedef struct pkv_block_scales {
     int32_t block_tokens;      /* slots that share a scale: 32, 64 or 128, at most page_size */
     int32_t reserved;          /* must be 0 */
@@ -388,11 +388,12 @@ typedef struct pkv_segment_quant {
  * coefficients of fp64 angles to 0.6 units in the last place, and quantised without
  * an intermediate rounding.  For a block that gets rows x_t, with `kept` the block's
  * other slots below kv_len[seq] (the slots in use before the call):
- *     need = the smallest e >= 1 with max |x_t| <= 448 * 2^(e - 127)
+ *     need = the smallest e in [1, 246] with max |x_t| <= 448 * 2^(e - 127), or 246
  *     e    = need if nothing is kept, else max(need, the block's old e)
  *     code = E4M3(x_t * 2^(127 - e)), to the nearest, ties to even
  *     kept code = E4M3(code * 2^(old e - e)) where e grew, else unchanged
- * A NaN or an infinity is stored as NaN and does not enter the maximum.  Slots that
+ * A NaN or an infinity is stored as NaN and does not enter the maximum; a finite
+ * magnitude above 448 * 2^119 (2.98e38) is stored as the largest code.  Slots that
  * are neither written nor kept are left as they are, and blocks that get no row
  * altogether.  Segments of one call may share a block (chunks spliced back to back);
  * they must not write the same slot, and different sequences must not write into the

@@ -5,13 +5,15 @@
 //
 // For a block that receives the rows x_t and keeps the rows that it held before in
 // other slots below the sequence's length:
-//     need = the smallest e in [1, 254] with max |x_t| <= 448 * 2^(e - 127)
+//     need = the smallest e in [1, 246] with max |x_t| <= 448 * 2^(e - 127)
 //     e    = need, or max(need, old e) if the block keeps a row
 //     code = E4M3(x_t * 2^(127 - e))  to the nearest, ties to even
 // and where e grew, kept codes become E4M3(code * 2^(old e - e)).  Products with
 // powers of two are exact, so each stored value is rounded once; a kept row loses
 // nothing but what falls below E4M3's smallest step.  A NaN or an infinity is
-// stored as NaN (E4M3 has no infinity) and does not enter the maximum.
+// stored as NaN (E4M3 has no infinity) and does not enter the maximum.  246 is the
+// last e under which every code is finite in bf16; finite magnitudes above
+// 448 * 2^119 (2.98e38) get the largest code.
 //
 // Design (a stream of 2 or 4 bytes read and 1 written per element):
 //   * A wave owns 32 slots of one (layer, tensor, KV head): 8 lanes a row at head
@@ -42,6 +44,7 @@ namespace {
 constexpr int kWaves = 4;
 constexpr int kSub = 32;           // slots per wave
 constexpr int kPairs = 64;         // most rotary pairs of a row
+constexpr int kTop = 0x7f600000;   // fp32 bits of 448 * 2^119, the largest magnitude that is stored
 constexpr int64_t kMaxGridX = 0xffffffffll / (kWaves * 64);   // blocks: HIP refuses 2^32 threads in one dimension
 
 struct Freqs {
@@ -413,7 +416,9 @@ __global__ __launch_bounds__(kWaves * 64, D == 64 ? 5 : F32 ? 3 : 4) void store_
             }
             if (!working || !in_pool || !(any & 1)) return;
             // 448 = 1.75 * 2^8 is the largest code.
-            const int need = (top >> 23) - 8 + ((top & 0x7fffff) > 0x600000 ? 1 : 0);
+            const bool beyond = __builtin_amdgcn_readfirstlane(top) > kTop;
+            top = min(top, kTop);
+            const int need = (top >> 23) - 8 + ((top & 0x7fffff) > 0x600000 ? 1 : 0);   // at most 246
             e = max(need, 1);
             if (any & 2) e = max(e, old);
             const float scale = __uint_as_float((uint32_t)min(e, 254) << 23);   // 2^(e - 127)
@@ -431,6 +436,22 @@ __global__ __launch_bounds__(kWaves * 64, D == 64 ? 5 : F32 ? 3 : 4) void store_
                         const float* y = x[t] + 8 * h;
                         w[h] = u32x2{pack4(y[0], y[1], y[2], y[3], scale), pack4(y[4], y[5], y[6], y[7], scale)};
                     }
+                }
+                if (__builtin_expect(beyond, 0)) {   // the codes of finite values that came out as NaN become the largest
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            uint32_t lost = ((w[h][i] & 0x7f7f7f7fu) + 0x01010101u) >> 7 & 0x01010101u;   // 1 in each NaN byte
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) {
+                                uint32_t bits;
+                                if constexpr (PACKED) bits = k & 1 ? raw[t][h].a[2 * i + k / 2] : raw[t][h].a[2 * i + k / 2] << 16;
+                                else bits = __float_as_uint(x[t][8 * h + 4 * i + k]);
+                                lost &= ~(((bits & 0x7f800000u) + 0x00800000u) >> 31 << 8 * k);   // NaN or infinite itself
+                            }
+                            w[h][i] -= lost;
+                        }
                 }
                 if (pairs) {
                     // lanes 2m and 2m + 1 hold neighbouring chunks of either half of the row: one
