@@ -357,8 +357,8 @@ pkv_status pkv_suffix_attention_noalloc(const void* q, const void* k_cache, cons
  * c * 2^(e - 127).  Pools and block tables are those of pkv_paged_cache with one byte
  * per element; the scale of (layer l, kv head h, page P, block b of the page) is at
  * l*stride[0] + h*stride[1] + P*stride[2] + b*stride[3].  The library writes e in
- * [1, 246], under which every finite code is finite in bf16; over a block with another
- * e a result is undefined.  Values go through paging->v_block_table when it is set,
+ * [1, 246], under which every finite code is finite in bf16; it takes a byte above 246
+ * as 246 and a byte of 0 as 1.  Values go through paging->v_block_table when it is set,
  * their scales too. */
 typedef struct pkv_block_scales {
     int32_t block_tokens;      /* slots that share a scale: 32, 64 or 128, at most page_size */
@@ -423,9 +423,11 @@ size_t pkv_attention_quant_workspace_size(const pkv_attn_desc* desc, int32_t n_q
                                        int32_t head_dim);
 
 /* Suffix attention over a paged cache held in 8 bits: as pkv_suffix_attention_paged
- * with keys and values code * scale, which the kernels form exactly.  desc->dtype is
- * that of q and out, PKV_BF16; k and v strides are in bytes; GQA only.  A row's result
- * does not depend on the contents of slots that it does not see, NaN codes included.
+ * with keys and values code * scale as bf16 numbers (exact for e of 3 and more; for 1
+ * and 2 rounded to the nearest where a code falls between bf16's smallest steps).
+ * desc->dtype is that of q and out, PKV_BF16; k and v strides are in bytes; GQA only.
+ * A row's result does not depend on the contents of slots that it does not see, NaN
+ * codes included, nor on the scales of blocks of which it sees no slot.
  * Errors: as pkv_suffix_attention_paged; PKV_ERR_NULL (scales, k_scale, v_scale),
  * PKV_ERR_SHAPE (block_tokens, reserved, negative strides), PKV_ERR_UNSUPPORTED (MLA,
  * a dtype other than PKV_BF16), PKV_ERR_ALIAS (out overlaps the scales too). */

@@ -57,7 +57,8 @@ struct TileWindow {
         v_page = a.v_block_table ? min(max(a.v_block_table[entry], 0), top) : k_page;
         const uint8_t* const k = s.k + layer * s.k_stride[0] + kvh * s.k_stride[1];
         const uint8_t* const v = s.v + layer * s.v_stride[0] + kvh * s.v_stride[1];
-        exps = k[k_page * s.k_stride[2] + block * s.k_stride[3]] | (v[v_page * s.v_stride[2] + block * s.v_stride[3]] << 8);
+        exps = (int)(q8_exponent(k[k_page * s.k_stride[2] + block * s.k_stride[3]]) |
+                     q8_exponent(v[v_page * s.v_stride[2] + block * s.v_stride[3]]) << 8);
     }
     __device__ __forceinline__ bool holds(int i) const { return i < first + 64; }   // (tiles are visited in order)
     __device__ __forceinline__ int of(int reg, int i) const { return __builtin_amdgcn_readlane(reg, (i - first) & 63); }

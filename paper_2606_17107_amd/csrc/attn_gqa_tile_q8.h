@@ -4,9 +4,12 @@
 //
 // Codes become bf16 two an instruction (v_cvt_scalef32_pk_bf16_fp8, at the rate of
 // an FMA), with the block's scale, a power of two, applied by the same instruction:
-// a code times its scale is exactly a bf16 number, so everything behind the
-// conversion is the bf16 kernels' arithmetic over the dequantised cache.  In the
-// few-row kernel one wave reads a tile and converts it at its operand reads; the
+// a code times its scale is exactly a bf16 number (under the scale bytes 1 and 2 the
+// nearest one, as the smallest codes lie between bf16's steps there), so everything
+// behind the conversion is the bf16 kernels' arithmetic over the dequantised cache.
+// Bytes above 246, whose largest codes bf16 cannot hold, are taken as 246 and 0 as 1,
+// so that only NaN codes are not finite, whatever byte a block has that no row sees.
+// In the few-row kernel one wave reads a tile and converts it at its operand reads; the
 // many-row kernel's four waves share a tile and convert it once, on its way to LDS.
 #pragma once
 
@@ -59,6 +62,9 @@ __device__ __forceinline__ bf16x8 q8_to_bf16(uint32_t lo, uint32_t hi, float sca
     return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
+// The scale byte e that counts for a stored one.
+__device__ __forceinline__ uint32_t q8_exponent(uint32_t e) { return max(min(e, 246u), 1u); }
+
 typedef int i32x2 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ u32x2 q8_v_read(const uint8_t* base) {
     return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32(PKV_LDS(i32x2, base)));
@@ -109,7 +115,7 @@ struct CodeWindow {
             const int key = key_of(min(i, n_tiles - 1));   // (below the slots that the table covers)
             page = min(max(row[key >> a.page_shift], 0), top);
             const int block = (key & ((1 << a.page_shift) - 1)) >> block_shift;
-            scale = __uint_as_float((uint32_t)scales[page * page_stride + block * block_stride] << 23);
+            scale = __uint_as_float(q8_exponent(scales[page * page_stride + block * block_stride]) << 23);
         };
         const int i = from + (int)__lane_id();
         lookup(i, p0, s0);

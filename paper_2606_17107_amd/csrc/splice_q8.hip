@@ -420,8 +420,8 @@ __global__ __launch_bounds__(kWaves * 64, D == 64 ? 5 : F32 ? 3 : 4) void store_
             top = min(top, kTop);
             const int need = (top >> 23) - 8 + ((top & 0x7fffff) > 0x600000 ? 1 : 0);   // at most 246
             e = max(need, 1);
-            if (any & 2) e = max(e, old);
-            const float scale = __uint_as_float((uint32_t)min(e, 254) << 23);   // 2^(e - 127)
+            if (any & 2) e = min(max(e, old), 246);   // (a byte above 246 means 246, one of 0 means 1)
+            const float scale = __uint_as_float((uint32_t)e << 23);   // 2^(e - 127)
 #pragma unroll
             for (int t = 0; t < STEPS; ++t) {
                 if (rec[t] < 0) continue;
@@ -477,7 +477,7 @@ __global__ __launch_bounds__(kWaves * 64, D == 64 ? 5 : F32 ? 3 : 4) void store_
         if (!working || !in_pool || !(any & 1)) continue;
         if ((any & 2) && e > old) {
             // 2^(old - e): codes below 2^-18 of the largest one vanish, so no smaller factor is needed
-            const float down = exp2_int(max(old - e, -126));
+            const float down = exp2_int(max(max(old, 1) - e, -126));
 #pragma unroll
             for (int t = 0; t < STEPS; ++t) {
                 if (!kept[t]) continue;
