@@ -259,8 +259,12 @@ __global__ __launch_bounds__(kThreads) void pages_apply(PagesArgs a, int64_t row
                 int entry = kNone;
                 if (e < whole) {
                     entry = a.table_in[(int64_t)f.parent * a.max_pages + e];
-                    if (in_pool(a, entry)) atomicAdd(a.ref + entry, 1);
-                    else flag(a);
+                    if (in_pool(a, entry)) {
+                        atomicAdd(a.ref + entry, 1);
+                    } else {
+                        entry = kNone;
+                        flag(a);
+                    }
                 } else if (e == whole && (f.n_tokens & (a.page_size - 1))) {
                     entry = page;
                 }
