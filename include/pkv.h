@@ -495,7 +495,8 @@ pkv_status pkv_pages_free(const pkv_page_pool* pool, int32_t* ref, int32_t* bloc
  * Skipped records, which leave their child's row alone and set *err_flag: a row or
  * length out of range; a child that a record before it names; with table_out equal to
  * table_in, a parent that is a child of some record in range.  Also flagged: a free page
- * is missing, or the parent has no page where one is needed (the entry is -1).
+ * is missing, or the parent has no page where one is needed, or one whose count was not
+ * above 0 before the call, and so may now be another child's (the entry is -1).
  * Errors: PKV_ERR_NULL, PKV_ERR_SHAPE (also a workspace that is too small), PKV_ERR_ALIGN
  * (forks and workspace 16 bytes), PKV_ERR_ALIAS (tables that overlap in part, or tensors),
  * PKV_ERR_UNSUPPORTED (more than 65535 records; 2^31 units in one tensor's page),

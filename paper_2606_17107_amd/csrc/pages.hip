@@ -101,8 +101,9 @@ __global__ __launch_bounds__(kPlan) void pages_fork_plan(PagesArgs a) {
             valid = in_range(f) && claimed(f.child) == i && !(in_place && claimed(f.parent) != 0x7fffffff);
             const int tail = f.n_tokens & (a.page_size - 1);
             if (valid && tail) {
-                wants = in_pool(a, a.table_in[(int64_t)f.parent * a.max_pages + (f.n_tokens >> a.page_shift)]);
-                if (!wants) flag(a);   // the parent has no such page
+                const int page = a.table_in[(int64_t)f.parent * a.max_pages + (f.n_tokens >> a.page_shift)];
+                wants = in_pool(a, page) && a.ref[page] > 0;
+                if (!wants) flag(a);   // the parent has no such page, or one that nobody counts
             }
             if (!valid) flag(a);
         }
@@ -247,6 +248,19 @@ template <bool FORK>
 __global__ __launch_bounds__(kThreads) void pages_apply(PagesArgs a, int64_t row_jobs, int pieces, int4 tiles, int4 runs) {
     const int64_t per_move = (int64_t)tiles.x + tiles.y + tiles.z + tiles.w;
     const int64_t jobs = row_jobs + per_move * a.head[0];
+    // Fork: the page had a count before the call.  One that the plan has handed out since has count 1 by
+    // now (which nobody raises) and is among a.found, in ascending order.
+    auto counted = [&](int page) {
+        const int ref = a.ref[page];
+        if (ref != 1) return ref > 0;
+        int lo = 0, hi = a.head[0];
+        while (lo < hi) {
+            const int mid = (lo + hi) >> 1;
+            if (a.found[mid] < page) lo = mid + 1;
+            else hi = mid;
+        }
+        return lo == a.head[0] || a.found[lo] != page;
+    };
     for (int64_t j = blockIdx.x; j < jobs; j += gridDim.x) {
         if (j < row_jobs) {
             if constexpr (FORK) {
@@ -259,7 +273,7 @@ __global__ __launch_bounds__(kThreads) void pages_apply(PagesArgs a, int64_t row
                 int entry = kNone;
                 if (e < whole) {
                     entry = a.table_in[(int64_t)f.parent * a.max_pages + e];
-                    if (in_pool(a, entry)) {
+                    if (in_pool(a, entry) && counted(entry)) {
                         atomicAdd(a.ref + entry, 1);
                     } else {
                         entry = kNone;

@@ -31,3 +31,76 @@ def test_whole_entries_outside_the_pool():
         assert table == [[3, bad, 5, 6], [3, -1, 5, 0]] and flag == 1
         assert ref == [1, 0, 0, 2, 0, 2, 1]
         assert (pool[0] == [7] * 4 + [1] * 28).all()
+
+
+def test_uncounted_pages():
+    """A parent's page with count 0 is a free page: it may go to another child, and is not shared or copied."""
+    # row 1's whole page 0 is uncounted and becomes the last page of row 2, a copy of page 4
+    table, ref, pool, flag = run([[4, 9], [0, 5], [-1, -1], [-1, -1]], [0, 1, 1, 1, 1, 1], [(0, 2, 9), (1, 3, 32)])
+    assert table[2:] == [[0, -1], [-1, -1]] and ref == [1, 1, 1, 1, 1, 1] and flag == 1
+    assert (pool[0] == [5] * 9 + [1] * 23).all()
+    # row 1's last page 0 is uncounted, and the only free page
+    table, ref, pool, flag = run([[4, 9], [5, 0], [-1, -1], [-1, -1]], [0, 1, 1, 1, 1, 1], [(1, 3, 40)])
+    assert table[3] == [5, -1] and ref == [0, 1, 1, 1, 1, 2] and flag == 1
+    table, ref, pool, flag = run([[4, 9], [5, 0], [-1, -1], [-1, -1]], [0, 1, 1, 1, 1, 1], [(1, 3, 40), (0, 2, 1)])
+    assert table[2:] == [[0, -1], [5, -1]] and ref == [1, 1, 1, 1, 1, 2] and flag == 1
+    assert (pool[0] == [5] + [1] * 31).all()
+    # a count below 0 is neither
+    table, ref, pool, flag = run([[1, 0], [-1, -1]], [0, -3], [(0, 1, 32)])
+    assert table[1] == [-1, -1] and ref == [0, -3] and flag == 1
+
+
+def fork(ref, table, out, forks, page, same):
+    """Reference: what `forks` do, entry by entry."""
+    before, ref, out, copies, bad = ref, ref.copy(), out.copy(), [], False
+    counted = lambda p: 0 <= p < len(before) and before[p] > 0   # noqa: E731
+    children = {f[1] for f in forks}
+    free = iter(np.nonzero(before == 0)[0].tolist())
+    done = set()
+    for a, b, n in forks:
+        if b in done or (same and a in children):
+            bad = True
+            continue
+        done.add(b)
+        row, whole, tail = np.full(table.shape[1], -1, np.int32), n // page, n % page
+        for e in range(whole):
+            if counted(table[a, e]):
+                row[e] = table[a, e]
+                ref[row[e]] += 1
+            else:
+                bad = True
+        if tail:
+            new = next(free, None) if counted(table[a, whole]) else None
+            if new is None:
+                bad = True
+            else:
+                row[whole], ref[new] = new, 1
+                copies.append((table[a, whole], new, tail))
+        out[b] = row
+    return ref, out, copies, bad
+
+
+@pytest.mark.parametrize("same", [True, False])
+@pytest.mark.parametrize("seed", range(3))
+def test_many_forks_over_uncounted_pages(seed, same):
+    """Hundreds of records over rows with pages of every kind: counted, free, given to another child by the same call,
+    outside the pool."""
+    rng = np.random.default_rng(seed)
+    page, P, rows, width, n = 32, 4000, 60, 300, 700
+    ref = rng.integers(-1, 3, P).astype(np.int32)
+    ref[ref == 2] = 0
+    table = rng.integers(-2, P + 3, (rows + n, width)).astype(np.int32)
+    forks = [(int(a), rows + i, int(t)) for i, (a, t) in enumerate(zip(rng.integers(0, rows, n), rng.integers(0, width * page + 1, n)))]
+    if not same:
+        forks = [(a, i, t) for i, (a, _, t) in enumerate(forks)]
+    out = table if same else np.full_like(table, 5)
+    want_ref, want, copies, bad = fork(ref, table, out, forks, page, same)
+    got, got_ref, pool, flag = run(table, ref, forks, out=None if same else out)
+    np.testing.assert_array_equal(got, want)
+    np.testing.assert_array_equal(got_ref, want_ref)
+    first = ((np.arange(P) + 1) % 256).astype(np.uint8)
+    expect = np.repeat(first[:, None], page, 1)
+    for src, dst, tail in copies:
+        expect[dst, :tail] = first[src]
+    np.testing.assert_array_equal(pool, expect)
+    assert bad and flag == 1 and len(copies) > 100
