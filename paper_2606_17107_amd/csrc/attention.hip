@@ -579,8 +579,8 @@ Plan make_plan(const AttnArgs& a, int splits, int rows = 0) {
 // Workgroups that fit on one CU at once (LDS and register bound).
 int wgs_per_cu(const AttnArgs& a, const Plan& p) {
     if (a.variant == 1) return 1;                     // MLA: two 36 KB stages, one wave per SIMD
-    const int tile = 32;                              // keys per K/V tile
-    const int lds = p.ns * 2 * tile * a.head_dim * (a.dtype == 2 ? 1 : 2);
+    const int tile = 32;                              // keys per K/V tile, in bf16 over caches of 8 bits too
+    const int lds = p.ns * 2 * tile * a.head_dim * 2;
     const int n = (160 * 1024) / lds;
     return n < 1 ? 1 : (n > 2 ? 2 : n);               // two waves per SIMD at most (registers)
 }
