@@ -341,9 +341,12 @@ __global__ __launch_bounds__(kThreads) void pages_apply(PagesArgs a, int64_t row
     }
 }
 
+// Pieces of a block-table row, an entry a thread.
+int row_pieces(const PagesArgs& a) { return (a.max_pages - 1) / kThreads + 1; }
+
 template <bool FORK>
 hipError_t launch_apply(const PagesArgs& a, hipStream_t stream) {
-    const int pieces = (a.max_pages + kThreads - 1) / kThreads;
+    const int pieces = row_pieces(a);
     const int64_t row_jobs = FORK ? (int64_t)a.n * pieces : ((int64_t)a.n_seqs * a.max_pages + kThreads - 1) / kThreads;
     int tiles[4] = {0, 0, 0, 0}, runs[4] = {0, 0, 0, 0};
     int64_t per_move = 0;
@@ -393,7 +396,7 @@ void pages_set_workspace(PagesArgs& a, int n_forks, void* ws) {
 }
 
 hipError_t launch_pages_free(const PagesArgs& a, hipStream_t stream) {
-    const int y = (a.max_pages + kThreads - 1) / kThreads;
+    const int y = row_pieces(a);
     hipLaunchKernelGGL(pages_free_kernel, dim3((unsigned)a.n, (unsigned)(y < 64 ? y : 64)), dim3(kThreads), 0, stream, a);
     return hipGetLastError();
 }

@@ -104,3 +104,25 @@ def test_many_forks_over_uncounted_pages(seed, same):
         expect[dst, :tail] = first[src]
     np.testing.assert_array_equal(pool, expect)
     assert bad and flag == 1 and len(copies) > 100
+
+
+def test_rows_of_all_lengths():
+    """Block tables up to the widest that int32 counts: the last entries of a row are shared, cleared and freed as any."""
+    for width in (1, 255, 256, 257, 2 ** 31 - 1):
+        page = 32
+        table = torch.full((2, width), 9, dtype=torch.int32, device="cuda")
+        table[0] = -1
+        whole = min(width - 1, 3)
+        table[0, :whole] = torch.arange(1, 1 + whole, dtype=torch.int32, device="cuda")
+        ref = torch.tensor([0] + [1] * 5, dtype=torch.int32, device="cuda")
+        flag = torch.zeros(1, dtype=torch.int32, device="cuda")
+        pool = torch.zeros((1, 6, page, 1, 4), dtype=torch.uint8, device="cuda")
+        pkv.pages_fork([pool], ref, table, page, pkv.make_forks([dict(parent=0, child=1, n_tokens=whole * page)], "cuda"), 1,
+                       err_flag=flag)
+        assert table[1, :whole].tolist() == list(range(1, 1 + whole)) and bool((table[1, whole:] == -1).all())
+        assert ref.tolist() == [0] + [2] * whole + [1] * (5 - whole) and int(flag) == 0
+        table[1, width - 1] = 5
+        pkv.pages_free([pool], ref, table, page, torch.tensor([1], dtype=torch.int32, device="cuda"), err_flag=flag)
+        assert bool((table[1] == -1).all()) and ref.tolist() == [0] + [1] * whole + [1] * (4 - whole) + [0] and int(flag) == 0
+        del table
+        torch.cuda.empty_cache()
