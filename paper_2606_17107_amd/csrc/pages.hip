@@ -79,7 +79,7 @@ constexpr int kNone = -1, kSkipped = -2;   // PagesArgs::pages of a fork
 __global__ __launch_bounds__(kPlan) void pages_fork_plan(PagesArgs a) {
     const int t = threadIdx.x;
     const bool in_place = a.table_in == a.table;
-    for (int s = t; s < a.n_seqs; s += kPlan) a.claim[s] = 0x7fffffff;
+    for (uint32_t s = t; s < (uint32_t)a.n_seqs; s += kPlan) a.claim[s] = 0x7fffffff;   // (an int would wrap on its last step)
     __syncthreads();
     auto in_range = [&](const PageFork& f) {
         return f.parent >= 0 && f.parent < a.n_seqs && f.child >= 0 && f.child < a.n_seqs && f.n_tokens >= 0 &&

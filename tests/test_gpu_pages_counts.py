@@ -126,3 +126,16 @@ def test_rows_of_all_lengths():
         assert bool((table[1] == -1).all()) and ref.tolist() == [0] + [1] * whole + [1] * (4 - whole) + [0] and int(flag) == 0
         del table
         torch.cuda.empty_cache()
+
+
+def test_as_many_rows_as_int32_counts():
+    n, page = 2 ** 31 - 1, 32
+    table = torch.full((n, 1), -1, dtype=torch.int32, device="cuda")
+    table[0], table[n - 2] = 1, 2
+    ref = torch.tensor([0, 1, 1, 0], dtype=torch.int32, device="cuda")
+    pool = torch.arange(4, dtype=torch.uint8, device="cuda").reshape(1, 4, 1, 1, 1).repeat(1, 1, page, 1, 4)
+    forks = [dict(parent=0, child=n - 1, n_tokens=32), dict(parent=n - 2, child=1, n_tokens=7)]
+    flag = torch.zeros(1, dtype=torch.int32, device="cuda")
+    pkv.pages_fork([pool], ref, table, page, pkv.make_forks(forks, "cuda"), 2, err_flag=flag)
+    assert table[[0, 1, n - 2, n - 1], 0].tolist() == [1, 0, 2, 1] and ref.tolist() == [1, 2, 1, 0] and int(flag) == 0
+    assert pool[0, 0, :, 0, 0].tolist() == [2] * 7 + [0] * 25
