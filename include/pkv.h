@@ -404,7 +404,8 @@ typedef struct pkv_segment_quant {
  * v_dim head_dim, or 0 without values.  rope_offset a multiple of 8, rope_dim of 16.
  * omega: host fp64 [rope_dim/2] per-pair frequencies as in pkv_reposition_splice_freqs,
  * or NULL for rope_theta^(-2i/rope_dim).  segs: DEVICE array; max_seg_tokens: at least
- * every n_tokens (longer segments are spliced all the same, by fewer workgroups).
+ * every n_tokens (longer segments are spliced all the same, by fewer workgroups; with 0,
+ * or a dst_capacity of 0, nothing is done).
  * kv_len: device int32 [n_seqs].  A token whose sequence, slot, source slot or page
  * entry is out of range is skipped (and *layout->err_flag set).
  * Errors: PKV_ERR_NULL, PKV_ERR_SHAPE, PKV_ERR_ALIGN (pools and sources 16 bytes, segs 8),

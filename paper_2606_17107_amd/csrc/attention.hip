@@ -686,7 +686,9 @@ int attention_splits(const AttnArgs& a) {
     // Over a cache held in 8 bits up to 8 splits may be as short as 128 keys while each
     // workgroup has a CU of its own (8 KV heads of 4: 40 queries over 1000 keys 31.5 us a
     // call in 1 split, 17.8 in 7; 64 over 2048 25.8 in 4, 22.6 in 8; beyond, 16 sequences
-    // of 40 over 1000 33.0 in 1, 38.3 in 2).
+    // of 40 over 1000 33.0 in 1, 38.3 in 2).  One sequence in more than 8, with the host's
+    // part of a call: 40 over 4000 25.8 in 8, 24.3 in 10, 23.9 in 16; 64 over 4096 27.6 in
+    // 8, 26.4 in 10, 28.3 in 16; 100 over 3000 28.5 in 8, 32.0 in 10.
     const Plan p = make_plan(a, 1);
     const int64_t wgs = (int64_t)p.n_groups * p.rbs;   // workgroups per split
     const int64_t kv = seen_keys(a);

@@ -21,11 +21,11 @@
 //   * A cache held in 8 bits (Q8, paged): tiles in LDS are bf16 tiles like any
 //     other.  A wave loads its share of a tile's codes into registers two tiles
 //     before they go to their stage, and converts and writes them among the MFMAs
-//     of segment 2.  1024 queries of 28 heads over 50176 slots: 786 us (938 TF/s),
-//     as long as over the bf16 cache; 904 us with codes in LDS that every wave
-//     converts at its operand reads (four times the conversions), 926 us with all
-//     of a step's conversions before its MFMAs, conditions around its loads (the
-//     compiler then waits for the newest) and LDS writes two to a bank.
+//     of segment 2.  1024 queries of 28 heads over 50176 slots: 778 us (938 TF/s),
+//     768 over bf16 pages and 716 over a contiguous bf16 cache; 904 us with codes in
+//     LDS that every wave converts at its operand reads (four times the conversions),
+//     926 us with all of a step's conversions before its MFMAs, conditions around its
+//     loads (the compiler then waits for the newest) and LDS writes two to a bank.
 #include <type_traits>
 
 #include "attn_gqa_tile.h"

@@ -31,9 +31,12 @@
 //     rotation decides as exactly as it can.
 //   * Measured (8 KV heads of 128): 4096 tokens into 32 layers 138 us a call, 808 MB at 5.9
 //     TB/s, what a copy of such rows reaches; 277 when every row was loaded once for the
-//     maximum and once for the codes.  16 contexts of 4052 tokens in 4 layers, whose source
-//     stays in the L2s, 184 us for 531 MB written: vector instructions take 72% of the
-//     cycles.  One token in each of 64 contexts 7 us, 5 in the kernel: a chain of loads.
+//     maximum and once for the codes; the same from fp32 into 16 layers 119 us, 671 MB at
+//     5.7 TB/s.  16 contexts of 4052 tokens in 4 layers, whose source stays in the L2s, 184
+//     us for 531 MB written: vector instructions take 72% of the cycles (168 us where no row
+//     turns), and a third of the workgroups, sized by the longest of three chunks, have no
+//     block (154 us in a grid of 7 block places a chunk instead of 18; 161 us for one chunk
+//     a context).  One token in each of 64 contexts 7 us, 5 in the kernel: a chain of loads.
 #include <math.h>
 
 #include "attn_columns.h"
