@@ -11,10 +11,10 @@
 // this one's value MFMAs with the maxima of the next one's scores; codes are turned
 // into bf16 one operand ahead of their MFMA.
 //
-// Bound by HBM and, nearly as much, by the steps of a tile: 16 caches of 8448..12544
-// slots, 32 heads over 8 KV heads of 128, one query each, 79 us a call, 70 of them in this
-// kernel (4.9 TB/s) and 5 in the merge; 63 us a call with every page in L2; 130 over the
-// bf16 cache.  The first form, one step after another, took 96.
+// Bound by the latency of a tile's steps and by HBM: 16 caches of 8448..12544 slots, 32
+// heads over 8 KV heads of 128, one query each, 79 us a call, 70 of them in this kernel
+// (4.9 TB/s, VALU 23% and MFMA 11% busy) and 5 in the merge; 63 us a call with every page
+// in L2; 130 over the bf16 cache.  The first form, one step after another, took 96.
 #include <type_traits>
 
 #include "attn_columns.h"
