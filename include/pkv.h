@@ -518,6 +518,137 @@ pkv_status pkv_pages_compact(const pkv_page_pool* pool, const int32_t* ref_in, i
                              size_t workspace_bytes, void* stream);
 
 /* ---------------------------------------------------------------------------
+ * Trees of drafted tokens (speculative decoding)
+ * ------------------------------------------------------------------------- */
+
+/* A draft model proposes several tokens behind each context, as a tree; the target
+ * model reads the whole tree in one pass, and the longest run of tokens that its
+ * probabilities accept is kept.  Rows are packed as for suffix attention: sequence s
+ * owns rows cu_q[s] .. cu_q[s+1]-1, its tree.  Row 0 of a sequence is the root, the last
+ * token that is certain and whose keys are not in the cache yet; parent[i] is the
+ * number within the sequence of row i's parent, always below i, or -1 for a row without
+ * one.  The rows' keys and values lie beside the cache until they are accepted: the
+ * cache (its pages, shared or not, and its 8-bit scales) is not touched by tokens that
+ * are refused, and nothing is rolled back. */
+
+/* Ancestor masks and positions of trees.  Bit c % 32 of mask[r * mask_words + c / 32],
+ * r = cu_q[s] + i, is 1 when row c of the sequence is row i or one of its ancestors; the
+ * other bits are 0.  q_pos[r] = kv_len[s] + the number of row i's ancestors (optional:
+ * NULL, then kv_len may be NULL too).  mask_words: at least ceil(max_q / 32).  max_q: at
+ * least every sequence's row count (rows behind it are left alone) and at most 1024.  A
+ * parent outside [-1, i) is taken as -1 and sets *err_flag (optional).  Rows that no
+ * sequence owns are not written.
+ * Errors: PKV_ERR_NULL, PKV_ERR_SHAPE, PKV_ERR_UNSUPPORTED (max_q), PKV_ERR_DEVICE. */
+pkv_status pkv_tree_masks(const int32_t* parent, const int32_t* cu_q, const int32_t* kv_len, int32_t n_seqs,
+                          int32_t total_q, int32_t max_q, uint32_t* mask, int32_t mask_words, int32_t* q_pos,
+                          int32_t* err_flag, void* stream);
+
+/* The drafted rows of a tree-attention call: post-RoPE keys and values of the call's
+ * rows, in the type of q. */
+typedef struct pkv_draft {
+    const void* k;             /* device [layer][kv_head][row][head_dim] */
+    const void* v;             /* device [layer][kv_head][row][head_dim_v]; MLA: equal to k, with its strides */
+    int64_t k_stride[3];       /* {layer, head, row}, elements, non-negative, multiples of 16 bytes */
+    int64_t v_stride[3];
+    const uint32_t* mask;      /* device [total_q][mask_words], as pkv_tree_masks writes it or any other bits;
+                                  NULL: every row sees the rows of its sequence up to itself (a chain) */
+    int32_t mask_words;        /* at least ceil(max_q / 32) */
+    int32_t reserved;          /* must be 0 */
+} pkv_draft;
+
+/* Bytes of device workspace of pkv_tree_attention; quant: 1 over a cache held in 8 bits.
+ * 0 for a max_kv_len of 0, and on invalid arguments. */
+size_t pkv_tree_attention_workspace_size(const pkv_attn_desc* desc, int32_t n_q_heads, int32_t n_kv_heads,
+                                         int32_t head_dim, int32_t quant);
+
+/* Attention of trees over their caches and over their own rows.  As suffix attention
+ * (desc, q, out, q_pos, kv_len as there), with row i of a sequence seeing
+ *     slot j of the cache:    0 <= j < kv_len[s], j <= q_pos[i], and j > q_pos[i] - window if window > 0
+ *     row c of its sequence:  bit c of its mask, and q_pos[c] > q_pos[i] - window if window > 0
+ * under one softmax.  kv_len counts the cache's slots only.  paging NULL: a contiguous
+ * cache (bf16 or fp32 GQA, bf16 MLA); else a paged one (bf16); scales with paging: one
+ * held in 8 bits (GQA).  Scores, sums and products with the drafted rows are fp32.  A row that
+ * sees nothing is zeros (lse_out -inf).  What a row does not see does not reach it,
+ * NaN and infinities included; a visible drafted row whose score is -inf weighs nothing,
+ * whatever its values.
+ * Errors: as pkv_suffix_attention, _paged and _quant; PKV_ERR_NULL (draft, its k or v; scales
+ * without paging), PKV_ERR_SHAPE and PKV_ERR_ALIGN (its fields), PKV_ERR_ALIAS (out overlaps
+ * it too). */
+pkv_status pkv_tree_attention(const void* q, const void* k_cache, const void* v_cache, void* out, const int32_t* q_pos,
+                              const int32_t* kv_len, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, float scale,
+                              const pkv_attn_desc* desc, const pkv_draft* draft, const pkv_paged_cache* paging,
+                              const pkv_block_scales* scales, void* workspace, size_t workspace_bytes, void* stream);
+
+typedef struct pkv_verify_desc {
+    int32_t dtype;             /* of the probabilities: PKV_BF16 or PKV_F32 */
+    int32_t n_seqs;            /* at most 65535 */
+    int32_t total_q;
+    int32_t max_q;             /* at least every sequence's row count, at most 1024 */
+    int32_t vocab;
+    int32_t max_path;          /* entries of a sequence's path */
+    const int32_t* cu_q;       /* device int32 [n_seqs+1]; NULL allowed when n_seqs == 1 */
+    int64_t target_stride;     /* elements between rows of target_probs */
+    int64_t draft_stride;      /* ... of draft_probs */
+    int32_t* err_flag;         /* optional device int32 */
+    int64_t reserved;          /* must be 0 */
+} pkv_verify_desc;
+
+/* Bytes of device workspace of pkv_tree_verify (scratch: nothing in it needs clearing, and
+ * calls that overlap in time need one each).  0 on invalid arguments. */
+size_t pkv_tree_verify_workspace_size(const pkv_verify_desc* desc);
+
+/* Which drafted tokens the target accepts.  target_probs [row][vocab]: the target's
+ * probabilities of the token after each row; draft_probs: those that the row's children
+ * were drawn from, or NULL for children that were not drawn (the draft's most likely tokens,
+ * a table's).  tokens[r]: the row's token.  Random numbers in [0, 1) are inputs: u_accept[r]
+ * tests row r, u_sample[s] draws the token after the path.
+ * The walk begins at row 0, with weights w = p of the row where it is, p = target_probs, and
+ * b = 1 the sum that they are taken to have.  The row's children are tried in their order:
+ *     drawn:      child c of token x is accepted if w(x) > 0 and u_accept[c] * q(x) * b < w(x),
+ *                 q = draft_probs of the row; else a += b (a is 0 at first), w = max(p - a q, 0),
+ *                 b = the sum of w
+ *     not drawn:  ... if w(x) > 0 and u_accept[c] * b < w(x); else b -= w(x), w(x) = 0
+ * An accepted child becomes the row where the walk is.  So the tokens kept are distributed as the
+ * target's own samples.  The walk ends at a row of which no child is accepted, or when
+ * max_path rows are on the path.
+ * path[s][..]: the accepted rows (numbers in 0..total_q-1, row 0 of the sequence first), -1 behind
+ * them; n_accepted[s]: how many.  next_token[s]: the smallest v with w(v) > 0 whose running sum of w
+ * passes u_sample[s] times the whole sum (the last v with w(v) > 0 if none does); where w is 0
+ * throughout, p takes its place; where p is 0 too, -1, and *err_flag is set.
+ * Probabilities that are NaN, infinite or not above 0 count as 0.  A row whose parent or
+ * token is out of range is no child of any row, and sets *err_flag (parent -1 does not).  A sequence
+ * without rows has n_accepted 0 and next_token -1.  Sums and comparisons are in 64 bits and
+ * do not depend on timing.
+ * Errors: PKV_ERR_NULL, PKV_ERR_SHAPE (also a workspace that is too small), PKV_ERR_ALIGN
+ * (workspace 16 bytes, probabilities their type), PKV_ERR_UNSUPPORTED (dtype, sizes above those
+ * limits), PKV_ERR_DEVICE. */
+pkv_status pkv_tree_verify(const void* target_probs, const void* draft_probs, const int32_t* tokens, const int32_t* parent,
+                           const float* u_accept, const float* u_sample, int32_t* path, int32_t* n_accepted,
+                           int32_t* next_token, const pkv_verify_desc* desc, void* workspace, size_t workspace_bytes,
+                           void* stream);
+
+/* Bytes of device workspace of pkv_tree_commit; 0 unless quant (a cache held in 8 bits). */
+size_t pkv_tree_commit_workspace_size(int32_t n_seqs, int32_t max_path, int32_t quant);
+
+/* Append the accepted rows to the cache: for every sequence and i < n_accepted[s] (at most
+ * max_path), slot kv_len[s] + i of sequence s becomes row path[s * max_path + i] of draft_k and
+ * draft_v, bit for bit, or, with scales, as pkv_reposition_splice_quant stores it (rows are at
+ * their positions already: nothing is turned).  kv_len is read only: the caller raises it
+ * afterwards.  layout: dtype of the drafted rows (and of a cache without scales), n_tokens their
+ * count, the source strides theirs; dst_capacity the slots of the tensors, or of a paged
+ * sequence; the destination strides those of the cache (bytes with scales); v_dim 0 without values;
+ * rope_offset and rope_style are not used.  kv_base: device int64 [n_seqs], as in
+ * pkv_attn_desc (contiguous caches only).  A row, slot or page entry out of range is skipped (and
+ * *layout->err_flag set).  Different sequences must not write the same slot.
+ * Errors: as pkv_reposition_splice, _paged and _quant; PKV_ERR_SHAPE (kv_base with paging, also a
+ * workspace that is too small), PKV_ERR_UNSUPPORTED (max_path, or with scales n_seqs * max_path, above
+ * 65535). */
+pkv_status pkv_tree_commit(const void* draft_k, const void* draft_v, void* cache_k, void* cache_v, const int32_t* path,
+                           const int32_t* n_accepted, const int32_t* kv_len, const int64_t* kv_base, int32_t n_seqs,
+                           int32_t max_path, const pkv_layout* layout, const pkv_paged_cache* paging,
+                           const pkv_block_scales* scales, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
  * Diagnostics
  * ------------------------------------------------------------------------- */
 

@@ -429,7 +429,11 @@ PKV_EXPORT pkv_status pkv_reposition_splice_batched(const void* src_k, const voi
 
 namespace {
 
-size_t workspace_size(const pkv_attn_desc* desc, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, bool q8) {
+// Splits of a call; 0 for a tree without any cache, which has no first step.
+int plan_splits(const pkv::AttnArgs& a) { return a.partials && a.max_kv_len == 0 ? 0 : pkv::attention_splits(a); }
+
+size_t workspace_size(const pkv_attn_desc* desc, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, bool q8,
+                      bool tree = false) {
     if (!desc) return 0;
     // Geometry checks only; pointers are not needed to size the workspace.
     static const char dummy[16] __attribute__((aligned(16))) = {0};
@@ -441,7 +445,8 @@ size_t workspace_size(const pkv_attn_desc* desc, int32_t n_q_heads, int32_t n_kv
                                     n_kv_heads, head_dim, 1.0f, desc, false, a, nullptr, q8);
     memcpy(g_err, saved, sizeof g_err);
     if (st != PKV_OK) return 0;
-    return pkv::attention_workspace_bytes(a, pkv::attention_splits(a));
+    a.partials = tree;
+    return pkv::attention_workspace_bytes(a, plan_splits(a));
 }
 
 }  // namespace
@@ -491,12 +496,53 @@ void set_workspace(pkv::AttnArgs& a, void* workspace) {
     a.ws_lse = a.ws_o + rows * a.head_dim_v;
 }
 
+// The drafted rows of a tree-attention call (its other arguments are checked already).
+pkv_status check_draft(const pkv_draft* t, const void* out, const pkv::AttnArgs& a, const pkv_attn_desc* d,
+                       pkv::DraftArgs& da) {
+    if (!t->k || !t->v) return fail(PKV_ERR_NULL, "draft.k and draft.v are required");
+    if (t->reserved != 0) return fail(PKV_ERR_SHAPE, "draft.reserved must be 0");
+    if (!aligned16(t->k) || !aligned16(t->v)) return fail(PKV_ERR_ALIGN, "draft.k and draft.v must be 16-byte aligned");
+    if ((uintptr_t)t->mask & 3u) return fail(PKV_ERR_ALIGN, "draft.mask must be 4-byte aligned");
+    const int eb = a.dtype == PKV_F32 ? 4 : 2;
+    for (int i = 0; i < 3; ++i) {
+        if (t->k_stride[i] < 0 || t->v_stride[i] < 0) return fail(PKV_ERR_SHAPE, "strides must be non-negative");
+        if ((t->k_stride[i] * eb) % 16 || (t->v_stride[i] * eb) % 16)
+            return fail(PKV_ERR_ALIGN, "strides must be multiples of 16 bytes");
+    }
+    if (a.variant == PKV_ATTN_MLA && (t->v != t->k || memcmp(t->v_stride, t->k_stride, sizeof t->k_stride) != 0))
+        return fail(PKV_ERR_SHAPE, "MLA reads values from the latent channels: draft.v must be draft.k with the same strides");
+    if (t->mask && (t->mask_words <= 0 || t->mask_words < (a.max_q + 31) / 32))
+        return fail(PKV_ERR_SHAPE, "draft.mask_words (%d) must hold max_q (%d) bits", t->mask_words, a.max_q);
+    if (a.total_q > 0) {
+        const int64_t oc[3] = {a.n_layers, a.total_q, a.n_heads}, kc[3] = {a.n_layers, a.n_kv_heads, a.total_q};
+        const Range ro = extent(out, d->o_stride, oc, 3, a.head_dim_v, eb);
+        Range rm;
+        if (t->mask) {
+            rm.lo = (uintptr_t)t->mask;
+            rm.hi = rm.lo + (uintptr_t)a.total_q * t->mask_words * 4;
+        }
+        if (overlap(ro, extent(t->k, t->k_stride, kc, 3, a.head_dim, eb)) ||
+            overlap(ro, extent(t->v, t->v_stride, kc, 3, a.head_dim_v, eb)) || overlap(ro, rm))
+            return fail(PKV_ERR_ALIAS, "out overlaps the drafted rows or their mask");
+    }
+    da.k = t->k;
+    da.v = t->v;
+    for (int i = 0; i < 3; ++i) {
+        da.k_stride[i] = t->k_stride[i];
+        da.v_stride[i] = t->v_stride[i];
+    }
+    da.mask = t->mask;
+    da.mask_words = t->mask_words;
+    return PKV_OK;
+}
+
 pkv_status run_attention(const void* q, const void* k_cache, const void* v_cache, void* out, const int32_t* q_pos,
                          const int32_t* kv_len, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, float scale,
                          const pkv_attn_desc* desc, const pkv_paged_cache* paging, const pkv_block_scales* scales,
-                         void* workspace, size_t workspace_bytes, void* stream) {
+                         void* workspace, size_t workspace_bytes, void* stream, const pkv_draft* draft = nullptr) {
     pkv::AttnArgs a;
     pkv::BlockScales bs;
+    pkv::DraftArgs da;
     pkv_status st = check_attention(q, k_cache, v_cache, out, q_pos, kv_len, n_q_heads, n_kv_heads,
                                     head_dim, scale, desc, true, a, paging, scales != nullptr);
     if (st != PKV_OK) return st;
@@ -517,7 +563,12 @@ pkv_status run_attention(const void* q, const void* k_cache, const void* v_cache
         }
         bs.block_shift = scales->block_tokens == 32 ? 5 : scales->block_tokens == 64 ? 6 : 7;
     }
-    const int splits = pkv::attention_splits(a);
+    if (draft) {
+        st = check_draft(draft, out, a, desc, da);
+        if (st != PKV_OK) return st;
+        a.partials = 1;
+    }
+    const int splits = plan_splits(a);
     const size_t need = pkv::attention_workspace_bytes(a, splits);
     if (need > 0) {
         if (!workspace) return fail(PKV_ERR_NULL, "workspace of %zu bytes is required", need);
@@ -528,6 +579,9 @@ pkv_status run_attention(const void* q, const void* k_cache, const void* v_cache
     a.n_splits = splits;
     if (need > 0) set_workspace(a, workspace);
     if (a.total_q == 0) return ok();
+    if (draft)
+        return device_status(pkv::launch_tree_attention(a, scales ? &bs : nullptr, da, (hipStream_t)stream),
+                             "tree_attention launch");
     return device_status(pkv::launch_attention(a, scales ? &bs : nullptr, (hipStream_t)stream),
                          "suffix_attention launch");
 }
@@ -598,12 +652,13 @@ PKV_EXPORT pkv_status pkv_suffix_attention_noalloc(const void* q, const void* k_
     return device_status(pkv::launch_attention(a, nullptr, (hipStream_t)stream), "suffix_attention_noalloc launch");
 }
 
-PKV_EXPORT pkv_status pkv_reposition_splice_quant(const void* src_k, const void* src_v, void* k_pages, void* v_pages,
-                                               const pkv_segment_quant* segs, int32_t n_segs, int32_t max_seg_tokens,
-                                               const int32_t* kv_len, int32_t n_seqs, const double* omega,
-                                               float rope_theta, int32_t rope_dim, const pkv_layout* layout,
-                                               const pkv_paged_cache* paging, const pkv_block_scales* scales,
-                                               void* stream) {
+namespace {
+
+// The quantising splice.  accepted: its segments, in device memory, are first formed from these.
+pkv_status splice_quant(const void* src_k, const void* src_v, void* k_pages, void* v_pages, const pkv_segment_quant* segs,
+                        int32_t n_segs, int32_t max_seg_tokens, const int32_t* kv_len, int32_t n_seqs, const double* omega,
+                        float rope_theta, int32_t rope_dim, const pkv_layout* layout, const pkv_paged_cache* paging,
+                        const pkv_block_scales* scales, const pkv::TreeCommitArgs* accepted, void* stream) {
     static_assert(sizeof(pkv_segment_quant) == sizeof(pkv::StoreSegment), "segment layout");
     const pkv_layout* L = layout;
     if (!L) return fail(PKV_ERR_NULL, "layout is NULL");
@@ -722,7 +777,25 @@ PKV_EXPORT pkv_status pkv_reposition_splice_quant(const void* src_k, const void*
     }
     if (!pkv::store_fits(a))
         return fail(PKV_ERR_UNSUPPORTED, "n_layers x n_kv_heads or max_seg_tokens beyond the grid's limits");
+    if (accepted) {
+        pkv::TreeCommitArgs t = *accepted;
+        t.table[0] = paging->block_table;
+        const hipError_t e = pkv::launch_tree_segments(t, (pkv::StoreSegment*)segs, (hipStream_t)stream);
+        if (e != hipSuccess) return device_status(e, "tree_commit launch");
+    }
     return device_status(pkv::launch_store(a, (hipStream_t)stream), "reposition_splice_quant launch");
+}
+
+}  // namespace
+
+PKV_EXPORT pkv_status pkv_reposition_splice_quant(const void* src_k, const void* src_v, void* k_pages, void* v_pages,
+                                               const pkv_segment_quant* segs, int32_t n_segs, int32_t max_seg_tokens,
+                                               const int32_t* kv_len, int32_t n_seqs, const double* omega,
+                                               float rope_theta, int32_t rope_dim, const pkv_layout* layout,
+                                               const pkv_paged_cache* paging, const pkv_block_scales* scales,
+                                               void* stream) {
+    return splice_quant(src_k, src_v, k_pages, v_pages, segs, n_segs, max_seg_tokens, kv_len, n_seqs, omega, rope_theta,
+                        rope_dim, layout, paging, scales, nullptr, stream);
 }
 
 namespace {
@@ -871,6 +944,193 @@ PKV_EXPORT pkv_status pkv_pages_compact(const pkv_page_pool* pool, const int32_t
     a.table = table_out;
     a.n_used = n_used;
     return device_status(pkv::launch_pages_compact(a, (hipStream_t)stream), "pages_compact launch");
+}
+
+// ---- trees of drafted tokens ------------------------------------------------------
+
+PKV_EXPORT pkv_status pkv_tree_masks(const int32_t* parent, const int32_t* cu_q, const int32_t* kv_len, int32_t n_seqs,
+                                     int32_t total_q, int32_t max_q, uint32_t* mask, int32_t mask_words, int32_t* q_pos,
+                                     int32_t* err_flag, void* stream) {
+    if (!parent || !mask) return fail(PKV_ERR_NULL, "parent and mask are required");
+    if (q_pos && !kv_len) return fail(PKV_ERR_NULL, "q_pos needs kv_len");
+    if (n_seqs <= 0 || total_q < 0 || max_q < 0 || mask_words <= 0)
+        return fail(PKV_ERR_SHAPE, "n_seqs (%d) and mask_words (%d) must be positive, total_q (%d) and max_q (%d) non-negative",
+                    n_seqs, mask_words, total_q, max_q);
+    if (n_seqs > 1 && !cu_q) return fail(PKV_ERR_NULL, "cu_q is required when n_seqs > 1");
+    if (!cu_q) {
+        if (max_q < total_q) return fail(PKV_ERR_SHAPE, "max_q (%d) < total_q (%d)", max_q, total_q);
+        max_q = total_q;
+    }
+    if (max_q > pkv::kTreeMaxRows)
+        return fail(PKV_ERR_UNSUPPORTED, "trees of %d rows (at most %d)", max_q, pkv::kTreeMaxRows);
+    if (mask_words < (max_q + 31) / 32) return fail(PKV_ERR_SHAPE, "mask_words (%d) must hold max_q (%d) bits", mask_words, max_q);
+    if (total_q == 0 || max_q == 0) return ok();
+    const pkv::TreeMaskArgs a = {parent, cu_q, kv_len, n_seqs, total_q, max_q, mask_words, mask, q_pos, err_flag};
+    return device_status(pkv::launch_tree_masks(a, (hipStream_t)stream), "tree_masks launch");
+}
+
+PKV_EXPORT size_t pkv_tree_attention_workspace_size(const pkv_attn_desc* desc, int32_t n_q_heads, int32_t n_kv_heads,
+                                                    int32_t head_dim, int32_t quant) {
+    return workspace_size(desc, n_q_heads, n_kv_heads, head_dim, quant != 0, true);
+}
+
+PKV_EXPORT pkv_status pkv_tree_attention(const void* q, const void* k_cache, const void* v_cache, void* out,
+                                         const int32_t* q_pos, const int32_t* kv_len, int32_t n_q_heads,
+                                         int32_t n_kv_heads, int32_t head_dim, float scale, const pkv_attn_desc* desc,
+                                         const pkv_draft* draft, const pkv_paged_cache* paging,
+                                         const pkv_block_scales* scales, void* workspace, size_t workspace_bytes,
+                                         void* stream) {
+    if (!draft) return fail(PKV_ERR_NULL, "draft is NULL");
+    if (scales && !paging) return fail(PKV_ERR_NULL, "a cache held in 8 bits is paged: paging is NULL");
+    return run_attention(q, k_cache, v_cache, out, q_pos, kv_len, n_q_heads, n_kv_heads, head_dim, scale, desc, paging,
+                         scales, workspace, workspace_bytes, stream, draft);
+}
+
+namespace {
+
+pkv_status check_verify(const pkv_verify_desc* d) {
+    if (!d) return fail(PKV_ERR_NULL, "desc is NULL");
+    if (d->dtype != PKV_BF16 && d->dtype != PKV_F32)
+        return fail(PKV_ERR_UNSUPPORTED, "dtype %d (expected PKV_BF16 or PKV_F32)", d->dtype);
+    if (d->n_seqs <= 0 || d->total_q < 0 || d->max_q < 0 || d->vocab <= 0 || d->max_path <= 0)
+        return fail(PKV_ERR_SHAPE,
+                    "n_seqs (%d), vocab (%d) and max_path (%d) must be positive, total_q (%d) and max_q (%d) non-negative",
+                    d->n_seqs, d->vocab, d->max_path, d->total_q, d->max_q);
+    if (d->reserved != 0) return fail(PKV_ERR_SHAPE, "desc.reserved must be 0");
+    if (d->n_seqs > 1 && !d->cu_q) return fail(PKV_ERR_NULL, "cu_q is required when n_seqs > 1");
+    if (!d->cu_q && d->max_q < d->total_q) return fail(PKV_ERR_SHAPE, "max_q (%d) < total_q (%d)", d->max_q, d->total_q);
+    if (d->target_stride < 0 || d->draft_stride < 0) return fail(PKV_ERR_SHAPE, "strides must be non-negative");
+    if ((d->cu_q ? d->max_q : d->total_q) > pkv::kTreeMaxRows)
+        return fail(PKV_ERR_UNSUPPORTED, "trees of %d rows (at most %d)", d->max_q, pkv::kTreeMaxRows);
+    if (d->n_seqs > 65535) return fail(PKV_ERR_UNSUPPORTED, "at most 65535 sequences per call");
+    return PKV_OK;
+}
+
+}  // namespace
+
+PKV_EXPORT size_t pkv_tree_verify_workspace_size(const pkv_verify_desc* desc) {
+    char saved[sizeof g_err];
+    memcpy(saved, g_err, sizeof g_err);
+    const pkv_status st = check_verify(desc);
+    memcpy(g_err, saved, sizeof g_err);
+    return st == PKV_OK ? pkv::tree_verify_workspace_bytes(desc->n_seqs, desc->vocab) : 0;
+}
+
+PKV_EXPORT pkv_status pkv_tree_verify(const void* target_probs, const void* draft_probs, const int32_t* tokens,
+                                      const int32_t* parent, const float* u_accept, const float* u_sample, int32_t* path,
+                                      int32_t* n_accepted, int32_t* next_token, const pkv_verify_desc* desc,
+                                      void* workspace, size_t workspace_bytes, void* stream) {
+    const pkv_status st = check_verify(desc);
+    if (st != PKV_OK) return st;
+    if (!target_probs || !tokens || !parent || !u_accept || !u_sample || !path || !n_accepted || !next_token)
+        return fail(PKV_ERR_NULL, "target_probs, tokens, parent, u_accept, u_sample, path, n_accepted and next_token are required");
+    const uintptr_t eb = desc->dtype == PKV_BF16 ? 2 : 4;
+    if ((uintptr_t)target_probs % eb || (uintptr_t)draft_probs % eb)
+        return fail(PKV_ERR_ALIGN, "probabilities must be aligned to their type");
+    const size_t need = pkv::tree_verify_workspace_bytes(desc->n_seqs, desc->vocab);
+    if (!workspace) return fail(PKV_ERR_NULL, "workspace of %zu bytes is required", need);
+    if (workspace_bytes < need) return fail(PKV_ERR_SHAPE, "workspace_bytes %zu < required %zu", workspace_bytes, need);
+    if (!aligned16(workspace)) return fail(PKV_ERR_ALIGN, "workspace must be 16-byte aligned");
+    pkv::TreeVerifyArgs a;
+    memset(&a, 0, sizeof a);
+    a.target = target_probs;
+    a.draft = draft_probs;
+    a.target_stride = desc->target_stride;
+    a.draft_stride = desc->draft_stride;
+    a.tokens = tokens;
+    a.parent = parent;
+    a.cu_q = desc->cu_q;
+    a.u_accept = u_accept;
+    a.u_sample = u_sample;
+    a.dtype = desc->dtype;
+    a.n_seqs = desc->n_seqs;
+    a.total_q = desc->total_q;
+    a.max_q = desc->cu_q ? desc->max_q : desc->total_q;
+    a.vocab = desc->vocab;
+    a.max_path = desc->max_path;
+    a.path = path;
+    a.n_accepted = n_accepted;
+    a.next_token = next_token;
+    a.err_flag = desc->err_flag;
+    a.workspace = workspace;
+    return device_status(pkv::launch_tree_verify(a, (hipStream_t)stream), "tree_verify launch");
+}
+
+PKV_EXPORT size_t pkv_tree_commit_workspace_size(int32_t n_seqs, int32_t max_path, int32_t quant) {
+    if (!quant || n_seqs <= 0 || max_path <= 0) return 0;
+    return (size_t)n_seqs * max_path * sizeof(pkv_segment_quant);
+}
+
+PKV_EXPORT pkv_status pkv_tree_commit(const void* draft_k, const void* draft_v, void* cache_k, void* cache_v,
+                                      const int32_t* path, const int32_t* n_accepted, const int32_t* kv_len,
+                                      const int64_t* kv_base, int32_t n_seqs, int32_t max_path, const pkv_layout* layout,
+                                      const pkv_paged_cache* paging, const pkv_block_scales* scales, void* workspace,
+                                      size_t workspace_bytes, void* stream) {
+    const pkv_layout* L = layout;
+    if (!L) return fail(PKV_ERR_NULL, "layout is NULL");
+    if (!path || !n_accepted || !kv_len) return fail(PKV_ERR_NULL, "path, n_accepted and kv_len are required");
+    if (n_seqs <= 0 || max_path <= 0)
+        return fail(PKV_ERR_SHAPE, "n_seqs (%d) and max_path (%d) must be positive", n_seqs, max_path);
+    if (paging && kv_base) return fail(PKV_ERR_SHAPE, "kv_base must be NULL for a paged cache");
+    if (scales && !paging) return fail(PKV_ERR_NULL, "a cache held in 8 bits is paged: paging is NULL");
+    if (max_path > 65535 || (scales && (int64_t)n_seqs * max_path > 65535))
+        return fail(PKV_ERR_UNSUPPORTED, "max_path (%d), or into 8 bits n_seqs x max_path, above 65535", max_path);
+    pkv::TreeCommitArgs t;
+    memset(&t, 0, sizeof t);
+    t.n_rows = L->n_tokens;
+    t.capacity = L->dst_capacity;
+    t.path = path;
+    t.n_accepted = n_accepted;
+    t.kv_len = kv_len;
+    t.kv_base = kv_base;
+    t.n_seqs = n_seqs;
+    t.max_path = max_path;
+    t.err_flag = L->err_flag;
+    if (scales) {
+        const size_t need = pkv_tree_commit_workspace_size(n_seqs, max_path, 1);
+        if (!workspace) return fail(PKV_ERR_NULL, "workspace of %zu bytes is required", need);
+        if (workspace_bytes < need) return fail(PKV_ERR_SHAPE, "workspace_bytes %zu < required %zu", workspace_bytes, need);
+        if (!aligned16(workspace)) return fail(PKV_ERR_ALIGN, "workspace must be 16-byte aligned");
+        // Rows that are at their positions: any rotary slice will do, the smallest one.
+        pkv_layout at = *L;
+        at.rope_offset = 0;
+        at.rope_style = PKV_ROPE_HALF;
+        // (the checks of the splice come first: on an error nothing is enqueued)
+        return splice_quant(draft_k, draft_v, cache_k, cache_v, (const pkv_segment_quant*)workspace, n_seqs * max_path, 1,
+                            kv_len, n_seqs, nullptr, 1.0f, 16, &at, paging, scales, &t, stream);
+    }
+    pkv::SpliceArgs a;
+    pkv_layout at = *L;
+    at.rope_offset = 0;
+    at.rope_style = PKV_ROPE_HALF;
+    const pkv_status st = check_splice(draft_k, draft_v, cache_k, cache_v, 1.0f, 2 * (at.dtype == PKV_F32 ? 4 : 8), &at, false, a,
+                                       paging);
+    if (st != PKV_OK) return st;
+    if (a.n_tokens == 0 || a.dst_capacity == 0) return ok();
+    t.src[0] = a.src_k;
+    t.src[1] = a.src_v;
+    t.dst[0] = a.dst_k;
+    t.dst[1] = a.dst_v;
+    for (int i = 0; i < 3; ++i) {
+        t.src_stride[0][i] = a.src_k_stride[i] * a.elem_bytes;
+        t.src_stride[1][i] = a.src_v_stride[i] * a.elem_bytes;
+        t.dst_stride[0][i] = a.dst_k_stride[i] * a.elem_bytes;
+        t.dst_stride[1][i] = a.dst_v_stride[i] * a.elem_bytes;
+    }
+    t.row_bytes[0] = a.head_dim * a.elem_bytes;
+    t.row_bytes[1] = a.v_dim * a.elem_bytes;
+    t.n_layers = a.n_layers;
+    t.n_kv_heads = a.n_kv_heads;
+    if (paging) {
+        t.table[0] = a.dst_pages;
+        t.table[1] = a.dst_v_pages ? a.dst_v_pages : a.dst_pages;
+        t.page_shift = a.page_shift;
+        t.max_pages = a.max_pages;
+        t.n_pages = a.n_pages;
+        t.page_stride[0] = a.dst_k_page_stride * a.elem_bytes;
+        t.page_stride[1] = a.dst_v_page_stride * a.elem_bytes;
+    }
+    return device_status(pkv::launch_tree_commit(t, (hipStream_t)stream), "tree_commit launch");
 }
 
 PKV_EXPORT const char* pkv_last_error(void) { return g_err; }

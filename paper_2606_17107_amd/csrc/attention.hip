@@ -186,7 +186,7 @@ __global__ __launch_bounds__(128) void attn_gqa_f32(AttnArgs a, Plan p) {
     const int64_t row = si.q0 + qi;
     // Element 4 jj + rr of block db holds channel 32 db + 8 jj + 4 hl + rr of the row.
     float* dst;
-    if (p.splits == 1) {
+    if (p.direct) {
         dst = (float*)a.out + (int64_t)layer * a.o_stride[0] + row * a.o_stride[1] + (int64_t)head * a.o_stride[2];
         if (a.lse_out && hl == 0)
             a.lse_out[((int64_t)layer * a.total_q + row) * a.n_heads + head] = lse2 * kLn2;
@@ -391,7 +391,7 @@ __global__ __launch_bounds__(256) void attn_gqa_f32_keys(AttnArgs a, Plan p) {
         const int q = (m0 + r) / p.G;
         const int hd = kvh * p.G + m0 + r - q * p.G;
         const int64_t row = si.q0 + q;
-        if (p.splits == 1) {
+        if (p.direct) {
             *(f32x4*)((float*)a.out + (int64_t)layer * a.o_stride[0] + row * a.o_stride[1] +
                       (int64_t)hd * a.o_stride[2] + c * 4) = acc * inv;
             if (a.lse_out && c == 0)
@@ -558,6 +558,7 @@ Plan make_plan(const AttnArgs& a, int splits, int rows = 0) {
     p.rbs = (int)((m_rows + p.BM - 1) / p.BM);
     if (p.rbs < 1) p.rbs = 1;
     p.splits = splits;
+    p.direct = splits == 1 && !a.partials;
     p.n_groups = a.n_layers * a.n_kv_heads * a.n_seqs * splits;
     p.longest_first = 0;
     // Row blocks on the fullest XCD when a group is shared by 1, 2, 4 or 8 XCDs;
@@ -721,7 +722,7 @@ int attention_splits(const AttnArgs& a) {
 }
 
 size_t attention_workspace_bytes(const AttnArgs& a, int n_splits) {
-    if (n_splits <= 1) return 0;
+    if (n_splits <= 1 && !a.partials) return 0;
     const size_t rows = (size_t)n_splits * a.n_layers * a.total_q * a.n_heads;
     return rows * a.head_dim_v * sizeof(float) + rows * sizeof(float);
 }
@@ -786,7 +787,7 @@ hipError_t launch_columns(const AttnArgs& a, const BlockScales* scales, hipStrea
     const hipError_t e = a.variant == 1 ? launch_attn_mla_rows(a, p, grid, stream)
                          : scales       ? launch_attn_gqa_rows_q8(a, p, *scales, grid, stream)
                                         : launch_attn_gqa_rows(a, p, grid, stream);
-    if (e != hipSuccess || p.columns == 0) return e;
+    if (e != hipSuccess || p.columns == 0 || a.partials) return e;
     return launch_combine(a, true, stream);
 }
 
@@ -821,7 +822,7 @@ hipError_t launch_attention(const AttnArgs& a, const BlockScales* scales, hipStr
     } else {
         e = a.variant == 1 ? launch_attn_mla_bf16(a, p, grid, stream) : launch_attn_gqa_bf16(a, p, scales, grid, stream);
     }
-    if (e != hipSuccess || p.splits == 1) return e;
+    if (e != hipSuccess || p.splits == 1 || a.partials) return e;
     return launch_combine(a, false, stream);
 }
 

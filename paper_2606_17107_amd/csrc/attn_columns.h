@@ -7,7 +7,8 @@
 // number of tiles however ragged the cache lengths are.  A column's run of tiles
 // covers the end of one item (stream, sequence), any number of whole items, and
 // the beginning of another: an item inside one column is finished there, an item
-// cut by column borders leaves one partial per column for the combine pass.  The
+// cut by column borders leaves one partial per column for the combine pass (with
+// a.partials every item leaves its partials).  The
 // borders follow all lengths of the call, so where one sequence is cut, and with
 // it the rounding of its result, depends on the others.  Short caches are not cut:
 // a workgroup takes a whole item, and sequences do not affect each other.
@@ -170,7 +171,7 @@ __device__ inline ColSegment col_segment(const ColSeqs& c, const ColPlan& p, uin
 // End of an item: the NW waves' O (row-major fp32 in LDS, wave w's at
 // o_lds + w * wave_stride, 16-byte chunk c of row r at chunk c ^ (r mod chunks)),
 // maxima and sums are merged over all threads of the workgroup and written: as
-// the output row when the item lies in this column, else as piece sg.piece of
+// the output row when the item lies in this column (and nothing joins it later), else as piece sg.piece of
 // the workspace (normalised, with its log2-sum-exp).  Row r < M is (query r / G,
 // head head0 + r % G) of the item.
 template <int NW, int ROWS, int DV>
@@ -206,7 +207,7 @@ __device__ __forceinline__ void col_merge_rows(const AttnArgs& a, const ColPlan&
         const int64_t row = si.q0 + q;
         const int64_t item = ((int64_t)layer * a.total_q + row) * a.n_heads + head;
         acc *= inv;
-        if (sg.pieces == 1) {
+        if (sg.pieces == 1 && !a.partials) {
             u32x2 w;
             w[0] = bf_rne(acc[0]) | (bf_rne(acc[1]) << 16);
             w[1] = bf_rne(acc[2]) | (bf_rne(acc[3]) << 16);

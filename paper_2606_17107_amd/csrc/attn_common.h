@@ -34,6 +34,7 @@ struct Plan {
     int n_groups;   // layers x kv heads x sequences x splits
     int shares, share_rbs;   // XCDs that share a group, row blocks of one share
     int splits;     // each workgroup's key range is shared by this many splits in equal runs of whole tiles
+    int direct;     // rows are finished here (one split, and nothing joins them later)
     int longest_first;   // sequences are dispatched longest first
     int qb, nw, ns; // bf16 GQA kernel shape: 32-row blocks per wave, waves, LDS stages
 };

@@ -863,7 +863,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_gqa_bf16_kernel(AttnArgs 
         const float inv = row_inverse(l_tot);
         const float lse2 = row_lse2(m_run[qb], l_tot);
         const int64_t row = si.q0 + qi[qb];
-        if (p.splits == 1) {
+        if (p.direct) {
             uint16_t* orow = (uint16_t*)a.out + (int64_t)layer * a.o_stride[0] + row * a.o_stride[1] +
                              (int64_t)head[qb] * a.o_stride[2];
 #pragma unroll

@@ -202,6 +202,7 @@ struct AttnArgs {
     int32_t max_kv_len;
     int32_t n_splits;
     int32_t auto_splits;      // n_splits is the library's own choice (the few-row kernels are eligible)
+    int32_t partials;         // every row goes to the workspace, for a pass that joins it with more keys
     int32_t window;           // 0: full causal; W > 0: slots j > q_pos - W only
     int64_t cache_slots;
     float scale;
@@ -224,5 +225,78 @@ struct AttnArgs {
 int attention_splits(const AttnArgs& a);
 size_t attention_workspace_bytes(const AttnArgs& a, int n_splits);
 hipError_t launch_attention(const AttnArgs& a, const BlockScales* scales, hipStream_t stream);   // scales: dtype 2
+
+// ---- trees of drafted tokens ----------------------------------------------------
+
+// The drafted rows of a tree-attention call, which lie beside the cache, and which of
+// them each row sees.
+struct DraftArgs {
+    const void* k;
+    const void* v;
+    int64_t k_stride[3];      // {layer, head, row}, elements
+    int64_t v_stride[3];
+    const uint32_t* mask;     // [total_q][mask_words], or null: a row sees the rows of its sequence up to itself
+    int32_t mask_words;
+};
+
+// Attention over the cache (its partials, if it has slots at all, into a.ws_o and
+// a.ws_lse: a.partials is set) joined with the drafted rows.
+hipError_t launch_tree_attention(const AttnArgs& a, const BlockScales* scales, const DraftArgs& d, hipStream_t stream);
+hipError_t launch_tree_join(const AttnArgs& a, const DraftArgs& d, hipStream_t stream);   // its second step
+
+struct TreeMaskArgs {
+    const int32_t* parent;
+    const int32_t* cu_q;      // may be null (one sequence)
+    const int32_t* kv_len;
+    int32_t n_seqs, total_q, max_q, mask_words;
+    uint32_t* mask;
+    int32_t* q_pos;           // may be null
+    int32_t* err_flag;        // may be null
+};
+constexpr int kTreeMaxRows = 1024;   // rows of one sequence whose tree is walked
+hipError_t launch_tree_masks(const TreeMaskArgs& a, hipStream_t stream);
+
+struct TreeVerifyArgs {
+    const void* target;       // [total_q][vocab], row strides in elements
+    const void* draft;        // or null
+    int64_t target_stride, draft_stride;
+    const int32_t* tokens;
+    const int32_t* parent;
+    const int32_t* cu_q;
+    const float* u_accept;
+    const float* u_sample;
+    int32_t dtype;            // 0 bf16, 1 fp32
+    int32_t n_seqs, total_q, max_q, vocab, max_path;
+    int32_t* path;
+    int32_t* n_accepted;
+    int32_t* next_token;
+    int32_t* err_flag;
+    void* workspace;
+};
+size_t tree_verify_workspace_bytes(int n_seqs, int vocab);
+hipError_t launch_tree_verify(const TreeVerifyArgs& a, hipStream_t stream);
+
+struct TreeCommitArgs {
+    const char* src[2];       // keys, values (or null)
+    char* dst[2];
+    int64_t src_stride[2][3]; // bytes, {layer, head, row}
+    int64_t dst_stride[2][3];
+    int32_t row_bytes[2];     // 0 without values
+    int32_t n_layers, n_kv_heads, n_rows;
+    int64_t capacity;         // slots of the tensor, or logical slots of a paged sequence
+    const int32_t* path;
+    const int32_t* n_accepted;
+    const int32_t* kv_len;
+    const int64_t* kv_base;   // may be null
+    int32_t n_seqs, max_path;
+    const int32_t* table[2];  // null: contiguous
+    int32_t page_shift, max_pages;
+    int64_t n_pages;
+    int64_t page_stride[2];   // bytes
+    int32_t* err_flag;
+};
+hipError_t launch_tree_commit(const TreeCommitArgs& a, hipStream_t stream);
+// The accepted rows as one-row segments of the quantising splice, n_seqs x max_path records.
+hipError_t launch_tree_segments(const TreeCommitArgs& a, StoreSegment* segs, hipStream_t stream);
 
 }  // namespace pkv

@@ -109,11 +109,29 @@ class pkv_fork(ctypes.Structure):
                 ("reserved", ctypes.c_int32)]
 
 
+class pkv_draft(ctypes.Structure):
+    _fields_ = [
+        ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_stride", _i64x3), ("v_stride", _i64x3),
+        ("mask", ctypes.c_void_p), ("mask_words", ctypes.c_int32), ("reserved", ctypes.c_int32),
+    ]
+
+
+class pkv_verify_desc(ctypes.Structure):
+    _fields_ = [
+        ("dtype", ctypes.c_int32), ("n_seqs", ctypes.c_int32), ("total_q", ctypes.c_int32), ("max_q", ctypes.c_int32),
+        ("vocab", ctypes.c_int32), ("max_path", ctypes.c_int32), ("cu_q", ctypes.c_void_p),
+        ("target_stride", ctypes.c_int64), ("draft_stride", ctypes.c_int64), ("err_flag", ctypes.c_void_p),
+        ("reserved", ctypes.c_int64),
+    ]
+
+
 SYMBOLS = ("pkv_reposition_splice", "pkv_reposition_splice_freqs", "pkv_reposition_splice_paged",
            "pkv_reposition_splice_batched", "pkv_attention_workspace_size", "pkv_suffix_attention",
            "pkv_suffix_attention_paged", "pkv_suffix_attention_noalloc", "pkv_reposition_splice_quant",
            "pkv_attention_quant_workspace_size", "pkv_suffix_attention_quant", "pkv_pages_workspace_size", "pkv_pages_free",
-           "pkv_pages_fork", "pkv_pages_compact", "pkv_last_error", "pkv_version")
+           "pkv_pages_fork", "pkv_pages_compact", "pkv_tree_masks", "pkv_tree_attention_workspace_size", "pkv_tree_attention",
+           "pkv_tree_verify_workspace_size", "pkv_tree_verify", "pkv_tree_commit_workspace_size", "pkv_tree_commit",
+           "pkv_last_error", "pkv_version")
 PKV_NOALLOC_SCRATCH_BYTES = 64 << 20
 
 _lib = None
@@ -178,6 +196,21 @@ def lib() -> ctypes.CDLL:
     L.pkv_pages_fork.argtypes = [pool, P, P, P, P, I, P, ctypes.c_size_t, P]
     L.pkv_pages_compact.restype = ctypes.c_int
     L.pkv_pages_compact.argtypes = [pool, P, P, P, P, P, P, ctypes.c_size_t, P]
+    L.pkv_tree_masks.restype = ctypes.c_int
+    L.pkv_tree_masks.argtypes = [P, P, P, I, I, I, P, I, P, P, P]
+    L.pkv_tree_attention_workspace_size.restype = ctypes.c_size_t
+    L.pkv_tree_attention_workspace_size.argtypes = [D, I, I, I, I]
+    L.pkv_tree_attention.restype = ctypes.c_int
+    L.pkv_tree_attention.argtypes = [P, P, P, P, P, P, I, I, I, F, D, ctypes.POINTER(pkv_draft), A, S, P, ctypes.c_size_t, P]
+    verify = ctypes.POINTER(pkv_verify_desc)
+    L.pkv_tree_verify_workspace_size.restype = ctypes.c_size_t
+    L.pkv_tree_verify_workspace_size.argtypes = [verify]
+    L.pkv_tree_verify.restype = ctypes.c_int
+    L.pkv_tree_verify.argtypes = [P, P, P, P, P, P, P, P, P, verify, P, ctypes.c_size_t, P]
+    L.pkv_tree_commit_workspace_size.restype = ctypes.c_size_t
+    L.pkv_tree_commit_workspace_size.argtypes = [I, I, I]
+    L.pkv_tree_commit.restype = ctypes.c_int
+    L.pkv_tree_commit.argtypes = [P, P, P, P, P, P, P, P, I, I, ctypes.POINTER(pkv_layout), A, S, P, ctypes.c_size_t, P]
     L.pkv_last_error.restype = ctypes.c_char_p
     L.pkv_last_error.argtypes = []
     L.pkv_version.restype = ctypes.c_int32
@@ -397,6 +430,44 @@ def pkv_pages_compact(pool, ref_in, ref_out, table_in, table_out, n_used, worksp
                       stream=None) -> int:
     return lib().pkv_pages_compact(_ref(pool), _ptr(ref_in), _ptr(ref_out), _ptr(table_in), _ptr(table_out),
                                    _ptr(n_used), _ptr(workspace), int(workspace_bytes), _stream(stream))
+
+
+def pkv_tree_masks(parent, cu_q, kv_len, n_seqs, total_q, max_q, mask, mask_words, q_pos, err_flag, stream=None) -> int:
+    return lib().pkv_tree_masks(_ptr(parent), _ptr(cu_q), _ptr(kv_len), int(n_seqs), int(total_q), int(max_q), _ptr(mask),
+                                int(mask_words), _ptr(q_pos), _ptr(err_flag), _stream(stream))
+
+
+def pkv_tree_attention_workspace_size(desc, n_q_heads, n_kv_heads, head_dim, quant) -> int:
+    return int(lib().pkv_tree_attention_workspace_size(_ref(desc), int(n_q_heads), int(n_kv_heads), int(head_dim), int(quant)))
+
+
+def pkv_tree_attention(q, k_cache, v_cache, out, q_pos, kv_len, n_q_heads, n_kv_heads, head_dim, scale, desc, draft, paging,
+                       scales, workspace, workspace_bytes, stream=None) -> int:
+    return lib().pkv_tree_attention(_ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(out), _ptr(q_pos), _ptr(kv_len),
+                                    int(n_q_heads), int(n_kv_heads), int(head_dim), float(scale), _ref(desc), _ref(draft),
+                                    _ref(paging), _ref(scales), _ptr(workspace), int(workspace_bytes), _stream(stream))
+
+
+def pkv_tree_verify_workspace_size(desc) -> int:
+    return int(lib().pkv_tree_verify_workspace_size(_ref(desc)))
+
+
+def pkv_tree_verify(target_probs, draft_probs, tokens, parent, u_accept, u_sample, path, n_accepted, next_token, desc,
+                    workspace, workspace_bytes, stream=None) -> int:
+    return lib().pkv_tree_verify(_ptr(target_probs), _ptr(draft_probs), _ptr(tokens), _ptr(parent), _ptr(u_accept),
+                                 _ptr(u_sample), _ptr(path), _ptr(n_accepted), _ptr(next_token), _ref(desc),
+                                 _ptr(workspace), int(workspace_bytes), _stream(stream))
+
+
+def pkv_tree_commit_workspace_size(n_seqs, max_path, quant) -> int:
+    return int(lib().pkv_tree_commit_workspace_size(int(n_seqs), int(max_path), int(quant)))
+
+
+def pkv_tree_commit(draft_k, draft_v, cache_k, cache_v, path, n_accepted, kv_len, kv_base, n_seqs, max_path, layout, paging,
+                    scales, workspace, workspace_bytes, stream=None) -> int:
+    return lib().pkv_tree_commit(_ptr(draft_k), _ptr(draft_v), _ptr(cache_k), _ptr(cache_v), _ptr(path), _ptr(n_accepted),
+                                 _ptr(kv_len), _ptr(kv_base), int(n_seqs), int(max_path), _ref(layout), _ref(paging),
+                                 _ref(scales), _ptr(workspace), int(workspace_bytes), _stream(stream))
 
 
 def pkv_last_error() -> str:
@@ -846,3 +917,253 @@ def pages_compact(tensors, ref, block_table, page_size, ref_out=None, block_tabl
     workspace, size = _pages_workspace(pool, 0, workspace, dev, stream)
     _check(pkv_pages_compact(pool, ref, ref_out, block_table, out, n_used, workspace, size, stream))
     return n_used
+
+
+# ---- trees of drafted tokens -------------------------------------------------------
+# Rows are packed as for suffix attention (cu_q); drafted keys and values are
+# [layer][kv_head][row][channel] (any strides, channels contiguous) beside the cache.
+# Masks are int32 (or uint32) words [total_q][ceil(max_q / 32)].
+
+_MASK_TYPES = tuple(t for t in (torch.int32, getattr(torch, "uint32", None)) if t is not None)
+
+
+def _check_mask(mask, dev, rows: int, max_q: int) -> None:
+    if mask is None:
+        return
+    _need(mask, "mask", dev, contiguous=True)
+    if mask.dtype not in _MASK_TYPES:
+        raise TypeError("mask must be one of %s, got %s" % (_MASK_TYPES, mask.dtype))
+    if mask.dim() != 2 or mask.shape[0] < rows or mask.shape[1] * 32 < max_q:
+        raise ValueError("mask %s must be [total_q][mask_words] for %d rows of %d bits" % (tuple(mask.shape), rows, max_q))
+
+
+def _most_rows(rows: int, max_q: Optional[int]) -> int:
+    return rows if max_q is None else int(max_q)
+
+
+def tree_masks(parent, kv_len, n_seqs=1, cu_q=None, max_q=None, mask=None, q_pos=None, err_flag=None, stream=None):
+    """Tensor-level call of pkv_tree_masks: parent int32 [total_q], numbers within each sequence.  Returns (mask, q_pos),
+    allocated with torch if not given."""
+    dev = _gpu_device(parent, "parent")
+    _need(parent, "parent", dev, torch.int32, contiguous=True)
+    rows = parent.numel()
+    _need(kv_len, "kv_len", dev, torch.int32, int(n_seqs), contiguous=True)
+    _need(cu_q, "cu_q", dev, torch.int32, int(n_seqs) + 1, contiguous=True)
+    _need(q_pos, "q_pos", dev, torch.int32, rows, contiguous=True)
+    _need(err_flag, "err_flag", dev, torch.int32, 1)
+    most = _most_rows(rows, max_q)
+    if mask is None:
+        mask = torch.zeros(rows, max(1, -(-most // 32)), dtype=torch.int32, device=dev)
+        _keep_until_done(mask, stream)
+    if q_pos is None:
+        q_pos = torch.zeros(rows, dtype=torch.int32, device=dev)
+        _keep_until_done(q_pos, stream)
+    _check_mask(mask, dev, rows, most)
+    if rows == 0:   # (an empty tensor has no address to pass down)
+        return mask, q_pos
+    _check(pkv_tree_masks(parent, cu_q, kv_len, n_seqs, rows, most, mask, mask.shape[1], q_pos, err_flag, stream))
+    return mask, q_pos
+
+
+def make_draft(draft_k: torch.Tensor, draft_v: torch.Tensor, mask: Optional[torch.Tensor] = None) -> pkv_draft:
+    """The drafted rows of a tree-attention call (MLA: draft_v is draft_k)."""
+    return pkv_draft(draft_k.data_ptr(), draft_v.data_ptr(), _strides3(draft_k), _strides3(draft_v),
+                     None if mask is None else mask.data_ptr(), 0 if mask is None else mask.shape[1], 0)
+
+
+def make_tree_desc(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, out: torch.Tensor, max_kv_len: int,
+                   n_seqs: int = 1, cu_q: Optional[torch.Tensor] = None, max_q: Optional[int] = None,
+                   variant: int = PKV_ATTN_GQA, n_splits: int = 0, lse_out: Optional[torch.Tensor] = None, window: int = 0,
+                   kv_base: Optional[torch.Tensor] = None, block_table: Optional[torch.Tensor] = None,
+                   cache_slots: Optional[int] = None) -> pkv_attn_desc:
+    """Descriptor of a tree-attention call: contiguous caches [L][Hkv][slots][*], or (block_table given) pools
+    [L][page][slot][Hkv][*]."""
+    if block_table is None:
+        d = make_attn_desc(q, k_cache, v_cache, out, max_kv_len, n_seqs, cu_q, kv_base, max_q, variant, n_splits, lse_out, window)
+        if cache_slots is not None:
+            d.cache_slots = int(cache_slots)
+        return d
+    d = make_attn_desc_quant(q, k_cache, v_cache, out, block_table, max_kv_len, n_seqs, cu_q, max_q, n_splits, lse_out, window,
+                             cache_slots)
+    d.variant = int(variant)
+    return d
+
+
+def tree_attention(q, k_cache, v_cache, draft_k, draft_v, out, q_pos, kv_len, scale, max_kv_len, mask=None, n_seqs=1, cu_q=None,
+                   kv_base=None, max_q=None, variant=PKV_ATTN_GQA, n_splits=0, lse_out=None, workspace=None, stream=None,
+                   window=0, block_table=None, v_block_table=None, k_scale=None, v_scale=None, cache_slots=None) -> None:
+    """Tensor-level call of pkv_tree_attention (allocates the workspace with torch if not given).  block_table: the caches
+    are pools; k_scale and v_scale: pools of 8-bit codes.  MLA: v_cache is k_cache and draft_v is draft_k."""
+    dev = _gpu_device(q, "q")
+    for t, name in ((k_cache, "k_cache"), (v_cache, "v_cache"), (draft_k, "draft_k"), (draft_v, "draft_v"), (out, "out")):
+        if t is None:
+            raise TypeError("%s is required" % name)
+    quant = k_scale is not None or v_scale is not None
+    for t, name in ((draft_k, "draft_k"), (draft_v, "draft_v"), (out, "out")):
+        _need(t, name, dev, q.dtype)
+    if q.dim() != 4 or out.dim() != 4 or out.shape[:3] != q.shape[:3]:
+        raise ValueError("q and out are [layer][row][q_head][channel]")
+    L, rows, H, D = q.shape
+    most = _most_rows(rows, max_q)
+    _need(q_pos, "q_pos", dev, torch.int32, rows, contiguous=True)
+    _need(kv_len, "kv_len", dev, torch.int32, int(n_seqs), contiguous=True)
+    _need(cu_q, "cu_q", dev, torch.int32, int(n_seqs) + 1, contiguous=True)
+    _need(kv_base, "kv_base", dev, torch.int64, int(n_seqs), contiguous=True)
+    _need(lse_out, "lse_out", dev, torch.float32, L * rows * H, contiguous=True)
+    _need(workspace, "workspace", dev, contiguous=True)
+    _check_mask(mask, dev, rows, most)
+    if quant:
+        if block_table is None:
+            raise ValueError("a cache held in 8 bits is paged: block_table is required")
+        _check_q8_cache(dev, k_cache, v_cache, k_scale, v_scale, block_table, v_block_table, None)
+    else:
+        for t, name in ((k_cache, "k_cache"), (v_cache, "v_cache")):
+            _need(t, name, dev, q.dtype)
+    if block_table is not None:
+        _need(block_table, "block_table", dev, torch.int32, contiguous=True)
+        _need(v_block_table, "v_block_table", dev, torch.int32, contiguous=True)
+        if block_table.dim() != 2 or block_table.shape[0] < int(n_seqs):
+            raise ValueError("block_table is [n_seqs][max_pages]")
+    dim = 4 if block_table is None else 5
+    if k_cache.dim() != dim or v_cache.dim() != dim:
+        raise ValueError("caches are [layer][kv_head][slot][channel], pools [layer][page][slot][kv_head][channel]")
+    Hkv = k_cache.shape[1 if block_table is None else 3]
+    for cache, draft, width, name in ((k_cache, draft_k, D, "k"), (v_cache, draft_v, D if variant == PKV_ATTN_MLA else out.shape[3], "v")):
+        if cache.shape[0] != L or cache.shape[-1] != width:
+            raise ValueError("%s_cache %s does not fit q %s" % (name, tuple(cache.shape), tuple(q.shape)))
+        if draft.dim() != 4 or (draft.shape[0], draft.shape[1], draft.shape[3]) != (L, Hkv, width) or draft.shape[2] < rows:
+            raise ValueError("draft_%s %s must be [%d][%d][%d][%d]" % (name, tuple(draft.shape), L, Hkv, rows, width))
+    if rows == 0:   # (an empty tensor has no address to pass down)
+        return
+    desc = make_tree_desc(q, k_cache, v_cache, out, max_kv_len, n_seqs, cu_q, max_q, variant, n_splits, lse_out, window, kv_base,
+                          block_table, cache_slots)
+    need = pkv_tree_attention_workspace_size(desc, H, Hkv, D, quant)
+    if need and (workspace is None or workspace.numel() * workspace.element_size() < need):
+        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+        _keep_until_done(workspace, stream)
+    paging = None if block_table is None else make_paging(block_table, k_cache, v_cache, v_block_table)
+    scales = make_block_scales(k_scale, v_scale, k_cache.shape[2]) if quant else None
+    _check(pkv_tree_attention(q, k_cache, v_cache, out, q_pos, kv_len, H, Hkv, D, scale, desc, make_draft(draft_k, draft_v, mask),
+                              paging, scales, workspace, need, stream))
+
+
+def make_verify_desc(target_probs: torch.Tensor, draft_probs: Optional[torch.Tensor], cu_q: Optional[torch.Tensor], n_seqs: int,
+                     max_q: int, max_path: int, err_flag: Optional[torch.Tensor] = None) -> pkv_verify_desc:
+    """Descriptor of a verification of probabilities [total_q][vocab] (any row stride)."""
+    rows, vocab = target_probs.shape
+    assert target_probs.stride(1) == 1 and (draft_probs is None or draft_probs.stride(1) == 1)
+    return pkv_verify_desc(_dtype_code(target_probs), int(n_seqs), rows, int(max_q), vocab, int(max_path),
+                           None if cu_q is None else cu_q.data_ptr(), target_probs.stride(0),
+                           0 if draft_probs is None else draft_probs.stride(0),
+                           None if err_flag is None else err_flag.data_ptr(), 0)
+
+
+def tree_verify(target_probs, tokens, parent, u_accept, u_sample, max_path, draft_probs=None, n_seqs=1, cu_q=None, max_q=None,
+                path=None, n_accepted=None, next_token=None, err_flag=None, workspace=None, stream=None):
+    """Tensor-level call of pkv_tree_verify; returns (path, n_accepted, next_token), allocated with torch if not given."""
+    dev = _gpu_device(target_probs, "target_probs")
+    if target_probs.dim() != 2 or target_probs.stride(1) != 1:
+        raise ValueError("target_probs is [total_q][vocab], contiguous along the vocabulary")
+    rows = target_probs.shape[0]
+    _need(draft_probs, "draft_probs", dev, target_probs.dtype)
+    if draft_probs is not None and (draft_probs.shape != target_probs.shape or draft_probs.stride(1) != 1):
+        raise ValueError("draft_probs must have target_probs' shape and be contiguous along the vocabulary")
+    for t, name, kind, n in ((tokens, "tokens", torch.int32, rows), (parent, "parent", torch.int32, rows),
+                             (u_accept, "u_accept", torch.float32, rows), (u_sample, "u_sample", torch.float32, int(n_seqs))):
+        if t is None:
+            raise TypeError("%s is required" % name)
+        _need(t, name, dev, kind, n, contiguous=True)
+    _need(cu_q, "cu_q", dev, torch.int32, int(n_seqs) + 1, contiguous=True)
+    _need(err_flag, "err_flag", dev, torch.int32, 1)
+    _need(workspace, "workspace", dev, contiguous=True)
+    outs = []
+    for t, name, shape in ((path, "path", (int(n_seqs), int(max_path))), (n_accepted, "n_accepted", (int(n_seqs),)),
+                           (next_token, "next_token", (int(n_seqs),))):
+        if t is None:
+            t = torch.empty(shape, dtype=torch.int32, device=dev)
+            _keep_until_done(t, stream)
+        _need(t, name, dev, torch.int32, contiguous=True)
+        if tuple(t.shape) != shape:
+            raise ValueError("%s must be %s, got %s" % (name, shape, tuple(t.shape)))
+        outs.append(t)
+    if rows == 0:   # (empty tensors have no address to pass down)
+        outs[0].fill_(-1)
+        outs[1].zero_()
+        outs[2].fill_(-1)
+        return tuple(outs)
+    desc = make_verify_desc(target_probs, draft_probs, cu_q, n_seqs, _most_rows(rows, max_q), max_path, err_flag)
+    need = pkv_tree_verify_workspace_size(desc)
+    if workspace is None or workspace.numel() * workspace.element_size() < need:
+        workspace = torch.empty(max(16, need), dtype=torch.uint8, device=dev)
+        _keep_until_done(workspace, stream)
+    _check(pkv_tree_verify(target_probs, draft_probs, tokens, parent, u_accept, u_sample, *outs, desc, workspace,
+                           workspace.numel() * workspace.element_size(), stream))
+    return tuple(outs)
+
+
+def make_commit_layout(draft_k: torch.Tensor, draft_v: Optional[torch.Tensor], cache_k: torch.Tensor,
+                       cache_v: Optional[torch.Tensor], block_table: Optional[torch.Tensor] = None, slots: int = 0,
+                       err_flag: Optional[torch.Tensor] = None) -> pkv_layout:
+    """Layout of a commit of drafted rows into contiguous caches (slots: those of the tensors) or, with a block table,
+    into pools (slots: those of a sequence, 0 for all that its row of the table holds)."""
+    L = make_layout(draft_k, draft_v, draft_k, draft_v, err_flag=err_flag)
+    if block_table is None:
+        L.dst_capacity = int(slots)
+        L.dst_k_stride, L.dst_v_stride = _strides3(cache_k), _strides3(cache_v)
+    else:
+        L.dst_capacity = int(slots) or block_table.shape[1] * cache_k.shape[2]
+        L.dst_k_stride, L.dst_v_stride = pool_strides3(cache_k), pool_strides3(cache_v)
+    return L
+
+
+def tree_commit(draft_k, draft_v, cache_k, cache_v, path, n_accepted, kv_len, kv_base=None, block_table=None, v_block_table=None,
+                k_scale=None, v_scale=None, slots=None, err_flag=None, workspace=None, stream=None) -> None:
+    """Tensor-level call of pkv_tree_commit (path int32 [n_seqs][max_path]); values may be None (MLA)."""
+    dev = _gpu_device(draft_k, "draft_k")
+    quant = k_scale is not None or v_scale is not None
+    _need(path, "path", dev, torch.int32, contiguous=True)
+    if path.dim() != 2:
+        raise ValueError("path is [n_seqs][max_path]")
+    n_seqs, max_path = path.shape
+    for t, name in ((n_accepted, "n_accepted"), (kv_len, "kv_len")):
+        if t is None:
+            raise TypeError("%s is required" % name)
+        _need(t, name, dev, torch.int32, n_seqs, contiguous=True)
+    _need(kv_base, "kv_base", dev, torch.int64, n_seqs, contiguous=True)
+    _need(err_flag, "err_flag", dev, torch.int32, 1)
+    _need(workspace, "workspace", dev, contiguous=True)
+    if cache_k is None:
+        raise TypeError("cache_k is required")
+    if (draft_v is None) != (cache_v is None):
+        raise ValueError("draft_v and cache_v are given both or not at all")
+    if quant:
+        if block_table is None:
+            raise ValueError("a cache held in 8 bits is paged: block_table is required")
+        _check_q8_cache(dev, cache_k, cache_v, k_scale, v_scale, block_table, v_block_table, None)
+        _need(draft_v, "draft_v", dev, draft_k.dtype)
+    else:
+        for t, name in ((draft_v, "draft_v"), (cache_k, "cache_k"), (cache_v, "cache_v")):
+            _need(t, name, dev, draft_k.dtype)
+    if block_table is not None:
+        _need(block_table, "block_table", dev, torch.int32, contiguous=True)
+        _need(v_block_table, "v_block_table", dev, torch.int32, contiguous=True)
+        if block_table.dim() != 2 or block_table.shape[0] < n_seqs:
+            raise ValueError("block_table is [n_seqs][max_pages]")
+    dim, heads = (4, 1) if block_table is None else (5, 3)
+    for draft, cache, name in ((draft_k, cache_k, "k"), (draft_v, cache_v, "v")):
+        if draft is None:
+            continue
+        if draft.dim() != 4 or cache.dim() != dim or draft.shape[:2] != draft_k.shape[:2] or draft.shape[2] != draft_k.shape[2] \
+                or (draft.shape[0], draft.shape[1], draft.shape[3]) != (cache.shape[0], cache.shape[heads], cache.shape[-1]):
+            raise ValueError("draft_%s %s does not fit cache_%s %s" % (name, tuple(draft.shape), name, tuple(cache.shape)))
+    if slots is None:
+        slots = cache_k.shape[2] if block_table is None else 0
+    layout = make_commit_layout(draft_k, draft_v, cache_k, cache_v, block_table, slots, err_flag)
+    need = pkv_tree_commit_workspace_size(n_seqs, max_path, quant)
+    if need and (workspace is None or workspace.numel() * workspace.element_size() < need):
+        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+        _keep_until_done(workspace, stream)
+    paging = None if block_table is None else make_paging(block_table, cache_k, cache_v, v_block_table)
+    scales = make_block_scales(k_scale, v_scale, cache_k.shape[2]) if quant else None
+    _check(pkv_tree_commit(draft_k, draft_v, cache_k, cache_v, path, n_accepted, kv_len, kv_base, n_seqs, max_path, layout, paging,
+                           scales, workspace, need, stream))
