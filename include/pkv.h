@@ -548,7 +548,8 @@ pkv_status pkv_tree_masks(const int32_t* parent, const int32_t* cu_q, const int3
 typedef struct pkv_draft {
     const void* k;             /* device [layer][kv_head][row][head_dim] */
     const void* v;             /* device [layer][kv_head][row][head_dim_v]; MLA: equal to k, with its strides */
-    int64_t k_stride[3];       /* {layer, head, row}, elements, non-negative, multiples of 16 bytes */
+    int64_t k_stride[3];       /* {layer, head, row}, elements, non-negative, multiples of 16 bytes; rows at
+                                  most 64 MiB apart */
     int64_t v_stride[3];
     const uint32_t* mask;      /* device [total_q][mask_words], as pkv_tree_masks writes it or any other bits;
                                   NULL: every row sees the rows of its sequence up to itself (a chain) */

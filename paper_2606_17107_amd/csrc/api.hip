@@ -509,6 +509,9 @@ pkv_status check_draft(const pkv_draft* t, const void* out, const pkv::AttnArgs&
         if ((t->k_stride[i] * eb) % 16 || (t->v_stride[i] * eb) % 16)
             return fail(PKV_ERR_ALIGN, "strides must be multiples of 16 bytes");
     }
+    constexpr int64_t kMaxRowBytes = (int64_t)1 << 26;   // as slot strides: rows by 32-bit strides
+    if (t->k_stride[2] > kMaxRowBytes / eb || t->v_stride[2] > kMaxRowBytes / eb)
+        return fail(PKV_ERR_SHAPE, "row strides of drafted rows exceed 64 MiB");
     if (a.variant == PKV_ATTN_MLA && (t->v != t->k || memcmp(t->v_stride, t->k_stride, sizeof t->k_stride) != 0))
         return fail(PKV_ERR_SHAPE, "MLA reads values from the latent channels: draft.v must be draft.k with the same strides");
     if (t->mask && (t->mask_words <= 0 || t->mask_words < (a.max_q + 31) / 32))

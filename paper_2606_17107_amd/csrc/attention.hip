@@ -4,7 +4,7 @@
 // The bf16 GQA kernel lives in attn_gqa_bf16.hip.
 #include <algorithm>
 
-#include "attn_columns.h"
+#include "attn_pieces.h"
 
 namespace pkv {
 
@@ -536,8 +536,9 @@ __global__ __launch_bounds__(256) void attn_combine(AttnArgs a, int seq0) {
         a.lse_out[item] = row_lse2(mx, wsum) * kLn2;
 }
 
-// rows: rows per workgroup, 0 for the dtype's usual count.
-Plan make_plan(const AttnArgs& a, int splits, int rows = 0) {
+// rows: rows per workgroup, 0 for the dtype's usual count.  pieces: of all sequences
+// together (attn_pieces.h), at most `splits` each; 0: `splits` of each.
+Plan make_plan(const AttnArgs& a, int splits, int rows = 0, int pieces = 0) {
     Plan p;
     p.G = a.n_heads / a.n_kv_heads;
     const int64_t m_rows = (int64_t)a.max_q * p.G;
@@ -559,7 +560,8 @@ Plan make_plan(const AttnArgs& a, int splits, int rows = 0) {
     if (p.rbs < 1) p.rbs = 1;
     p.splits = splits;
     p.direct = splits == 1 && !a.partials;
-    p.n_groups = a.n_layers * a.n_kv_heads * a.n_seqs * splits;
+    p.pieces = pieces;
+    p.n_groups = a.n_layers * a.n_kv_heads * (pieces ? pieces : a.n_seqs * splits);
     p.longest_first = 0;
     // Row blocks on the fullest XCD when a group is shared by 1, 2, 4 or 8 XCDs;
     // one XCD (every K/V byte through one L2) unless sharing fills them better:
@@ -660,9 +662,48 @@ bool col_route(const AttnArgs& a) {
     return col_items(a) * ((int64_t)a.max_kv_len / kColTile + (a.dtype == 2 ? 32 : 16)) < 0x7fffffff;
 }
 
+// ---- pieces (attn_pieces.h) ----------------------------------------------------
+
+bool piece_route(const AttnArgs& a) {
+    return a.partials && a.auto_splits && a.dtype != 1 && a.n_seqs <= kColMaxSeqs && !col_route(a);
+}
+
+struct PieceCut {
+    int pieces;    // of all sequences together
+    int records;   // most of one sequence
+};
+
+// As many pieces as there are workgroup slots, but no more of a sequence than pay: a
+// piece shortens the longest run of tiles, and adds a record of every row that is
+// written and read back (measured at 4 TB/s).  One sequence of 2000 keys, 32 rows, 32
+// heads over 8 KV heads of 128: 32 pieces 20.0 us, 16 pieces 17.5, 8 pieces 19.1; 8000
+// keys: 32 pieces 24.5, 16 pieces 26.5; MLA, 16 sequences of 8 rows and 1000..4000 keys:
+// 16 on average 54.9 us, 8 47.5.  More sequences than half the slots are cut in two on
+// average while that leaves 32 tiles, which evens out their lengths over two rounds.
+PieceCut piece_cut(const AttnArgs& a) {
+    const Plan p = make_plan(a, 1);
+    const int64_t slots = kCUs * (int64_t)wgs_per_cu(a, p), seqs = a.n_seqs;
+    const int64_t tiles = std::max<int64_t>(1, (seen_keys(a) + kColTile - 1) / kColTile);
+    const double tile = a.variant == 1 ? 2.2e-6 : a.dtype == 2 ? 1.0e-6 : a.head_dim == 128 ? 0.8e-6 : 0.45e-6;
+    const double record = (double)a.n_layers * a.total_q * a.n_heads * (a.head_dim_v + 1) * 4.0 * 2.0 / 4e12;
+    int64_t each = 1;
+    for (int64_t n = 2; n <= 32 && n * kPieceTiles <= tiles + kPieceTiles - 1; ++n)
+        if (n * record + tiles * tile / n < each * record + tiles * tile / each) each = n;
+    // Row blocks of one piece and KV head go to one XCD (decode): what its CUs hold at once.
+    const int64_t per_xcd = slots / kXcds / p.rbs;
+    const int64_t groups = per_xcd > 0 ? per_xcd * kXcds : std::max<int64_t>(1, slots / p.rbs);
+    int64_t pieces = groups / ((int64_t)a.n_layers * a.n_kv_heads);
+    if (pieces < 2 * seqs) pieces = tiles >= 32 ? 2 * seqs : std::max(pieces, seqs);
+    pieces = std::min(pieces, seqs * each);
+    int64_t records = seqs == 1 ? pieces : std::min(2 * ((pieces + seqs - 1) / seqs) + 2, pieces - seqs + 1);
+    records = std::min<int64_t>(records, 32);
+    return {(int)std::min(pieces, seqs * records), (int)records};
+}
+
 }  // namespace
 
 int attention_splits(const AttnArgs& a) {
+    if (a.n_splits == 0 && piece_route(a)) return piece_cut(a).records;
     if (a.n_splits == 0 && col_route(a)) {
         // Columns have records for twice the pieces that sequences of one length
         // would be cut into (a sequence longer than that makes the columns longer).
@@ -795,7 +836,7 @@ hipError_t launch_columns(const AttnArgs& a, const BlockScales* scales, hipStrea
 
 hipError_t launch_attention(const AttnArgs& a, const BlockScales* scales, hipStream_t stream) {
     if (col_route(a)) return launch_columns(a, scales, stream);
-    Plan p = make_plan(a, a.n_splits < 1 ? 1 : a.n_splits);
+    Plan p = make_plan(a, a.n_splits < 1 ? 1 : a.n_splits, 0, piece_route(a) ? piece_cut(a).pieces : 0);
     // fp32 calls of at most one workgroup of 32 rows per CU split the keys over
     // its waves.
     const bool keys = a.dtype == 1 && (int64_t)p.n_groups * (((int64_t)a.max_q * p.G + 31) / 32) <= kCUs;

@@ -31,11 +31,12 @@ struct Plan {
     int G;          // query heads per KV head
     int BM;         // rows per workgroup
     int rbs;        // row blocks per group
-    int n_groups;   // layers x kv heads x sequences x splits
+    int n_groups;   // layers x kv heads x (sequences x splits, or pieces)
     int shares, share_rbs;   // XCDs that share a group, row blocks of one share
     int splits;     // each workgroup's key range is shared by this many splits in equal runs of whole tiles
     int direct;     // rows are finished here (one split, and nothing joins them later)
     int longest_first;   // sequences are dispatched longest first
+    int pieces;     // > 0: the sequences share this many pieces by their lengths (attn_pieces.h), at most `splits` each
     int qb, nw, ns; // bf16 GQA kernel shape: 32-row blocks per wave, waves, LDS stages
 };
 

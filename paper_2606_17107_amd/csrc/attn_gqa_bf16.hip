@@ -29,6 +29,7 @@
 #include <type_traits>
 
 #include "attn_gqa_tile.h"
+#include "attn_pieces.h"
 #include "attn_gqa_tile_q8.h"
 
 namespace pkv {
@@ -46,7 +47,8 @@ constexpr int kAhead = 3;    // LDS operand reads issued this many operands ahea
 // their own, since an option costs a one-round call up to 0.5 us by being there).
 // kFull: every row block but the last of a sequence is full.  kFew: no sequence
 // fills its one row block.  kOrdered: sequences are dispatched longest first.
-enum { kFull, kFew, kOrdered };
+// kPieces: sequences are cut by their lengths.
+enum { kFull, kFew, kOrdered, kPieces };
 template <int D, bool PAGED, int FORM, bool Q8>
 __global__ __launch_bounds__(kWaves * 64, 2) void attn_gqa_bf16_kernel(AttnArgs a, Plan p, ScaleArg<Q8> sa) {
     static_assert(PAGED || !Q8, "a cache held in 8 bits is paged");
@@ -80,14 +82,25 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_gqa_bf16_kernel(AttnArgs 
 
     int group, rb;
     if (!decode(p, group, rb)) return;
-    const int split = group % p.splits;
-    int rest = group / p.splits;
+    const int cuts = FORM == kPieces ? p.pieces : p.splits;
+    int split = group % cuts, n_split = p.splits;
+    int rest = group / cuts;
     const int kvh = rest % a.n_kv_heads;
     rest /= a.n_kv_heads;
     const int layer = rest % a.n_layers;
     int seq = rest / a.n_layers;
     if constexpr (FORM == kOrdered) seq = longest_seq(a, seq);
-    const SeqInfo si = seq_info(a, seq);
+    SeqInfo si;
+    if constexpr (FORM == kPieces) {
+        const PieceOf piece = piece_of(a, p, split);
+        if (piece.count == 0) return;
+        seq = piece.seq;
+        split = piece.index;
+        n_split = piece.count;
+        si = piece.si;
+    } else {
+        si = seq_info(a, seq);
+    }
     const int M = si.nq * p.G;
     const int m0 = rb * (NW * 32 * QB);
     if (m0 >= M) return;
@@ -174,7 +187,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_gqa_bf16_kernel(AttnArgs 
     // skipped); the splits share them in equal runs of whole tiles.
     const int lo = s_min == 0x7fffffff ? 0 : s_min / BN * BN;
     const int hi = min(si.kvl, e_max);
-    const int run = hi > lo ? ((hi - lo + p.splits - 1) / p.splits + BN - 1) / BN * BN : 0;
+    const int run = hi > lo ? ((hi - lo + n_split - 1) / n_split + BN - 1) / BN * BN : 0;
     const int k_begin = lo + split * run;
     const int loop_end = min(hi, k_begin + run);
     const int n_tiles = loop_end > k_begin ? (loop_end - k_begin + BN - 1) / BN : 0;
@@ -892,6 +905,10 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_gqa_bf16_kernel(AttnArgs 
                 }
             }
             if (hl == 0) a.ws_lse[item] = lse2;
+            if (FORM == kPieces && hl == 0 && split == n_split - 1) {   // records beyond the pieces weigh nothing
+                const int64_t items = (int64_t)a.n_layers * a.total_q * a.n_heads;
+                for (int k = 1; k < p.splits - split; ++k) a.ws_lse[item + k * items] = -INFINITY;
+            }
         }
     }
 }
@@ -900,7 +917,9 @@ template <int D, bool PAGED, bool Q8>
 hipError_t launch_d(const AttnArgs& a, const Plan& p, const ScaleArg<Q8>& sa, dim3 grid, hipStream_t stream) {
     if (p.nw != kWaves || p.qb != kQB || p.ns != kStages) return hipErrorInvalidValue;
     const dim3 block(kWaves * 64);
-    if (p.longest_first)
+    if (p.pieces)
+        hipLaunchKernelGGL((attn_gqa_bf16_kernel<D, PAGED, kPieces, Q8>), grid, block, 0, stream, a, p, sa);
+    else if (p.longest_first)
         hipLaunchKernelGGL((attn_gqa_bf16_kernel<D, PAGED, kOrdered, Q8>), grid, block, 0, stream, a, p, sa);
     else if ((int64_t)a.max_q * p.G < p.BM)
         hipLaunchKernelGGL((attn_gqa_bf16_kernel<D, PAGED, kFew, Q8>), grid, block, 0, stream, a, p, sa);

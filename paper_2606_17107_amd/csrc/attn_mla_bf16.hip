@@ -43,6 +43,7 @@
 #include <type_traits>
 
 #include "attn_mla_tile.h"
+#include "attn_pieces.h"
 
 namespace pkv {
 namespace {
@@ -51,7 +52,8 @@ constexpr int kMlaWaves = 4;    // 32 rows per wave, 128 per workgroup
 constexpr int kMlaStages = 2;   // LDS stages of 32-key tiles
 constexpr int kMlaAhead = 2;    // LDS operand reads issued this many operands ahead of their MFMA
 
-template <bool PAGED>
+// PIECES: sequences are cut by their lengths (attn_pieces.h).
+template <bool PAGED, bool PIECES>
 __global__ __launch_bounds__(kMlaWaves * 64, 1) void attn_mla_bf16_kernel(AttnArgs a, Plan p) {
     constexpr int NS = kMlaStages, NW = kMlaWaves;
     constexpr int NBLK = MBN * MCH / 64;       // 64-lane LDS-DMA blocks per tile: 36
@@ -69,11 +71,22 @@ __global__ __launch_bounds__(kMlaWaves * 64, 1) void attn_mla_bf16_kernel(AttnAr
 
     int group, rb;
     if (!decode(p, group, rb)) return;
-    const int split = group % p.splits;
-    int rest = group / p.splits;   // one KV head
+    const int cuts = PIECES ? p.pieces : p.splits;
+    int split = group % cuts, n_split = p.splits;
+    int rest = group / cuts;   // one KV head
     const int layer = rest % a.n_layers;
-    const int seq = rest / a.n_layers;
-    const SeqInfo si = seq_info(a, seq);
+    int seq = rest / a.n_layers;
+    SeqInfo si;
+    if constexpr (PIECES) {
+        const PieceOf piece = piece_of(a, p, split);
+        if (piece.count == 0) return;
+        seq = piece.seq;
+        split = piece.index;
+        n_split = piece.count;
+        si = piece.si;
+    } else {
+        si = seq_info(a, seq);
+    }
     const int H = a.n_heads;
     const int M = si.nq * H;
     const int m0 = rb * RPW;
@@ -128,7 +141,7 @@ __global__ __launch_bounds__(kMlaWaves * 64, 1) void attn_mla_bf16_kernel(AttnAr
     // whole tiles.
     const int lo = s_min == 0x7fffffff ? 0 : s_min / MBN * MBN;
     const int hi = min(si.kvl, e_max);
-    const int run = hi > lo ? ((hi - lo + p.splits - 1) / p.splits + MBN - 1) / MBN * MBN : 0;
+    const int run = hi > lo ? ((hi - lo + n_split - 1) / n_split + MBN - 1) / MBN * MBN : 0;
     const int k_begin = lo + split * run;
     const int loop_end = min(hi, k_begin + run);
     const int n_tiles = loop_end > k_begin ? (loop_end - k_begin + MBN - 1) / MBN : 0;
@@ -423,6 +436,10 @@ __global__ __launch_bounds__(kMlaWaves * 64, 1) void attn_mla_bf16_kernel(AttnAr
             }
         }
         if (hl == 0) a.ws_lse[item] = lse2;
+        if (PIECES && hl == 0 && split == n_split - 1) {   // records beyond the pieces weigh nothing
+            const int64_t items = (int64_t)a.n_layers * a.total_q * H;
+            for (int k = 1; k < p.splits - split; ++k) a.ws_lse[item + k * items] = -INFINITY;
+        }
     }
 }
 
@@ -430,10 +447,15 @@ __global__ __launch_bounds__(kMlaWaves * 64, 1) void attn_mla_bf16_kernel(AttnAr
 
 hipError_t launch_attn_mla_bf16(const AttnArgs& a, const Plan& p, dim3 grid, hipStream_t stream) {
     if (p.nw != kMlaWaves || p.ns != kMlaStages || p.BM != kMlaWaves * 32) return hipErrorInvalidValue;
-    if (a.block_table)
-        hipLaunchKernelGGL((attn_mla_bf16_kernel<true>), grid, dim3(kMlaWaves * 64), 0, stream, a, p);
+    const dim3 block(kMlaWaves * 64);
+    if (a.block_table && p.pieces)
+        hipLaunchKernelGGL((attn_mla_bf16_kernel<true, true>), grid, block, 0, stream, a, p);
+    else if (a.block_table)
+        hipLaunchKernelGGL((attn_mla_bf16_kernel<true, false>), grid, block, 0, stream, a, p);
+    else if (p.pieces)
+        hipLaunchKernelGGL((attn_mla_bf16_kernel<false, true>), grid, block, 0, stream, a, p);
     else
-        hipLaunchKernelGGL((attn_mla_bf16_kernel<false>), grid, dim3(kMlaWaves * 64), 0, stream, a, p);
+        hipLaunchKernelGGL((attn_mla_bf16_kernel<false, false>), grid, block, 0, stream, a, p);
     return hipGetLastError();
 }
 

@@ -8,202 +8,355 @@
 // drafted rows by one running softmax: a partial enters like a key whose score is its
 // log-sum-exp, with the partial's output in the place of a value.
 //
-// A tree's row sees few drafted rows (its depth, not the size of the tree), so a wave
-// goes through the set bits of the row's mask and loads only those keys and values:
-// scores, sums and outputs stay in fp32 registers.  Head sizes 64 and 128: CH = D/8
-// lanes share a key, 64 / CH keys (or partials) are in work at once, merged at the end.
-// Latent rows (576 channels): the whole wave shares a key, whose first 512 channels are
-// its value.  A wave holds HB heads of one KV head, so a key is loaded once for them.
-#include "attn_common.h"
+// A tree's row sees few drafted rows (its depth, not the size of the tree), so a wave,
+// which holds one row of one head, lists the set bits of the row's mask and loads only
+// those keys and values: scores, sums and outputs stay in fp32 registers.  Head sizes
+// 64 and 128: CH = D/8 lanes share a key (or a partial), KG = 64 / CH groups of lanes
+// take U keys each at a time, and are merged at the end.  Latent rows (576 channels):
+// the whole wave shares a key, whose first 512 channels are its value.
+// The step is a chain of memory round trips (bounds; log-sum-exps, mask and query;
+// partials, keys and values), so what does not depend on each other is asked for together.
+#include "attn_columns.h"
 
 namespace pkv {
 namespace {
 
 constexpr int kJoinWaves = 4;
+constexpr int kJoinKeys = 2;
 
+// Eight values as they lie in memory, and as floats.
 template <typename T>
-__device__ __forceinline__ void load8(const T* p, float (&x)[8]);
+struct Raw8;
 template <>
-__device__ __forceinline__ void load8<float>(const float* p, float (&x)[8]) {
-    const f32x4 a = *(const f32x4*)p, b = *(const f32x4*)(p + 4);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        x[e] = a[e];
-        x[4 + e] = b[e];
+struct Raw8<float> {
+    f32x4 a, b;
+    __device__ __forceinline__ void load(const char* p) {
+        a = *(const f32x4*)p;
+        b = *(const f32x4*)(p + 16);
     }
-}
+    __device__ __forceinline__ void get(float (&x)[8]) const {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            x[e] = a[e];
+            x[4 + e] = b[e];
+        }
+    }
+};
 template <>
-__device__ __forceinline__ void load8<uint16_t>(const uint16_t* p, float (&x)[8]) {
-    const u32x4 a = *(const u32x4*)p;
+struct Raw8<uint16_t> {
+    u32x4 a;
+    __device__ __forceinline__ void load(const char* p) { a = *(const u32x4*)p; }
+    __device__ __forceinline__ void get(float (&x)[8]) const {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        x[2 * e] = __uint_as_float(a[e] << 16);
-        x[2 * e + 1] = __uint_as_float(a[e] & 0xffff0000u);
+        for (int e = 0; e < 4; ++e) {
+            x[2 * e] = __uint_as_float(a[e] << 16);
+            x[2 * e + 1] = __uint_as_float(a[e] & 0xffff0000u);
+        }
     }
-}
+};
 __device__ __forceinline__ float load1(const float* p) { return *p; }
 __device__ __forceinline__ float load1(const uint16_t* p) { return __uint_as_float((uint32_t)*p << 16); }
 
-// One entry with weight 2^s (s > -inf, or NaN) and value x joins the sums.  A NaN or
-// +inf score makes the sum NaN, which stays NaN.
-__device__ __forceinline__ void join_entry(float s, const float (&x)[8], float& m, float& l, float (&acc)[8]) {
-    const float m_new = fmaxf(m, s);
-    const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - m_new);
-    const float w = __builtin_amdgcn_exp2f(s - m_new);
-    l = l * keep + w;
+// Sum over the CH lanes that share a key, the same in each of them.
+template <int CTRL>
+__device__ __forceinline__ float dpp_add(float v) {
+    return v + __uint_as_float((uint32_t)dpp<CTRL>(0, (int)__float_as_uint(v)));
+}
+template <int CH>
+__device__ __forceinline__ float group_sum(float v) {
+    if constexpr (CH == 8) {
+        constexpr int kSwap1 = 0xb1, kSwap2 = 0x4e, kHalfMirror = 0x141;   // quad_perm [1,0,3,2], [2,3,0,1]; lane 7 - i of 8
+        return dpp_add<kHalfMirror>(dpp_add<kSwap2>(dpp_add<kSwap1>(v)));
+    } else {
+        v = dpp_add<kDppRor + 1>(dpp_add<kDppRor + 2>(dpp_add<kDppRor + 4>(dpp_add<kDppRor + 8>(v))));
+        if constexpr (CH == 16) return v;
+        float r[4];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) acc[e] = acc[e] * keep + w * x[e];
-    m = m_new;
+        for (int k = 0; k < 4; ++k) r[k] = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v), 16 * k));
+        return (r[0] + r[1]) + (r[2] + r[3]);
+    }
+}
+__device__ __forceinline__ float lane_value(float v, int lane) {
+    return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v), lane));
+}
+template <int CTRL>
+__device__ __forceinline__ float dpp_max(float v) {
+    return fmaxf(v, __uint_as_float((uint32_t)dpp<CTRL>((int)__float_as_uint(v), (int)__float_as_uint(v))));
+}
+__device__ __forceinline__ float wave_max_f(float v) {   // a NaN counts for nothing
+    v = dpp_max<kDppRor + 1>(dpp_max<kDppRor + 2>(dpp_max<kDppRor + 4>(dpp_max<kDppRor + 8>(v))));
+    return fmaxf(fmaxf(lane_value(v, 0), lane_value(v, 16)), fmaxf(lane_value(v, 32), lane_value(v, 48)));
+}
+// v of this lane and of the one in the other half (32) or the neighbouring row of 16 lanes.
+template <int W>
+__device__ __forceinline__ void both(float v, float& x, float& y) {
+    const uint32_t u = __float_as_uint(v);
+    const auto r = W == 32 ? __builtin_amdgcn_permlane32_swap(u, u, false, false) : __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    x = __uint_as_float(r[0]);
+    y = __uint_as_float(r[1]);
+}
+// Sums over the same two lanes: of v in the lower, of w in the upper one.
+template <int W>
+__device__ __forceinline__ float scatter_sum(float v, float w) {
+    const uint32_t a = __float_as_uint(v), b = __float_as_uint(w);
+    const auto r = W == 32 ? __builtin_amdgcn_permlane32_swap(a, b, false, false) : __builtin_amdgcn_permlane16_swap(a, b, false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-template <typename T, int D, int HB>
+template <typename T, int D>
 __global__ __launch_bounds__(kJoinWaves * 64) void tree_join(AttnArgs a, DraftArgs d, int seq0) {
     constexpr bool MLA = D == 576;
     constexpr int DV = MLA ? 512 : D;
     constexpr int CH = DV / 8;          // lanes per key
-    constexpr int KG = 64 / CH;         // keys in work at once
+    constexpr int KG = 64 / CH;         // groups of lanes
+    constexpr int U = kJoinKeys;        // keys (partials) of a group at a time
+    // The arguments of the set-up are asked for together, not one round trip after another.
+    asm volatile("" ::"s"(a.cu_q), "s"(a.total_q), "s"(a.max_q), "s"(a.n_heads), "s"(a.n_kv_heads), "s"(a.n_layers), "s"(a.n_splits),
+                 "s"(a.ws_lse), "s"(a.ws_o), "s"(a.q), "s"(a.q_stride[0]), "s"(a.q_stride[1]), "s"(a.q_stride[2]), "s"(a.window));
+    asm volatile("" ::"s"(d.mask), "s"(d.mask_words), "s"(d.k), "s"(d.v), "s"(d.k_stride[0]), "s"(d.k_stride[1]), "s"(d.k_stride[2]),
+                 "s"(d.v_stride[0]), "s"(d.v_stride[1]), "s"(d.v_stride[2]), "s"(a.scale));
     const int lane = threadIdx.x & 63;
     const int kg = lane / CH, c = lane % CH;
-    const int G = a.n_heads / a.n_kv_heads;
-    const int blocks = (G + HB - 1) / HB;              // waves per row and KV head
-    const int64_t unit = (int64_t)blockIdx.x * kJoinWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int per_row = blocks * a.n_kv_heads;
-    const int i = (int)(unit / per_row);
-    const int rest = (int)(unit - (int64_t)i * per_row);
-    const int kvh = rest / blocks;
-    const int h0 = (rest - kvh * blocks) * HB;          // first head within the KV head
+    const uint32_t unit = blockIdx.x * kJoinWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int i = (int)(unit / (uint32_t)a.n_heads), head = (int)(unit - (uint32_t)i * (uint32_t)a.n_heads);
     const int seq = seq0 + (int)blockIdx.y;
     const int layer = (int)blockIdx.z;
-    const SeqInfo si = seq_info(a, seq);
-    if (i >= si.nq || i >= a.max_q) return;
-    const int64_t row = si.q0 + i;
-    const int64_t items = (int64_t)a.n_layers * a.total_q * a.n_heads;
-    const int64_t item0 = ((int64_t)layer * a.total_q + row) * a.n_heads + kvh * G + h0;
-
-    float m[HB], l[HB], acc[HB][8];
-#pragma unroll
-    for (int h = 0; h < HB; ++h) {
-        m[h] = -INFINITY;
-        l[h] = 0.f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) acc[h][e] = 0.f;
+    int q0 = 0, nq = a.total_q;
+    if (a.cu_q) {
+        q0 = a.cu_q[seq];
+        nq = a.cu_q[seq + 1] - q0;
     }
+    if (q0 < 0 || nq < 0 || (int64_t)q0 + nq > a.total_q) nq = 0;   // as seq_info
+    if (i >= nq || i >= a.max_q) return;
+    const int kvh = head / (a.n_heads / a.n_kv_heads);
+    const int64_t row = q0 + i;
+    const int64_t items = (int64_t)a.n_layers * a.total_q * a.n_heads;
+    const int64_t item = ((int64_t)layer * a.total_q + row) * a.n_heads + head;
 
-    // The cache's partials.
+    // The first records' log-sum-exps, one a lane; the query; 64 columns of the mask, one a lane.
     const int ns = a.n_splits;
+    float lse = lane < ns ? a.ws_lse[lane * items + item] : -INFINITY;
+    const char* const qrow = (const char*)((const T*)a.q + (int64_t)layer * a.q_stride[0] + row * a.q_stride[1] + (int64_t)head * a.q_stride[2]);
+    Raw8<T> q_raw;
+    q_raw.load(qrow + c * (8 * sizeof(T)));
+    const float q_rope = MLA ? load1((const T*)qrow + 512 + c) : 0.f;
+    const int64_t pos = a.window > 0 ? a.q_pos[row] : 0;
+    auto columns = [&](int b) __attribute__((always_inline)) -> uint64_t {   // columns 64 b .. of the row's mask
+        const int col = b * 64 + lane;
+        bool seen = col < nq;                                                 // no rows behind the sequence
+        if (d.mask) {
+            const int w = col >> 5;
+            const uint32_t word = w < d.mask_words ? d.mask[row * d.mask_words + w] : 0u;
+            seen = seen && ((word >> (col & 31)) & 1);
+        } else {
+            seen = seen && col <= i;
+        }
+        if (a.window > 0 && seen) seen = a.q_pos[q0 + col] > pos - a.window;
+        return __builtin_amdgcn_ballot_w64(seen);
+    };
+    uint64_t seen = columns(0);
+
+    constexpr int EB = sizeof(T);
+    const char* const k0 = (const char*)d.k + ((int64_t)layer * d.k_stride[0] + (int64_t)kvh * d.k_stride[1] + q0 * d.k_stride[2]) * EB;
+    const char* const v0 = (const char*)d.v + ((int64_t)layer * d.v_stride[0] + (int64_t)kvh * d.v_stride[1] + q0 * d.v_stride[2]) * EB;
+    const uint32_t k_row = (uint32_t)d.k_stride[2] * EB, v_row = (uint32_t)d.v_stride[2] * EB;   // (64 MiB at most)
+    const float sc2 = a.scale * kLog2e;
+    // The places of the set bits: entry x in lane x.  (Lanes without a bit send theirs behind.)
+    auto list_of = [&](uint64_t bits) __attribute__((always_inline)) {
+        const int rank = __builtin_amdgcn_mbcnt_hi((uint32_t)(bits >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)bits, 0));
+        const int to = (bits >> lane) & 1 ? rank : __builtin_popcountll(bits) + lane - rank;
+        return __builtin_amdgcn_ds_permute(to * 4, lane);
+    };
+    auto entry = [&](int list, int x) __attribute__((always_inline)) {
+        return KG == 1 ? __builtin_amdgcn_readlane(list, x & 63) : __builtin_amdgcn_ds_bpermute(x * 4, list);
+    };
+    // Entries x0 + KG u + kg of a list, u < U, in each group of lanes.  Behind the list's
+    // end its last entry is loaded again (and weighs nothing); a u of which no group has an entry is left out.
+    Raw8<T> k_raw[U], v_raw[U];
+    float k_rope[U];
+    auto load_keys = [&](int list, int count, int b, int x0) __attribute__((always_inline)) {
 #pragma unroll
-    for (int h = 0; h < HB; ++h) {
-        if (h0 + h >= G) continue;
-        for (int s = kg; s < ns; s += KG) {
-            const int64_t item = s * items + item0 + h;
-            const float lse = a.ws_lse[item];
-            if (lse == -INFINITY) continue;
-            float x[8];
-            load8<float>(a.ws_o + item * DV + c * 8, x);
-            join_entry(lse, x, m[h], l[h], acc[h]);
+        for (int u = 0; u < U; ++u) {
+            if (x0 + u * KG < count) {   // uniform
+                const uint32_t r = b * 64 + entry(list, min(x0 + u * KG + kg, count - 1));
+                const char* const k = k0 + (uint64_t)r * k_row;
+                k_raw[u].load(k + c * (8 * EB));
+                if constexpr (MLA) k_rope[u] = load1((const T*)k + 512 + c);
+                else v_raw[u].load(v0 + (uint64_t)r * v_row + c * (8 * EB));
+            }
+        }
+    };
+    int list = list_of(seen), count = __builtin_popcountll(seen);
+
+    // The cache's partials: weights relative to the largest of 64 records, each group of
+    // lanes sums its share.  A NaN log-sum-exp makes the sum NaN, and so the row.
+    float m = -INFINITY, l = 0.f, acc[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc[e] = 0.f;
+    const uint64_t rec_bytes = (uint64_t)items * (DV * 4);
+    int recs, n_recs;        // records with a weight (a list), how many, and the weights by record
+    float w;
+    auto weigh = [&](float lse) __attribute__((always_inline)) {
+        const uint64_t used = __builtin_amdgcn_ballot_w64(lse != -INFINITY);
+        recs = list_of(used);
+        n_recs = __builtin_popcountll(used);
+        const float m_new = fmaxf(m, wave_max_f(lse));
+        w = lse == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(lse - m_new);
+        return m_new;
+    };
+    Raw8<float> x[U];
+    float wu[U];
+    auto load_records = [&](int s0, int x0) __attribute__((always_inline)) {
+        const char* const o0 = (const char*)(a.ws_o + (s0 * items + item) * DV + c * 8);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (x0 + u * KG < n_recs) {
+                const int at = x0 + u * KG + kg;
+                const int rec = entry(recs, min(at, n_recs - 1));
+                const float weight = __uint_as_float((uint32_t)entry((int)__float_as_uint(w), rec));
+                wu[u] = at < n_recs ? weight : 0.f;
+                x[u].load(o0 + (uint32_t)rec * rec_bytes);
+            }
+        }
+    };
+    auto add_records = [&](int x0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (x0 + u * KG < n_recs) {
+                const bool in = x0 + u * KG + kg < n_recs;
+                float v[8];
+                x[u].get(v);
+                l += wu[u];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) acc[e] = fmaf(wu[u], in ? v[e] : 0.f, acc[e]);
+            }
+        }
+    };
+    m = weigh(lse);
+    load_records(0, 0);
+    load_keys(list, count, 0, 0);
+    add_records(0);
+    for (int x0 = KG * U; x0 < n_recs; x0 += KG * U) {
+        load_records(0, x0);
+        add_records(x0);
+    }
+    for (int s0 = 64; s0 < ns; s0 += 64) {   // (many splits, by the caller's choice)
+        lse = s0 + lane < ns ? a.ws_lse[(int64_t)(s0 + lane) * items + item] : -INFINITY;
+        const float m_new = weigh(lse);
+        const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - m_new);
+        l *= keep;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) acc[e] *= keep;
+        m = m_new;
+        for (int x0 = 0; x0 < n_recs; x0 += KG * U) {
+            load_records(s0, x0);
+            add_records(x0);
         }
     }
 
     // The drafted rows it sees.
-    float q[HB][8], q_rope[HB];
+    float q[8];
+    q_raw.get(q);
+    auto add_keys = [&](int count, int x0) __attribute__((always_inline)) {
+        float s[U], top = m;
 #pragma unroll
-    for (int h = 0; h < HB; ++h) {
-        const int head = kvh * G + min(h0 + h, G - 1);
-        const T* src = (const T*)a.q + (int64_t)layer * a.q_stride[0] + row * a.q_stride[1] + (int64_t)head * a.q_stride[2];
-        load8<T>(src + c * 8, q[h]);
-        q_rope[h] = MLA ? load1(src + 512 + c) : 0.f;
-    }
-    const int64_t pos = a.q_pos[row];
-    const T* const k0 = (const T*)d.k + (int64_t)layer * d.k_stride[0] + (int64_t)kvh * d.k_stride[1] + si.q0 * d.k_stride[2];
-    const T* const v0 = (const T*)d.v + (int64_t)layer * d.v_stride[0] + (int64_t)kvh * d.v_stride[1] + si.q0 * d.v_stride[2];
-    const float sc2 = a.scale * kLog2e;
-    const int words = (si.nq + 31) / 32;
-    for (int w = 0; w < words; ++w) {
-        uint32_t bits;
-        if (d.mask) bits = w < d.mask_words ? d.mask[row * d.mask_words + w] : 0u;
-        else bits = i >= w * 32 + 31 ? ~0u : i >= w * 32 ? (2u << (i - w * 32)) - 1 : 0u;
-        if (si.nq - w * 32 < 32) bits &= (1u << (si.nq - w * 32)) - 1;   // no rows behind the sequence
-        bits = (uint32_t)__builtin_amdgcn_readfirstlane((int)bits);
-        while (bits) {
-            // The next KG set bits, one for each group of lanes.
-            int at = -1;
+        for (int u = 0; u < U; ++u) {
+            s[u] = -INFINITY;
+            if (x0 + u * KG < count) {
+                float k[8], x = MLA ? q_rope * k_rope[u] : 0.f;
+                k_raw[u].get(k);
 #pragma unroll
-            for (int g = 0; g < KG; ++g) {
-                const int b = bits ? __builtin_ctz(bits) : -1;
-                bits &= bits - 1;
-                if (g == kg) at = b;
-            }
-            if (at < 0) continue;
-            const int64_t r = w * 32 + at;
-            if (a.window > 0 && a.q_pos[si.q0 + r] <= pos - a.window) continue;
-            float k[8], v[8];
-            load8<T>(k0 + r * d.k_stride[2] + c * 8, k);
-            const float k_rope = MLA ? load1(k0 + r * d.k_stride[2] + 512 + c) : 0.f;
-            if constexpr (!MLA) load8<T>(v0 + r * d.v_stride[2] + c * 8, v);
-#pragma unroll
-            for (int h = 0; h < HB; ++h) {
-                float s = q_rope[h] * k_rope;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) s = fmaf(q[h][e], k[e], s);
-#pragma unroll
-                for (int o = CH / 2; o >= 1; o >>= 1) s += __shfl_xor(s, o);
-                s *= sc2;
-                if (s == -INFINITY) continue;   // weighs nothing
-                join_entry(s, MLA ? k : v, m[h], l[h], acc[h]);
+                for (int e = 0; e < 8; ++e) x = fmaf(q[e], k[e], x);
+                x = group_sum<CH>(x) * sc2;
+                if (x0 + u * KG + kg < count) s[u] = x;
+                top = fmaxf(top, s[u]);
             }
         }
+        const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+        l *= keep;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) acc[e] *= keep;
+        m = top;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (x0 + u * KG < count) {
+                const bool weighs = s[u] != -INFINITY;   // (a score of -inf: nothing, whatever the value)
+                const float p = weighs ? __builtin_amdgcn_exp2f(s[u] - top) : 0.f;
+                float v[8];
+                if constexpr (MLA) k_raw[u].get(v);
+                else v_raw[u].get(v);
+                l += p;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) acc[e] = fmaf(p, weighs ? v[e] : 0.f, acc[e]);
+            }
+        }
+    };
+    if (count > 0) add_keys(count, 0);
+    for (int b = 0;;) {
+        for (int x0 = b == 0 ? KG * U : 0; x0 < count; x0 += KG * U) {
+            load_keys(list, count, b, x0);
+            add_keys(count, x0);
+        }
+        if (++b * 64 >= (d.mask ? nq : i + 1)) break;
+        seen = columns(b);
+        list = list_of(seen);
+        count = __builtin_popcountll(seen);
     }
 
-    // The groups of lanes hold disjoint entries.
+    // The groups of lanes hold disjoint entries: their sums, relative to the largest
+    // maximum, are added and dealt out at once, so that a lane ends with `OUT` channels.
+    constexpr int OUT = MLA ? 8 : 2;
+    if constexpr (!MLA) {
+        float x, y, top;
+        both<32>(m, x, y);
+        both<16>(fmaxf(x, y), x, y);
+        top = fmaxf(x, y);
+        if constexpr (CH == 8) top = dpp_max<kDppRor + 8>(top);
+        const float r = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+        m = top;
+        both<32>(l * r, x, y);
+        both<16>(x + y, x, y);
+        l = x + y;
 #pragma unroll
-    for (int h = 0; h < HB; ++h) {
+        for (int e = 0; e < 4; ++e) acc[e] = scatter_sum<32>(acc[e] * r, acc[4 + e] * r);
 #pragma unroll
-        for (int o = CH; o < 64; o <<= 1) {
-            const float m2 = __shfl_xor(m[h], o), l2 = __shfl_xor(l[h], o);
-            const float m_new = fmaxf(m[h], m2);
-            const float r1 = m[h] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[h] - m_new);
-            const float r2 = m2 == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m2 - m_new);
-            l[h] = l[h] * r1 + l2 * r2;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) acc[h][e] = acc[h][e] * r1 + __shfl_xor(acc[h][e], o) * r2;
-            m[h] = m_new;
+        for (int e = 0; e < 2; ++e) acc[e] = scatter_sum<16>(acc[e], acc[2 + e]);
+        if constexpr (CH == 8) {
+            l = dpp_add<kDppRor + 8>(l);
+            acc[0] = dpp_add<kDppRor + 8>(acc[0]);
+            acc[1] = dpp_add<kDppRor + 8>(acc[1]);
+            if (lane & 8) return;   // the row's other half has the same
         }
-        if (h0 + h >= G || kg != 0) continue;
-        const float inv = row_inverse(l[h]);
-        T* dst = (T*)a.out + (int64_t)layer * a.o_stride[0] + row * a.o_stride[1] +
-                 (int64_t)(kvh * G + h0 + h) * a.o_stride[2] + c * 8;
-        if constexpr (sizeof(T) == 4) {
-            *(f32x4*)dst = f32x4{acc[h][0] * inv, acc[h][1] * inv, acc[h][2] * inv, acc[h][3] * inv};
-            *(f32x4*)(dst + 4) = f32x4{acc[h][4] * inv, acc[h][5] * inv, acc[h][6] * inv, acc[h][7] * inv};
-        } else {
-            u32x4 o;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) o[e] = bf_rne(acc[h][2 * e] * inv) | (bf_rne(acc[h][2 * e + 1] * inv) << 16);
-            *(u32x4*)dst = o;
-        }
-        if (a.lse_out && c == 0) a.lse_out[item0 + h] = row_lse2(m[h], l[h]) * kLn2;
     }
+    const float inv = row_inverse(l);
+    // Channels of the lane: the upper half and the odd rows of lanes hold the later ones.
+    const int at = c * 8 + (MLA ? 0 : (lane >> 5) * 4 + ((lane >> 4) & 1) * 2);
+    T* const dst = (T*)a.out + (int64_t)layer * a.o_stride[0] + row * a.o_stride[1] + (int64_t)head * a.o_stride[2] + at;
+    if constexpr (sizeof(T) == 4) {
+        typedef float f32x2 __attribute__((ext_vector_type(2)));
+        *(f32x2*)dst = f32x2{acc[0] * inv, acc[1] * inv};
+    } else {
+        uint32_t o[OUT / 2];
+#pragma unroll
+        for (int e = 0; e < OUT / 2; ++e) o[e] = bf_rne(acc[2 * e] * inv) | (bf_rne(acc[2 * e + 1] * inv) << 16);
+        if constexpr (MLA) *(u32x4*)dst = u32x4{o[0], o[1], o[2], o[3]};
+        else *(uint32_t*)dst = o[0];
+    }
+    if (a.lse_out && lane == 0) a.lse_out[item] = row_lse2(m, l) * kLn2;
 }
 
-template <typename T, int D, int HB>
-hipError_t launch_hb(const AttnArgs& a, const DraftArgs& d, hipStream_t stream) {
-    const int G = a.n_heads / a.n_kv_heads;
-    const int64_t units = (int64_t)a.max_q * a.n_kv_heads * ((G + HB - 1) / HB);
-    const int64_t blocks = (units + kJoinWaves - 1) / kJoinWaves;
-    if (blocks > 0x7fffffff || a.n_layers > 65535) return hipErrorInvalidValue;
+template <typename T, int D>
+hipError_t launch_d(const AttnArgs& a, const DraftArgs& d, hipStream_t stream) {
+    const int64_t units = (int64_t)a.max_q * a.n_heads;
+    if (units > 0x7fffffff || a.n_layers > 65535) return hipErrorInvalidValue;
     for (int seq0 = 0; seq0 < a.n_seqs; seq0 += 65535) {
         const int n = a.n_seqs - seq0 < 65535 ? a.n_seqs - seq0 : 65535;
-        hipLaunchKernelGGL((tree_join<T, D, HB>), dim3((unsigned)blocks, (unsigned)n, (unsigned)a.n_layers),
+        hipLaunchKernelGGL((tree_join<T, D>), dim3((unsigned)((units + kJoinWaves - 1) / kJoinWaves), (unsigned)n, (unsigned)a.n_layers),
                            dim3(kJoinWaves * 64), 0, stream, a, d, seq0);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
-}
-
-template <typename T, int D>
-hipError_t launch_d(const AttnArgs& a, const DraftArgs& d, hipStream_t stream) {
-    return a.n_heads / a.n_kv_heads >= 4 ? launch_hb<T, D, 4>(a, d, stream) : launch_hb<T, D, 1>(a, d, stream);
 }
 
 }  // namespace

@@ -80,7 +80,7 @@ ATTENTION_REFUSALS = [
     (dict(workspace_bytes=64), 2), (dict(workspace=BASE + 8), 3), (dict(t__reserved=1), 2), (dict(t__k=BASE + 8), 3),
     (dict(t__v=BASE + 4), 3), (dict(t__mask=BASE + 2), 3), (dict(t__mask_words=0), 2), (dict(d__max_q=33), 2),
     (dict(t__k_stride=pkv._i64x3(-8, 128, 256)), 2), (dict(t__v_stride=pkv._i64x3(4, 128, 256)), 3),
-    (dict(out=BASE + 2 * GB), 4), (dict(out=BASE + 3 * GB), 4), (dict(out=BASE + 4 * GB), 4), (dict(out=BASE + 6 * GB), 4),
+    (dict(t__k_stride=pkv._i64x3(0, 0, (1 << 25) + 8)), 2), (dict(out=BASE + 2 * GB), 4), (dict(out=BASE + 3 * GB), 4), (dict(out=BASE + 4 * GB), 4), (dict(out=BASE + 6 * GB), 4),
     (dict(head_dim=96), 5), (dict(d__dtype=3), 5), (dict(d__window=-1), 2), (dict(n_kv_heads=3), 2), (dict(scale=float("nan")), 2),
 ]
 
