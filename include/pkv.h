@@ -628,7 +628,8 @@ pkv_status pkv_tree_verify(const void* target_probs, const void* draft_probs, co
                            int32_t* next_token, const pkv_verify_desc* desc, void* workspace, size_t workspace_bytes,
                            void* stream);
 
-/* Bytes of device workspace of pkv_tree_commit; 0 unless quant (a cache held in 8 bits). */
+/* Bytes of device workspace of pkv_tree_commit: 0 in this version of the library, for caches
+ * of every kind (quant: held in 8 bits); workspace may be NULL then. */
 size_t pkv_tree_commit_workspace_size(int32_t n_seqs, int32_t max_path, int32_t quant);
 
 /* Append the accepted rows to the cache: for every sequence and i < n_accepted[s] (at most
@@ -641,9 +642,8 @@ size_t pkv_tree_commit_workspace_size(int32_t n_seqs, int32_t max_path, int32_t 
  * rope_offset and rope_style are not used.  kv_base: device int64 [n_seqs], as in
  * pkv_attn_desc (contiguous caches only).  A row, slot or page entry out of range is skipped (and
  * *layout->err_flag set).  Different sequences must not write the same slot.
- * Errors: as pkv_reposition_splice, _paged and _quant; PKV_ERR_SHAPE (kv_base with paging, also a
- * workspace that is too small), PKV_ERR_UNSUPPORTED (max_path, or with scales n_seqs * max_path, above
- * 65535). */
+ * Errors: as pkv_reposition_splice, _paged and _quant; PKV_ERR_SHAPE (kv_base with paging),
+ * PKV_ERR_UNSUPPORTED (max_path above 65535, with scales also n_seqs). */
 pkv_status pkv_tree_commit(const void* draft_k, const void* draft_v, void* cache_k, void* cache_v, const int32_t* path,
                            const int32_t* n_accepted, const int32_t* kv_len, const int64_t* kv_base, int32_t n_seqs,
                            int32_t max_path, const pkv_layout* layout, const pkv_paged_cache* paging,

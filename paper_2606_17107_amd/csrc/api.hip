@@ -657,7 +657,7 @@ PKV_EXPORT pkv_status pkv_suffix_attention_noalloc(const void* q, const void* k_
 
 namespace {
 
-// The quantising splice.  accepted: its segments, in device memory, are first formed from these.
+// The quantising splice.  accepted: instead of segments, the rows that are accepted.
 pkv_status splice_quant(const void* src_k, const void* src_v, void* k_pages, void* v_pages, const pkv_segment_quant* segs,
                         int32_t n_segs, int32_t max_seg_tokens, const int32_t* kv_len, int32_t n_seqs, const double* omega,
                         float rope_theta, int32_t rope_dim, const pkv_layout* layout, const pkv_paged_cache* paging,
@@ -699,8 +699,8 @@ pkv_status splice_quant(const void* src_k, const void* src_v, void* k_pages, voi
     } else if (!(rope_theta > 0.0f) || !isfinite(rope_theta)) {
         return fail(PKV_ERR_SHAPE, "rope_theta must be finite and positive");
     }
-    if (n_segs > 65535) return fail(PKV_ERR_UNSUPPORTED, "at most 65535 segments per call");
-    if (n_segs > 0 && !segs) return fail(PKV_ERR_NULL, "segs is NULL");
+    if (n_segs > 65535) return fail(PKV_ERR_UNSUPPORTED, "at most 65535 %s per call", accepted ? "sequences" : "segments");
+    if (n_segs > 0 && !segs && !accepted) return fail(PKV_ERR_NULL, "segs is NULL");
     if ((uintptr_t)segs & 7u) return fail(PKV_ERR_ALIGN, "segs must be 8-byte aligned");
     const int eb = L->dtype == PKV_BF16 ? 2 : 4;
     for (int i = 0; i < 3; ++i) {
@@ -781,12 +781,11 @@ pkv_status splice_quant(const void* src_k, const void* src_v, void* k_pages, voi
     if (!pkv::store_fits(a))
         return fail(PKV_ERR_UNSUPPORTED, "n_layers x n_kv_heads or max_seg_tokens beyond the grid's limits");
     if (accepted) {
-        pkv::TreeCommitArgs t = *accepted;
-        t.table[0] = paging->block_table;
-        const hipError_t e = pkv::launch_tree_segments(t, (pkv::StoreSegment*)segs, (hipStream_t)stream);
-        if (e != hipSuccess) return device_status(e, "tree_commit launch");
+        a.rows = accepted->path;
+        a.n_rows = accepted->n_accepted;
+        a.max_rows = accepted->max_path;
     }
-    return device_status(pkv::launch_store(a, (hipStream_t)stream), "reposition_splice_quant launch");
+    return device_status(pkv::launch_store(a, (hipStream_t)stream), accepted ? "tree_commit launch" : "reposition_splice_quant launch");
 }
 
 }  // namespace
@@ -1060,8 +1059,8 @@ PKV_EXPORT pkv_status pkv_tree_verify(const void* target_probs, const void* draf
 }
 
 PKV_EXPORT size_t pkv_tree_commit_workspace_size(int32_t n_seqs, int32_t max_path, int32_t quant) {
-    if (!quant || n_seqs <= 0 || max_path <= 0) return 0;
-    return (size_t)n_seqs * max_path * sizeof(pkv_segment_quant);
+    (void)n_seqs, (void)max_path, (void)quant;
+    return 0;
 }
 
 PKV_EXPORT pkv_status pkv_tree_commit(const void* draft_k, const void* draft_v, void* cache_k, void* cache_v,
@@ -1069,6 +1068,7 @@ PKV_EXPORT pkv_status pkv_tree_commit(const void* draft_k, const void* draft_v, 
                                       const int64_t* kv_base, int32_t n_seqs, int32_t max_path, const pkv_layout* layout,
                                       const pkv_paged_cache* paging, const pkv_block_scales* scales, void* workspace,
                                       size_t workspace_bytes, void* stream) {
+    (void)workspace, (void)workspace_bytes;
     const pkv_layout* L = layout;
     if (!L) return fail(PKV_ERR_NULL, "layout is NULL");
     if (!path || !n_accepted || !kv_len) return fail(PKV_ERR_NULL, "path, n_accepted and kv_len are required");
@@ -1076,8 +1076,7 @@ PKV_EXPORT pkv_status pkv_tree_commit(const void* draft_k, const void* draft_v, 
         return fail(PKV_ERR_SHAPE, "n_seqs (%d) and max_path (%d) must be positive", n_seqs, max_path);
     if (paging && kv_base) return fail(PKV_ERR_SHAPE, "kv_base must be NULL for a paged cache");
     if (scales && !paging) return fail(PKV_ERR_NULL, "a cache held in 8 bits is paged: paging is NULL");
-    if (max_path > 65535 || (scales && (int64_t)n_seqs * max_path > 65535))
-        return fail(PKV_ERR_UNSUPPORTED, "max_path (%d), or into 8 bits n_seqs x max_path, above 65535", max_path);
+    if (max_path > 65535) return fail(PKV_ERR_UNSUPPORTED, "max_path (%d) above 65535", max_path);
     pkv::TreeCommitArgs t;
     memset(&t, 0, sizeof t);
     t.n_rows = L->n_tokens;
@@ -1089,23 +1088,14 @@ PKV_EXPORT pkv_status pkv_tree_commit(const void* draft_k, const void* draft_v, 
     t.n_seqs = n_seqs;
     t.max_path = max_path;
     t.err_flag = L->err_flag;
-    if (scales) {
-        const size_t need = pkv_tree_commit_workspace_size(n_seqs, max_path, 1);
-        if (!workspace) return fail(PKV_ERR_NULL, "workspace of %zu bytes is required", need);
-        if (workspace_bytes < need) return fail(PKV_ERR_SHAPE, "workspace_bytes %zu < required %zu", workspace_bytes, need);
-        if (!aligned16(workspace)) return fail(PKV_ERR_ALIGN, "workspace must be 16-byte aligned");
-        // Rows that are at their positions: any rotary slice will do, the smallest one.
-        pkv_layout at = *L;
-        at.rope_offset = 0;
-        at.rope_style = PKV_ROPE_HALF;
-        // (the checks of the splice come first: on an error nothing is enqueued)
-        return splice_quant(draft_k, draft_v, cache_k, cache_v, (const pkv_segment_quant*)workspace, n_seqs * max_path, 1,
-                            kv_len, n_seqs, nullptr, 1.0f, 16, &at, paging, scales, &t, stream);
-    }
-    pkv::SpliceArgs a;
+    // Rows that are at their positions: any rotary slice will do, the smallest one.
     pkv_layout at = *L;
     at.rope_offset = 0;
     at.rope_style = PKV_ROPE_HALF;
+    if (scales)
+        return splice_quant(draft_k, draft_v, cache_k, cache_v, nullptr, n_seqs, max_path, kv_len, n_seqs, nullptr, 1.0f, 16, &at,
+                            paging, scales, &t, stream);
+    pkv::SpliceArgs a;
     const pkv_status st = check_splice(draft_k, draft_v, cache_k, cache_v, 1.0f, 2 * (at.dtype == PKV_F32 ? 4 : 8), &at, false, a,
                                        paging);
     if (st != PKV_OK) return st;

@@ -110,6 +110,11 @@ struct StoreArgs {
     uint8_t* v_scale;
     int64_t k_scale_stride[4];   // {layer, head, page, block in page}
     int64_t v_scale_stride[4];
+    // instead of segments (then n_segs is n_seqs): sequence s appends source rows
+    // rows[s][0 .. n_rows[s]) of at most max_rows, unturned, behind its kv_len[s] slots
+    const int32_t* rows;      // or null
+    const int32_t* n_rows;
+    int32_t max_rows;
 };
 
 bool store_fits(const StoreArgs& a);   // the launch is within the grid's limits
@@ -296,7 +301,5 @@ struct TreeCommitArgs {
     int32_t* err_flag;
 };
 hipError_t launch_tree_commit(const TreeCommitArgs& a, hipStream_t stream);
-// The accepted rows as one-row segments of the quantising splice, n_seqs x max_path records.
-hipError_t launch_tree_segments(const TreeCommitArgs& a, StoreSegment* segs, hipStream_t stream);
 
 }  // namespace pkv

@@ -141,7 +141,9 @@ struct Raw8<false> {
 __device__ inline uint32_t swap1(uint32_t v) { return (uint32_t)dpp<0xb1>((int)v, (int)v); }   // quad_perm [1, 0, 3, 2]
 
 // D: head size.  SUBS: waves (of 32 slots) per scale block.  INTER: interleaved pairs.
-template <int D, int SUBS, bool F32, bool INTER>
+// LISTED: instead of records, sequence s appends rows a.rows[s][0 .. a.n_rows[s]) of the
+// source behind its a.kv_len[s] slots, as they are.
+template <int D, int SUBS, bool F32, bool INTER, bool LISTED>
 __global__ __launch_bounds__(kWaves * 64, D == 64 ? 5 : F32 ? 3 : 4) void store_kernel(StoreArgs a, StoreGeo g, Freqs ft) {
     constexpr int LPT = D / 16;           // lanes per row
     constexpr int TPS = 64 / LPT;         // rows per step
@@ -153,10 +155,17 @@ __global__ __launch_bounds__(kWaves * 64, D == 64 ? 5 : F32 ? 3 : 4) void store_
 
     // The first look at the records (below) is under way before this segment's own is here.
     const int lane = threadIdx.x & 63;
-    StoreSegment look = a.segs[min(lane, a.n_segs - 1)];
+    StoreSegment look{};
+    if constexpr (!LISTED) look = a.segs[min(lane, a.n_segs - 1)];
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int seg_i = blockIdx.y;
-    const StoreSegment mine = a.segs[seg_i];
+    StoreSegment mine;
+    if constexpr (LISTED) {
+        const int at = a.kv_len[seg_i];
+        mine = StoreSegment{0, seg_i, min(a.n_rows[seg_i], a.max_rows), at, at};
+    } else {
+        mine = a.segs[seg_i];
+    }
     const int spot = g.parts == 1 ? (int)blockIdx.x : (int)(blockIdx.x / (uint32_t)g.parts);
     const int part = (int)blockIdx.x - spot * g.parts;
     const int tensor = g.tensors == 2 ? blockIdx.z & 1 : 0, layer = g.tensors == 2 ? blockIdx.z >> 1 : blockIdx.z;
@@ -174,9 +183,9 @@ __global__ __launch_bounds__(kWaves * 64, D == 64 ? 5 : F32 ? 3 : 4) void store_
     if (mine.n_tokens <= 0) return;
     const int64_t past = (int64_t)mine.dst_pos0 + mine.n_tokens;
     if (teller && (mine.seq < 0 || mine.seq >= a.n_seqs || mine.dst_pos0 < 0 || past > a.dst_capacity ||
-                   mine.src_slot0 < 0 || mine.src_slot0 > a.n_src - mine.n_tokens))
+                   (LISTED ? a.n_src <= 0 : mine.src_slot0 < 0 || mine.src_slot0 > a.n_src - mine.n_tokens)))
         flag();
-    if (mine.seq < 0 || mine.seq >= a.n_seqs || a.n_src <= 0) return;
+    if (mine.seq < 0 || mine.seq >= a.n_seqs || a.n_src <= 0 || (LISTED && mine.dst_pos0 < 0)) return;
     const int cap = (int)a.dst_capacity;   // at most 2^30: slots and block ends are int32
     const int end = (int)min(past, (int64_t)cap);
     const int live = min(a.kv_len[mine.seq], cap);
@@ -239,7 +248,8 @@ __global__ __launch_bounds__(kWaves * 64, D == 64 ? 5 : F32 ? 3 : 4) void store_
             // the block's slots [lo, hi) that the record fills from rows that exist
             const int64_t shift = (int64_t)s.dst_pos0 - s.src_slot0;   // slot - source slot
             const int lo = (int)min(max(max((int64_t)slot0, (int64_t)s.dst_pos0), shift), (int64_t)block_end);
-            const int hi = (int)max(min(min((int64_t)block_end, (int64_t)s.dst_pos0 + s.n_tokens), shift + a.n_src), (int64_t)slot0);
+            const int64_t rows_end = LISTED ? past : shift + a.n_src;
+            const int hi = (int)max(min(min((int64_t)block_end, (int64_t)s.dst_pos0 + s.n_tokens), rows_end), (int64_t)slot0);
 #pragma unroll
             for (int t = 0; t < STEPS; ++t) {
                 const int slot = first + t * TPS;
@@ -252,11 +262,29 @@ __global__ __launch_bounds__(kWaves * 64, D == 64 ? 5 : F32 ? 3 : 4) void store_
         {
             int lo;
             const char* const p = assign(mine, 0, &lo);
+            if constexpr (LISTED) {
+                int row[STEPS];
 #pragma unroll
-            for (int t = 0; t < STEPS; ++t) {
-                const uint32_t off = rec[t] == 0 ? (uint32_t)(first + t * TPS - lo) * src_row : 0u;
-                raw[t][0].load(p + (off + ca * 8 * EB));
-                raw[t][1].load(p + (off + cb * 8 * EB));
+                for (int t = 0; t < STEPS; ++t)
+                    row[t] = rec[t] == 0 ? a.rows[(int64_t)seg_i * a.max_rows + (first + t * TPS - mine.dst_pos0)] : 0;
+#pragma unroll
+                for (int t = 0; t < STEPS; ++t) {
+                    const bool is = row[t] >= 0 && row[t] < a.n_src;
+                    if (!is) {
+                        rec[t] = -1;
+                        flag();
+                    }
+                    const char* const at = src + (is ? (uint64_t)(uint32_t)row[t] * src_row : 0);
+                    raw[t][0].load(at + ca * 8 * EB);
+                    raw[t][1].load(at + cb * 8 * EB);
+                }
+            } else {
+#pragma unroll
+                for (int t = 0; t < STEPS; ++t) {
+                    const uint32_t off = rec[t] == 0 ? (uint32_t)(first + t * TPS - lo) * src_row : 0u;
+                    raw[t][0].load(p + (off + ca * 8 * EB));
+                    raw[t][1].load(p + (off + cb * 8 * EB));
+                }
             }
         }
         const int old = (int)*scale_at;
@@ -271,7 +299,7 @@ __global__ __launch_bounds__(kWaves * 64, D == 64 ? 5 : F32 ? 3 : 4) void store_
         int records = 1;
         bool owner = true, moved = mine.dst_pos0 != mine.src_pos0;
 #pragma unroll 1
-        for (int j0 = 0; j0 < a.n_segs && owner; j0 += 64) {
+        for (int j0 = 0; !LISTED && j0 < a.n_segs && owner; j0 += 64) {
 #pragma unroll 1
             for (uint64_t hits = others(j0); hits; hits &= hits - 1) {
                 const int h = j0 + __builtin_ctzll(hits);
@@ -381,7 +409,7 @@ __global__ __launch_bounds__(kWaves * 64, D == 64 ? 5 : F32 ? 3 : 4) void store_
                 turn_rows(mine, 0);
                 // The other records' rows, found once more.
 #pragma unroll 1
-                for (int j0 = 0, r = 1; r < records && j0 < a.n_segs; j0 += 64)
+                for (int j0 = 0, r = 1; !LISTED && r < records && j0 < a.n_segs; j0 += 64)
 #pragma unroll 1
                     for (uint64_t hits = others(j0); hits; hits &= hits - 1, ++r)
                         turn_rows(a.segs[j0 + __builtin_ctzll(hits)], r);
@@ -507,11 +535,13 @@ template <int D, int SUBS>
 void launch_geo(const StoreArgs& a, const StoreGeo& g, const Freqs& f, dim3 grid, hipStream_t stream) {
     const dim3 block(kWaves * 64);
     if (a.elem_bytes == 4) {
-        if (a.rope_style) hipLaunchKernelGGL((store_kernel<D, SUBS, true, true>), grid, block, 0, stream, a, g, f);
-        else hipLaunchKernelGGL((store_kernel<D, SUBS, true, false>), grid, block, 0, stream, a, g, f);
+        if (a.rows) hipLaunchKernelGGL((store_kernel<D, SUBS, true, false, true>), grid, block, 0, stream, a, g, f);
+        else if (a.rope_style) hipLaunchKernelGGL((store_kernel<D, SUBS, true, true, false>), grid, block, 0, stream, a, g, f);
+        else hipLaunchKernelGGL((store_kernel<D, SUBS, true, false, false>), grid, block, 0, stream, a, g, f);
     } else {
-        if (a.rope_style) hipLaunchKernelGGL((store_kernel<D, SUBS, false, true>), grid, block, 0, stream, a, g, f);
-        else hipLaunchKernelGGL((store_kernel<D, SUBS, false, false>), grid, block, 0, stream, a, g, f);
+        if (a.rows) hipLaunchKernelGGL((store_kernel<D, SUBS, false, false, true>), grid, block, 0, stream, a, g, f);
+        else if (a.rope_style) hipLaunchKernelGGL((store_kernel<D, SUBS, false, true, false>), grid, block, 0, stream, a, g, f);
+        else hipLaunchKernelGGL((store_kernel<D, SUBS, false, false, false>), grid, block, 0, stream, a, g, f);
     }
 }
 
@@ -553,7 +583,9 @@ hipError_t launch_store(const StoreArgs& a, hipStream_t stream) {
     if (!fits) return hipErrorInvalidValue;
     const int subs = a.block_tokens / kSub;
     Freqs f;
-    if (a.omega) {
+    if (a.rows) {   // nothing is turned
+        for (int i = 0; i < kPairs; ++i) f.w[i] = 0.0;
+    } else if (a.omega) {
         for (int i = 0; i < kPairs; ++i) f.w[i] = i < a.rope_dim / 2 ? a.omega[i] : 0.0;
     } else {
         for (int i = 0; i < kPairs; ++i) f.w[i] = i < a.rope_dim / 2 ? pow(a.theta, -2.0 * i / a.rope_dim) : 0.0;
