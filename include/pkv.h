@@ -568,8 +568,12 @@ size_t pkv_tree_attention_workspace_size(const pkv_attn_desc* desc, int32_t n_q_
  *     row c of its sequence:  bit c of its mask, and q_pos[c] > q_pos[i] - window if window > 0
  * under one softmax.  kv_len counts the cache's slots only.  paging NULL: a contiguous
  * cache (bf16 or fp32 GQA, bf16 MLA); else a paged one (bf16); scales with paging: one
- * held in 8 bits (GQA).  Scores, sums and products with the drafted rows are fp32.  A row that
- * sees nothing is zeros (lse_out -inf).  What a row does not see does not reach it,
+ * held in 8 bits (GQA).  Arithmetic as in suffix attention; over the drafted rows scores, sums
+ * and products are fp32, save that calls of many bf16 GQA rows round their probabilities to
+ * bf16 before the product there too.  How the keys are cut follows n_seqs, max_q, max_kv_len and
+ * the cache lengths, so a sequence's result may differ in rounding when those of others
+ * change; it depends on nothing else outside the sequence.  A row that sees nothing is zeros
+ * (lse_out -inf).  What a row does not see does not reach it,
  * NaN and infinities included; a visible drafted row whose score is -inf weighs nothing,
  * whatever its values.
  * Errors: as pkv_suffix_attention, _paged and _quant; PKV_ERR_NULL (draft, its k or v; scales
@@ -618,8 +622,8 @@ size_t pkv_tree_verify_workspace_size(const pkv_verify_desc* desc);
  * throughout, p takes its place; where p is 0 too, -1, and *err_flag is set.
  * Probabilities that are NaN, infinite or not above 0 count as 0.  A row whose parent or
  * token is out of range is no child of any row, and sets *err_flag (parent -1 does not).  A sequence
- * without rows has n_accepted 0 and next_token -1.  Sums and comparisons are in 64 bits and
- * do not depend on timing.
+ * without rows has n_accepted 0 and next_token -1 (with total_q 0 the tensors of rows may be
+ * NULL).  Sums and comparisons are in 64 bits and do not depend on timing.
  * Errors: PKV_ERR_NULL, PKV_ERR_SHAPE (also a workspace that is too small), PKV_ERR_ALIGN
  * (workspace 16 bytes, probabilities their type), PKV_ERR_UNSUPPORTED (dtype, sizes above those
  * limits), PKV_ERR_DEVICE. */

@@ -1024,7 +1024,8 @@ PKV_EXPORT pkv_status pkv_tree_verify(const void* target_probs, const void* draf
                                       void* workspace, size_t workspace_bytes, void* stream) {
     const pkv_status st = check_verify(desc);
     if (st != PKV_OK) return st;
-    if (!target_probs || !tokens || !parent || !u_accept || !u_sample || !path || !n_accepted || !next_token)
+    const bool rows = desc->total_q > 0;   // (a call without rows has no tensors of rows)
+    if ((rows && (!target_probs || !tokens || !parent || !u_accept)) || !u_sample || !path || !n_accepted || !next_token)
         return fail(PKV_ERR_NULL, "target_probs, tokens, parent, u_accept, u_sample, path, n_accepted and next_token are required");
     const uintptr_t eb = desc->dtype == PKV_BF16 ? 2 : 4;
     if ((uintptr_t)target_probs % eb || (uintptr_t)draft_probs % eb)

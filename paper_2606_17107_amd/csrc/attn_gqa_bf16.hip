@@ -115,6 +115,9 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_gqa_bf16_kernel(AttnArgs 
     // Rows of this lane (one per 32-row block) and their visible key ranges
     // [row_start, row_end): causal, and with a sliding window also
     // row_start = q_pos - window + 1.
+    // kPieces: trees seldom fill a row block.  A wave without rows only stages its share of
+    // the tiles (16 sequences of 16 rows of 4 heads, 2000..9000 keys in 8 bits: 76.9 -> 73.2 us).
+    const bool busy = FORM != kPieces || m0 + wave * 32 * QB < M;
     int qi[QB], head[QB], row_end[QB], row_start[QB];
     bool row_ok[QB];
 #pragma unroll
@@ -500,6 +503,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_gqa_bf16_kernel(AttnArgs 
         lds_reads_done();
         bare_barrier();
         refill(i, stage_tag);
+        if (!busy) return;
         f32x16 sc[NKB][QB];
         qk(kst(S), sc);
         bf16x8 pb[QB][2 * NKB];
@@ -708,14 +712,19 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_gqa_bf16_kernel(AttnArgs 
                 const float scale = win.scale(ahead);
                 char* const dst = (char*)kst(S);
                 load_codes(i + NS + 1, later);
-                half_step(kst((U + 1) % NS), 0, vst(U), 0, cur, nxt, [&](int q) __attribute__((always_inline)) {
-                    if (q % EVERY == 0) put_codes(set[q / EVERY], scale, dst + lds8[q / EVERY]);
-                });
+                if (busy) {
+                    half_step(kst((U + 1) % NS), 0, vst(U), 0, cur, nxt, [&](int q) __attribute__((always_inline)) {
+                        if (q % EVERY == 0) put_codes(set[q / EVERY], scale, dst + lds8[q / EVERY]);
+                    });
+                } else {
+#pragma unroll
+                    for (int n = 0; n < PER; ++n) put_codes(set[n], scale, dst + lds8[n]);
+                }
 #pragma unroll
                 for (int n = 0; n < PER; ++n) set[n] = later[n];
             } else {
                 refill(i, u_tag);
-                half_step(kst((U + 1) % NS), 0, vst(U), 0, cur, nxt, [](int) {});
+                if (busy) half_step(kst((U + 1) % NS), 0, vst(U), 0, cur, nxt, [](int) {});
             }
         };
 
@@ -726,6 +735,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_gqa_bf16_kernel(AttnArgs 
             lds_reads_done();
             bare_barrier();
             refill(i, u_tag);
+            if (!busy) return;
             bf16x8 pb[QB][2];
 #pragma unroll
             for (int qb = 0; qb < QB; ++qb) {

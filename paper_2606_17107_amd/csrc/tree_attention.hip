@@ -17,11 +17,13 @@
 // The step is a chain of memory round trips (bounds; log-sum-exps, mask and query;
 // partials, keys and values), so what does not depend on each other is asked for together.
 #include "attn_columns.h"
+#include "attn_gqa_tile.h"
 
 namespace pkv {
 namespace {
 
 constexpr int kJoinWaves = 4;
+constexpr int64_t kTileRows = 64, kTileTotal = 24576;
 constexpr int kJoinKeys = 2;
 
 // Eight values as they lie in memory, and as floats.
@@ -345,6 +347,234 @@ __global__ __launch_bounds__(kJoinWaves * 64) void tree_join(AttnArgs a, DraftAr
     if (a.lse_out && lane == 0) a.lse_out[item] = row_lse2(m, l) * kLn2;
 }
 
+// The same for many rows of bf16 heads: a workgroup takes 128 (row, head-in-group) rows
+// of one KV head, 32 a wave, and the drafted rows 32 at a time through LDS and the
+// matrix cores, in the layouts of the many-row attention kernels (S^T = K Q^T, then
+// O^T += V^T P^T with probabilities rounded to bf16, as over the cache).  Above, a thousand
+// rows of a head cost about 0.7 us, most of it instructions; here keys, values and masks are
+// read once for 128 rows.
+// A value that is no finite number is left out of the tile (0 * inf would reach rows
+// that do not see it) and added by hand to the rows that do.
+template <int D>
+__global__ __launch_bounds__(256, 2) void tree_join_tiles(AttnArgs a, DraftArgs d, int seq0) {
+    constexpr int BN = 32, KS = D / 16, DB = D / 32, CH = D / 8;
+    constexpr int PER = BN * CH / 256;     // 16-byte chunks of a tile a thread stages
+    __shared__ __attribute__((aligned(16))) uint16_t k_lds[BN * D], v_lds[BN * D];
+    __shared__ uint32_t odd_keys[2];       // keys of the tile with values that were left out
+    const int tid = threadIdx.x, lane = tid & 63, j = lane & 31, hl = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int seq = seq0 + (int)blockIdx.y, layer = (int)blockIdx.z / a.n_kv_heads, kvh = (int)blockIdx.z - layer * a.n_kv_heads;
+    int q0 = 0, nq = a.total_q;
+    if (a.cu_q) {
+        q0 = a.cu_q[seq];
+        nq = a.cu_q[seq + 1] - q0;
+    }
+    if (q0 < 0 || nq < 0 || (int64_t)q0 + nq > a.total_q) nq = 0;   // as seq_info
+    const int G = a.n_heads / a.n_kv_heads, M = min(nq, a.max_q) * G, m0 = (int)blockIdx.x * 128;
+    if (m0 >= M) return;   // uniform
+    const int m = m0 + wave * 32 + j;
+    const bool row_ok = m < M;
+    const int i = row_ok ? m / G : 0, head = kvh * G + (row_ok ? m - i * G : 0);   // rows past M repeat row 0 (never written)
+    const int64_t row = q0 + i;
+    const int64_t items = (int64_t)a.n_layers * a.total_q * a.n_heads;
+    const int64_t item = ((int64_t)layer * a.total_q + row) * a.n_heads + head;
+
+    // The first tile's keys and values, the query.
+    const uint16_t* const k0 = (const uint16_t*)d.k + (int64_t)layer * d.k_stride[0] + (int64_t)kvh * d.k_stride[1] + q0 * d.k_stride[2];
+    const uint16_t* const v0 = (const uint16_t*)d.v + (int64_t)layer * d.v_stride[0] + (int64_t)kvh * d.v_stride[1] + q0 * d.v_stride[2];
+    u32x4 k_raw[PER], v_raw[PER];
+    auto load_tile = [&](int t) __attribute__((always_inline)) {
+#pragma unroll
+        for (int n = 0; n < PER; ++n) {
+            const int key = (tid + n * 256) / CH, c = (tid + n * 256) % CH, r = t * BN + key;
+            const bool in = r < nq;
+            const u32x4 k = *(const u32x4*)(k0 + (int64_t)(in ? r : 0) * d.k_stride[2] + c * 8);
+            const u32x4 v = *(const u32x4*)(v0 + (int64_t)(in ? r : 0) * d.v_stride[2] + c * 8);
+            const u32x4 none = {0u, 0u, 0u, 0u};
+            k_raw[n] = in ? k : none;
+            v_raw[n] = in ? v : none;
+        }
+    };
+    load_tile(0);
+    bf16x8 qf[KS];
+    {
+        const uint16_t* const qrow = (const uint16_t*)a.q + (int64_t)layer * a.q_stride[0] + row * a.q_stride[1] + (int64_t)head * a.q_stride[2];
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) qf[ks] = __builtin_bit_cast(bf16x8, *(const u32x4*)(qrow + ks * 16 + hl * 8));
+    }
+    const int64_t pos = a.window > 0 ? a.q_pos[row] : 0;
+    if (tid < 2) odd_keys[tid] = 0;
+
+    // The cache's partials, relative to the largest log-sum-exp.  Element 4b + e of o[db]
+    // is channel 32 db + 8 b + 4 hl + e of row j; both halves of a row hold all records.
+    f32x16 o[DB];
+#pragma unroll
+    for (int db = 0; db < DB; ++db) o[db] = f32x16{};
+    float mx = -INFINITY, l = 0.f;
+    for (int s = 0; s < a.n_splits; ++s) mx = fmaxf(mx, a.ws_lse[s * items + item]);
+#pragma unroll 1
+    for (int s = 0; s < a.n_splits; ++s) {
+        const float lse = a.ws_lse[s * items + item];
+        const bool used = lse != -INFINITY;
+        if (__builtin_amdgcn_ballot_w64(used) == 0) continue;
+        const float w = used ? __builtin_amdgcn_exp2f(lse - mx) : 0.f;
+        if (!used) continue;   // (its output was not written)
+        const float* const x = a.ws_o + (s * items + item) * D + hl * 4;
+        l += w;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+                const f32x4 v = *(const f32x4*)(x + db * 32 + b * 8);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[db][4 * b + e] = fmaf(w, v[e], o[db][4 * b + e]);
+            }
+    }
+    if (hl != 0) l = 0.f;   // counted once: the halves hold different drafted rows
+
+    int kofs[KS], vofs[DB];
+    gqa_operand_offsets<D>(lane, kofs, vofs);
+    const float sc2 = a.scale * kLog2e;
+    // Drafted rows that the workgroup can see: with a mask all, in a chain those up to its last row.
+    const int last_row = (min(M, m0 + 128) - 1) / G;
+    const int tiles = ((d.mask ? nq : last_row + 1) + BN - 1) / BN;
+#pragma unroll 1
+    for (int t = 0; t < tiles; ++t) {
+        __syncthreads();   // every wave is done with the tile before
+        if (tid == 0) odd_keys[(t + 1) & 1] = 0;
+#pragma unroll
+        for (int n = 0; n < PER; ++n) {
+            const int key = (tid + n * 256) / CH, c = (tid + n * 256) % CH;
+            u32x4 v = v_raw[n];
+            bool odd = false;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const bool lo = (v[e] & 0x7f80u) == 0x7f80u, hi = (v[e] & 0x7f800000u) == 0x7f800000u;
+                odd = odd || lo || hi;
+                v[e] &= (lo ? 0xffff0000u : ~0u) & (hi ? 0xffffu : ~0u);
+            }
+            if (odd) atomicOr(&odd_keys[t & 1], 1u << key);
+            *(u32x4*)(k_lds + key * D + ((c ^ swz_k<D>(key)) << 3)) = k_raw[n];
+            *(u32x4*)(v_lds + key * D + ((c ^ swz_v<D>(key)) << 3)) = v;
+        }
+        // Which of the tile's rows this row sees.
+        uint32_t word;
+        if (d.mask) word = t < d.mask_words ? d.mask[row * d.mask_words + t] : 0u;
+        else word = i >= t * BN + 31 ? ~0u : i >= t * BN ? (2u << (i - t * BN)) - 1 : 0u;
+        if (nq - t * BN < 32) word &= (1u << (nq - t * BN)) - 1;   // no rows behind the sequence
+        if (!row_ok) word = 0;
+        if (a.window > 0) {
+            for (int c = 0; c < BN; ++c)   // (a position past the sequence's end is not read)
+                if (t * BN + c < nq && a.q_pos[q0 + t * BN + c] <= pos - a.window) word &= ~(1u << c);
+        }
+        __syncthreads();
+        if (t + 1 < tiles) load_tile(t + 1);
+        if (__builtin_amdgcn_ballot_w64(word != 0) == 0) continue;   // (the barriers are behind)
+
+        f32x16 s = f32x16{};
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks)
+            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, *(const u32x4*)(k_lds + kofs[ks])), qf[ks], s, 0, 0, 0);
+        // Element r holds drafted row 8 (r / 4) + 4 hl + r % 4 of the tile.
+        float top = -INFINITY;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            s[r] = (word >> ((r >> 2) * 8 + hl * 4 + (r & 3))) & 1 ? s[r] * sc2 : -INFINITY;
+            top = fmaxf(top, s[r]);
+        }
+        float x, y;
+        both<32>(top, x, y);
+        const float m_new = fmaxf(mx, fmaxf(x, y));
+        const float keep = mx == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mx - m_new);
+        l *= keep;
+#pragma unroll
+        for (int db = 0; db < DB; ++db) o[db] *= keep;
+        mx = m_new;
+        bf16x8 pb[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            f32x8 p;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int r = h * 8 + e;
+                s[r] = s[r] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s[r] - m_new);
+                p[e] = s[r];
+            }
+            pb[h] = __builtin_convertvector(p, bf16x8);
+        }
+        // The sum takes the probabilities as they enter the product.
+        const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
+#pragma unroll
+        for (int e = 0; e < 16; e += 2)
+            l = __builtin_amdgcn_fdot2_f32_bf16((bf16x2){pb[e >> 3][e & 7], pb[e >> 3][(e & 7) + 1]}, ones, l, false);
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+                o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(gqa_v_operand<D>(v_lds + vofs[db] + h * 16 * D), pb[h], o[db], 0, 0, 0);
+        // Values that were left out, key by key.
+        uint32_t odd = (uint32_t)__builtin_amdgcn_readfirstlane((int)odd_keys[t & 1]);
+        while (odd) {
+            const int key = __builtin_ctz(odd);
+            odd &= odd - 1;
+            float mine = 0.f;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) mine = r == (key >> 3) * 4 + (key & 3) ? s[r] : mine;
+            const float other = __shfl_xor(mine, 32);
+            const float p = hl == ((key >> 2) & 1) ? mine : other;
+            const uint16_t* const v = v0 + (int64_t)(t * BN + key) * d.v_stride[2] + hl * 4;
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+#pragma unroll
+                for (int b = 0; b < 4; ++b)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float z = load1(v + db * 32 + b * 8 + e);
+                        if (p != 0.f && !(fabsf(z) < INFINITY)) o[db][4 * b + e] += p * z;
+                    }
+        }
+    }
+
+    const float l_tot = l + __shfl_xor(l, 32);
+    if (!row_ok) return;
+    const float inv = row_inverse(l_tot);
+    uint16_t* const dst = (uint16_t*)a.out + (int64_t)layer * a.o_stride[0] + row * a.o_stride[1] + (int64_t)head * a.o_stride[2];
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            u32x2 w;
+            w[0] = bf_rne(o[db][4 * b] * inv) | (bf_rne(o[db][4 * b + 1] * inv) << 16);
+            w[1] = bf_rne(o[db][4 * b + 2] * inv) | (bf_rne(o[db][4 * b + 3] * inv) << 16);
+            *(u32x2*)(dst + db * 32 + b * 8 + hl * 4) = w;
+        }
+    if (a.lse_out && hl == 0) a.lse_out[item] = row_lse2(mx, l_tot) * kLn2;
+}
+
+// Tiles pay where they fill, and where there are enough workgroups to hide that each of
+// them waits for one record after another (a wave a row and head / tiles, us a call, 32
+// heads over 8 KV heads of 128; 16 sequences of 32 rows over 2000..9000 keys 109 / 115; 24
+// of 24 over 200..500 36 / 33, over 2000..5000 103 / 103; 8 of 96 over 2000..5000 82 / 82; 48
+// of 24 over 200..500 57 / 45; 48 of 96 over 50 148 / 97, over 2000 325 / 273; as chains,
+// whose rows see many drafted rows, 8 of 96 over 1000 73 / 47, 48 of 96 over 50 262 / 89).
+bool tile_route(const AttnArgs& a) {
+    const int64_t rows = (int64_t)a.max_q * (a.n_heads / a.n_kv_heads);
+    return a.variant == 0 && a.dtype != 1 && a.n_splits <= 16 && rows >= kTileRows && rows * a.n_kv_heads * a.n_layers * a.n_seqs >= kTileTotal;
+}
+
+template <int D>
+hipError_t launch_tiles(const AttnArgs& a, const DraftArgs& d, hipStream_t stream) {
+    const int64_t rows = (int64_t)a.max_q * (a.n_heads / a.n_kv_heads), z = (int64_t)a.n_layers * a.n_kv_heads;
+    if (rows > 0x7fffffff || z > 65535) return hipErrorInvalidValue;
+    for (int seq0 = 0; seq0 < a.n_seqs; seq0 += 65535) {
+        const int n = a.n_seqs - seq0 < 65535 ? a.n_seqs - seq0 : 65535;
+        hipLaunchKernelGGL((tree_join_tiles<D>), dim3((unsigned)((rows + 127) / 128), (unsigned)n, (unsigned)z), dim3(256), 0, stream, a, d, seq0);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
 template <typename T, int D>
 hipError_t launch_d(const AttnArgs& a, const DraftArgs& d, hipStream_t stream) {
     const int64_t units = (int64_t)a.max_q * a.n_heads;
@@ -364,6 +594,7 @@ hipError_t launch_d(const AttnArgs& a, const DraftArgs& d, hipStream_t stream) {
 hipError_t launch_tree_join(const AttnArgs& a, const DraftArgs& d, hipStream_t stream) {
     if (a.max_q == 0) return hipSuccess;
     if (a.variant == 1) return launch_d<uint16_t, 576>(a, d, stream);
+    if (tile_route(a)) return a.head_dim == 64 ? launch_tiles<64>(a, d, stream) : launch_tiles<128>(a, d, stream);
     if (a.dtype == 1) return a.head_dim == 64 ? launch_d<float, 64>(a, d, stream) : launch_d<float, 128>(a, d, stream);
     return a.head_dim == 64 ? launch_d<uint16_t, 64>(a, d, stream) : launch_d<uint16_t, 128>(a, d, stream);
 }

@@ -920,6 +920,7 @@ def pages_compact(tensors, ref, block_table, page_size, ref_out=None, block_tabl
 
 
 # ---- trees of drafted tokens -------------------------------------------------------
+# The tensor-level calls run on the device of their tensors, whichever is current.
 # Rows are packed as for suffix attention (cu_q); drafted keys and values are
 # [layer][kv_head][row][channel] (any strides, channels contiguous) beside the cache.
 # Masks are int32 (or uint32) words [total_q][ceil(max_q / 32)].
@@ -961,7 +962,8 @@ def tree_masks(parent, kv_len, n_seqs=1, cu_q=None, max_q=None, mask=None, q_pos
     _check_mask(mask, dev, rows, most)
     if rows == 0:   # (an empty tensor has no address to pass down)
         return mask, q_pos
-    _check(pkv_tree_masks(parent, cu_q, kv_len, n_seqs, rows, most, mask, mask.shape[1], q_pos, err_flag, stream))
+    with torch.cuda.device(dev):
+        _check(pkv_tree_masks(parent, cu_q, kv_len, n_seqs, rows, most, mask, mask.shape[1], q_pos, err_flag, stream))
     return mask, q_pos
 
 
@@ -1043,8 +1045,9 @@ def tree_attention(q, k_cache, v_cache, draft_k, draft_v, out, q_pos, kv_len, sc
         _keep_until_done(workspace, stream)
     paging = None if block_table is None else make_paging(block_table, k_cache, v_cache, v_block_table)
     scales = make_block_scales(k_scale, v_scale, k_cache.shape[2]) if quant else None
-    _check(pkv_tree_attention(q, k_cache, v_cache, out, q_pos, kv_len, H, Hkv, D, scale, desc, make_draft(draft_k, draft_v, mask),
-                              paging, scales, workspace, need, stream))
+    with torch.cuda.device(dev):
+        _check(pkv_tree_attention(q, k_cache, v_cache, out, q_pos, kv_len, H, Hkv, D, scale, desc,
+                                  make_draft(draft_k, draft_v, mask), paging, scales, workspace, need, stream))
 
 
 def make_verify_desc(target_probs: torch.Tensor, draft_probs: Optional[torch.Tensor], cu_q: Optional[torch.Tensor], n_seqs: int,
@@ -1086,18 +1089,14 @@ def tree_verify(target_probs, tokens, parent, u_accept, u_sample, max_path, draf
         if tuple(t.shape) != shape:
             raise ValueError("%s must be %s, got %s" % (name, shape, tuple(t.shape)))
         outs.append(t)
-    if rows == 0:   # (empty tensors have no address to pass down)
-        outs[0].fill_(-1)
-        outs[1].zero_()
-        outs[2].fill_(-1)
-        return tuple(outs)
     desc = make_verify_desc(target_probs, draft_probs, cu_q, n_seqs, _most_rows(rows, max_q), max_path, err_flag)
     need = pkv_tree_verify_workspace_size(desc)
     if workspace is None or workspace.numel() * workspace.element_size() < need:
         workspace = torch.empty(max(16, need), dtype=torch.uint8, device=dev)
         _keep_until_done(workspace, stream)
-    _check(pkv_tree_verify(target_probs, draft_probs, tokens, parent, u_accept, u_sample, *outs, desc, workspace,
-                           workspace.numel() * workspace.element_size(), stream))
+    with torch.cuda.device(dev):
+        _check(pkv_tree_verify(target_probs, draft_probs, tokens, parent, u_accept, u_sample, *outs, desc, workspace,
+                               workspace.numel() * workspace.element_size(), stream))
     return tuple(outs)
 
 
@@ -1165,5 +1164,6 @@ def tree_commit(draft_k, draft_v, cache_k, cache_v, path, n_accepted, kv_len, kv
         _keep_until_done(workspace, stream)
     paging = None if block_table is None else make_paging(block_table, cache_k, cache_v, v_block_table)
     scales = make_block_scales(k_scale, v_scale, cache_k.shape[2]) if quant else None
-    _check(pkv_tree_commit(draft_k, draft_v, cache_k, cache_v, path, n_accepted, kv_len, kv_base, n_seqs, max_path, layout, paging,
-                           scales, workspace, need, stream))
+    with torch.cuda.device(dev):
+        _check(pkv_tree_commit(draft_k, draft_v, cache_k, cache_v, path, n_accepted, kv_len, kv_base, n_seqs, max_path, layout,
+                               paging, scales, workspace, need, stream))

@@ -223,6 +223,15 @@ def test_rows_out_of_range():
         c.check()
 
 
+def test_no_rows():
+    """Sequences without rows, and a call without any."""
+    for sizes in ([0, 3, 0], [0, 0]):
+        c = Case(sizes, 50, 1, True, seed=14)
+        path, count, after, flag = c.call(4)
+        assert (count[np.array(sizes) == 0] == 0).all() and (after[np.array(sizes) == 0] == -1).all() and flag == 0
+        assert (path[np.array(sizes) == 0] == -1).all()
+
+
 def test_nothing_is_written_elsewhere():
     c = Case([4, 3], 100, 1, True, seed=12)
     need = pkv.pkv_tree_verify_workspace_size(pkv.make_verify_desc(c.target, c.draft, T.as_tensor(c.cu), 2, 4, 3))
