@@ -159,3 +159,42 @@ def test_captured_step(quant):
         for a, b in zip(g.state(), e.state()):
             assert same(a, b), i
     assert g.kv_len.tolist() == e.kv_len.tolist() and min(g.kv_len.tolist()) >= 8
+
+
+def test_steps_of_two_servers_at_once():
+    """Two captured steps, replayed on streams of their own at the same time, and an eager one on a third."""
+    servers = [Server(q, seed) for q, seed in ((False, 4), (True, 5), (False, 6))]
+    alone = [Server(q, seed) for q, seed in ((False, 4), (True, 5), (False, 6))]
+    warm = Server(False)
+    warm.draw(np.random.default_rng(3))
+    warm.step()
+    torch.cuda.synchronize()
+    graphs = [torch.cuda.CUDAGraph() for _ in "ab"]
+    for graph, x in zip(graphs, servers):
+        with torch.cuda.graph(graph):
+            x.step()
+    streams = [torch.cuda.Stream() for _ in "abc"]
+    for i in range(4):
+        for s, a, seed in zip(servers, alone, range(10 * i, 10 * i + 3)):
+            s.draw(np.random.default_rng(seed))
+            a.draw(np.random.default_rng(seed))
+        torch.cuda.synchronize()
+        for st, run in zip(streams, [g.replay for g in graphs] + [servers[2].step]):
+            with torch.cuda.stream(st):
+                run()
+        torch.cuda.synchronize()
+        for s, a in zip(servers, alone):
+            a.step()
+            torch.cuda.synchronize()
+            for x, y in zip(s.state(), a.state()):
+                assert same(x, y), i
+
+
+def test_the_same_sequence_twice():
+    """Two trees over one stretch of a cache (two drafts of one context) attend as each alone, also when a row bound is high."""
+    c = Case("bf16", [300, 300], [7, 7], seed=30)
+    c.base[1] = c.base[0]
+    out, lse = c.call(c.masks())
+    c.check(out, lse)
+    out, lse = c.call(c.masks(), max_q=32, max_kv=5000)
+    c.check(out, lse)
