@@ -23,7 +23,7 @@ namespace pkv {
 namespace {
 
 constexpr int kJoinWaves = 4;
-constexpr int64_t kTileRows = 64, kTileTotal = 24576;
+constexpr int64_t kTileRows = 64;
 constexpr int kJoinKeys = 2;
 
 // Eight values as they lie in memory, and as floats.
@@ -557,9 +557,14 @@ __global__ __launch_bounds__(256, 2) void tree_join_tiles(AttnArgs a, DraftArgs 
 // of 24 over 200..500 36 / 33, over 2000..5000 103 / 103; 8 of 96 over 2000..5000 82 / 82; 48
 // of 24 over 200..500 57 / 45; 48 of 96 over 50 148 / 97, over 2000 325 / 273; as chains,
 // whose rows see many drafted rows, 8 of 96 over 1000 73 / 47, 48 of 96 over 50 262 / 89).
+// Few workgroups do where a row has one record (28 heads over 4 KV heads of 128: chains of
+// 93 rows of 4 sequences over 21..37 keys 33.5 / 24.0, of 29 rows of 18 over 1 key 29.1 / 21.9,
+// trees of 49 rows of 11 over 7..11 keys 19.9 / 22.0; with more records, 47 rows of 9
+// over 76..247 keys 19.4 / 29.6).
 bool tile_route(const AttnArgs& a) {
-    const int64_t rows = (int64_t)a.max_q * (a.n_heads / a.n_kv_heads);
-    return a.variant == 0 && a.dtype != 1 && a.n_splits <= 16 && rows >= kTileRows && rows * a.n_kv_heads * a.n_layers * a.n_seqs >= kTileTotal;
+    if (a.variant == 1 || a.dtype == 1 || a.n_splits > 16) return false;
+    const int64_t rows = (int64_t)a.max_q * (a.n_heads / a.n_kv_heads), total = rows * a.n_kv_heads * a.n_layers * a.n_seqs;
+    return rows >= kTileRows && total >= (a.n_splits > 1 ? 24576 : 8192);
 }
 
 template <int D>
