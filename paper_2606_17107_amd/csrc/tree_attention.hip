@@ -25,7 +25,6 @@ namespace pkv {
 namespace {
 
 constexpr int kJoinWaves = 4;
-constexpr int64_t kTileRows = 64;
 constexpr int kJoinKeys = 2;
 
 // Eight values as they lie in memory, and as floats.
@@ -559,14 +558,16 @@ __global__ __launch_bounds__(256, 2) void tree_join_tiles(AttnArgs a, DraftArgs 
 // of 24 over 200..500 36 / 33, over 2000..5000 103 / 103; 8 of 96 over 2000..5000 82 / 82; 48
 // of 24 over 200..500 57 / 45; 48 of 96 over 50 148 / 97, over 2000 325 / 273; as chains,
 // whose rows see many drafted rows, 8 of 96 over 1000 73 / 47, 48 of 96 over 50 262 / 89).
-// Few workgroups do where a row has one record (28 heads over 4 KV heads of 128: chains of
+// Less will do where a row has one record (28 heads over 4 KV heads of 128: chains of
 // 93 rows of 4 sequences over 21..37 keys 33.5 / 24.0, of 29 rows of 18 over 1 key 29.1 / 21.9,
-// trees of 49 rows of 11 over 7..11 keys 19.9 / 22.0; with more records, 47 rows of 9
-// over 76..247 keys 19.4 / 29.6).
+// trees of 49 rows of 11 over 7..11 keys 19.9 / 22.0; 9 of 24 over 0..3, two layers, 21.8 / 18.0; 8
+// heads of 8: 27 of 43 over 5..17, two layers, 26.8 / 31.0, 48 of 23 over 4..13 25.5 / 22.7; with
+// more records, 47 rows of 9 over 76..247 keys 19.4 / 29.6), down to 8192 rows (46 of 4, 32
+// heads over 8, 5888 rows 18.0 / 21.9).
 bool tile_route(const AttnArgs& a) {
     if (a.variant == 1 || a.dtype == 1 || a.n_splits > 16) return false;
     const int64_t rows = (int64_t)a.max_q * (a.n_heads / a.n_kv_heads), total = rows * a.n_kv_heads * a.n_layers * a.n_seqs;
-    return rows >= kTileRows && total >= (a.n_splits > 1 ? 24576 : 8192);
+    return a.n_splits > 1 ? rows >= 64 && total >= 24576 : rows >= 16 && total >= 8192;
 }
 
 template <int D>

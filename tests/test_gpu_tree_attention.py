@@ -397,6 +397,18 @@ def test_wide_rows_of_more_than_a_tile():
         assert np.isneginf(lse.cpu().numpy()[0, 7]).all()
 
 
+@pytest.mark.parametrize("most", [0, 40])
+@pytest.mark.parametrize("kind", ["bf16", "paged", "quant"])
+def test_wide_of_few_rows(kind, most):
+    """Many small trees whose rows have one record, or none."""
+    rng = np.random.default_rng(31)
+    for d in (64, 128):
+        c = Case(kind, rng.integers(0, most + 1, 60), np.r_[9, rng.integers(1, 10, 59)], G=4, Hkv=4, d=d, seed=31 + d)
+        assert 60 * 9 * c.H >= 8192
+        out, lse = c.call(c.masks())
+        c.check(out, lse, max_abs=0.047)
+
+
 @pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
 def test_wide_nonfinite_rows(bad):
     """In the join in tiles a value that is no finite number is left out of the tile and reaches the rows that see it,
