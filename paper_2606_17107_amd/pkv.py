@@ -232,15 +232,27 @@ def _ptr(t) -> Optional[int]:
     return t.data_ptr()
 
 
-def _keep_until_done(t: Optional[torch.Tensor], stream) -> None:
-    """A workspace allocated here is freed when the call returns; when the kernels run on a stream other
-    than torch's current one, tell the caching allocator that stream still uses it."""
-    if t is None or stream is None:
-        return
+def _on_stream(make, device: torch.device, stream, returned: bool = False) -> torch.Tensor:
+    """A tensor that a call on `stream` needs, made (and filled, if `make` fills) on that stream: what torch's current
+    stream still does with the memory is behind it, and the call's kernels are behind a fill.  The caching allocator
+    hands a block back to the stream it was made on, so scratch memory may go when the call returns; one that is
+    returned may also be read on the current stream, and is kept until that is done."""
+    if stream is None:
+        return make()
     if isinstance(stream, int):
-        stream = torch.cuda.ExternalStream(stream)
-    if stream != torch.cuda.current_stream(t.device):
-        t.record_stream(stream)
+        stream = torch.cuda.ExternalStream(stream, device=device)
+    current = torch.cuda.current_stream(device)
+    if stream.cuda_stream == current.cuda_stream:
+        return make()
+    with torch.cuda.stream(stream):
+        t = make()
+    if returned:
+        t.record_stream(current)
+    return t
+
+
+def _scratch(nbytes: int, device: torch.device, stream) -> torch.Tensor:
+    return _on_stream(lambda: torch.empty(nbytes, dtype=torch.uint8, device=device), device, stream)
 
 
 # torch's raw accessors of the current stream and device; private, so a torch
@@ -584,8 +596,7 @@ def suffix_attention(q, k_cache, v_cache, out, q_pos, kv_len, scale, max_kv_len,
                           n_splits, lse_out, window)
     need = pkv_attention_workspace_size(desc, H, Hkv, D)
     if need and (workspace is None or workspace.numel() * workspace.element_size() < need):
-        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
-        _keep_until_done(workspace, stream)
+        workspace = _scratch(need, q.device, stream)
     _check(pkv_suffix_attention(q, k_cache, v_cache, out, q_pos, kv_len, H, Hkv, D, scale, desc,
                                 workspace, need, stream))
 
@@ -669,8 +680,7 @@ def suffix_attention_paged(q, k_pool, v_pool, out, q_pos, kv_len, block_table, s
     pg = make_paging(block_table, k_pool, v_pool, v_block_table)
     need = pkv_attention_workspace_size(d, H, Hkv, D)
     if need and (workspace is None or workspace.numel() * workspace.element_size() < need):
-        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
-        _keep_until_done(workspace, stream)
+        workspace = _scratch(need, q.device, stream)
     _check(pkv_suffix_attention_paged(q, k_pool, v_pool, out, q_pos, kv_len, H, Hkv, D, scale, d, pg, workspace,
                                       need, stream))
 
@@ -810,8 +820,7 @@ def suffix_attention_quant(q, k_pool, v_pool, k_scale, v_scale, out, q_pos, kv_l
                              window, cache_slots)
     need = pkv_attention_quant_workspace_size(desc, H, Hkv, D)
     if need and (workspace is None or workspace.numel() * workspace.element_size() < need):
-        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
-        _keep_until_done(workspace, stream)
+        workspace = _scratch(need, dev, stream)
     _check(pkv_suffix_attention_quant(q, k_pool, v_pool, out, q_pos, kv_len, H, Hkv, D, scale, desc,
                                    make_paging(block_table, k_pool, v_pool, v_block_table),
                                    make_block_scales(k_scale, v_scale, k_pool.shape[2]), workspace, need, stream))
@@ -868,8 +877,7 @@ def _pages_workspace(pool, n_forks, workspace, dev, stream):
     need = pkv_pages_workspace_size(pool, n_forks)
     _need(workspace, "workspace", dev, contiguous=True)
     if workspace is None or workspace.numel() * workspace.element_size() < need:
-        workspace = torch.empty(max(16, need), dtype=torch.uint8, device=dev)
-        _keep_until_done(workspace, stream)
+        workspace = _scratch(max(16, need), dev, stream)
     return workspace, workspace.numel() * workspace.element_size()
 
 
@@ -910,8 +918,7 @@ def pages_compact(tensors, ref, block_table, page_size, ref_out=None, block_tabl
     if out.shape != block_table.shape:
         raise ValueError("block_table and block_table_out have different shapes")
     if n_used is None:
-        n_used = torch.empty(1, dtype=torch.int32, device=dev)
-        _keep_until_done(n_used, stream)
+        n_used = _on_stream(lambda: torch.empty(1, dtype=torch.int32, device=dev), dev, stream, returned=True)
     _need(n_used, "n_used", dev, torch.int32, 1)
     pool = make_page_pool(tensors, block_table, page_size, err_flag)
     workspace, size = _pages_workspace(pool, 0, workspace, dev, stream)
@@ -954,11 +961,10 @@ def tree_masks(parent, kv_len, n_seqs=1, cu_q=None, max_q=None, mask=None, q_pos
     _need(err_flag, "err_flag", dev, torch.int32, 1)
     most = _most_rows(rows, max_q)
     if mask is None:
-        mask = torch.zeros(rows, max(1, -(-most // 32)), dtype=torch.int32, device=dev)
-        _keep_until_done(mask, stream)
+        words = max(1, -(-most // 32))
+        mask = _on_stream(lambda: torch.zeros(rows, words, dtype=torch.int32, device=dev), dev, stream, returned=True)
     if q_pos is None:
-        q_pos = torch.zeros(rows, dtype=torch.int32, device=dev)
-        _keep_until_done(q_pos, stream)
+        q_pos = _on_stream(lambda: torch.zeros(rows, dtype=torch.int32, device=dev), dev, stream, returned=True)
     _check_mask(mask, dev, rows, most)
     if rows == 0:   # (an empty tensor has no address to pass down)
         return mask, q_pos
@@ -1041,8 +1047,7 @@ def tree_attention(q, k_cache, v_cache, draft_k, draft_v, out, q_pos, kv_len, sc
                           block_table, cache_slots)
     need = pkv_tree_attention_workspace_size(desc, H, Hkv, D, quant)
     if need and (workspace is None or workspace.numel() * workspace.element_size() < need):
-        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
-        _keep_until_done(workspace, stream)
+        workspace = _scratch(need, dev, stream)
     paging = None if block_table is None else make_paging(block_table, k_cache, v_cache, v_block_table)
     scales = make_block_scales(k_scale, v_scale, k_cache.shape[2]) if quant else None
     with torch.cuda.device(dev):
@@ -1083,8 +1088,7 @@ def tree_verify(target_probs, tokens, parent, u_accept, u_sample, max_path, draf
     for t, name, shape in ((path, "path", (int(n_seqs), int(max_path))), (n_accepted, "n_accepted", (int(n_seqs),)),
                            (next_token, "next_token", (int(n_seqs),))):
         if t is None:
-            t = torch.empty(shape, dtype=torch.int32, device=dev)
-            _keep_until_done(t, stream)
+            t = _on_stream(lambda: torch.empty(shape, dtype=torch.int32, device=dev), dev, stream, returned=True)
         _need(t, name, dev, torch.int32, contiguous=True)
         if tuple(t.shape) != shape:
             raise ValueError("%s must be %s, got %s" % (name, shape, tuple(t.shape)))
@@ -1092,8 +1096,7 @@ def tree_verify(target_probs, tokens, parent, u_accept, u_sample, max_path, draf
     desc = make_verify_desc(target_probs, draft_probs, cu_q, n_seqs, _most_rows(rows, max_q), max_path, err_flag)
     need = pkv_tree_verify_workspace_size(desc)
     if workspace is None or workspace.numel() * workspace.element_size() < need:
-        workspace = torch.empty(max(16, need), dtype=torch.uint8, device=dev)
-        _keep_until_done(workspace, stream)
+        workspace = _scratch(max(16, need), dev, stream)
     with torch.cuda.device(dev):
         _check(pkv_tree_verify(target_probs, draft_probs, tokens, parent, u_accept, u_sample, *outs, desc, workspace,
                                workspace.numel() * workspace.element_size(), stream))
@@ -1160,8 +1163,7 @@ def tree_commit(draft_k, draft_v, cache_k, cache_v, path, n_accepted, kv_len, kv
     layout = make_commit_layout(draft_k, draft_v, cache_k, cache_v, block_table, slots, err_flag)
     need = pkv_tree_commit_workspace_size(n_seqs, max_path, quant)
     if need and (workspace is None or workspace.numel() * workspace.element_size() < need):
-        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
-        _keep_until_done(workspace, stream)
+        workspace = _scratch(need, dev, stream)
     paging = None if block_table is None else make_paging(block_table, cache_k, cache_v, v_block_table)
     scales = make_block_scales(k_scale, v_scale, cache_k.shape[2]) if quant else None
     with torch.cuda.device(dev):
