@@ -945,6 +945,21 @@ def _check_mask(mask, dev, rows: int, max_q: int) -> None:
         raise ValueError("mask %s must be [total_q][mask_words] for %d rows of %d bits" % (tuple(mask.shape), rows, max_q))
 
 
+def _check_values(k_cache, v_cache, block_table, v_block_table, slots: Optional[int]) -> None:
+    """The library takes its bounds (slots, or pages and their size) from the key cache: the values have at least as many, and
+    `slots` of a contiguous cache lie in it."""
+    if block_table is None:
+        if slots is not None and int(slots) > k_cache.shape[2]:
+            raise ValueError("%d slots, the caches have %d" % (int(slots), k_cache.shape[2]))
+        if v_cache is not None and v_cache.shape[2] < k_cache.shape[2]:
+            raise ValueError("the value cache has %d slots, the key cache %d" % (v_cache.shape[2], k_cache.shape[2]))
+        return
+    if v_cache is not None and (v_cache.shape[1] < k_cache.shape[1] or v_cache.shape[2] != k_cache.shape[2]):
+        raise ValueError("the value pool has %d pages of %d slots, the key pool %d of %d" % (*v_cache.shape[1:3], *k_cache.shape[1:3]))
+    if v_block_table is not None and v_block_table.shape != block_table.shape:
+        raise ValueError("block_table and v_block_table have different shapes")
+
+
 def _most_rows(rows: int, max_q: Optional[int]) -> int:
     return rows if max_q is None else int(max_q)
 
@@ -1041,6 +1056,9 @@ def tree_attention(q, k_cache, v_cache, draft_k, draft_v, out, q_pos, kv_len, sc
             raise ValueError("%s_cache %s does not fit q %s" % (name, tuple(cache.shape), tuple(q.shape)))
         if draft.dim() != 4 or (draft.shape[0], draft.shape[1], draft.shape[3]) != (L, Hkv, width) or draft.shape[2] < rows:
             raise ValueError("draft_%s %s must be [%d][%d][%d][%d]" % (name, tuple(draft.shape), L, Hkv, rows, width))
+    if v_cache.shape[1 if block_table is None else 3] != Hkv:
+        raise ValueError("k_cache %s and v_cache %s have different heads" % (tuple(k_cache.shape), tuple(v_cache.shape)))
+    _check_values(k_cache, v_cache, block_table, v_block_table, cache_slots)
     if rows == 0:   # (an empty tensor has no address to pass down)
         return
     desc = make_tree_desc(q, k_cache, v_cache, out, max_kv_len, n_seqs, cu_q, max_q, variant, n_splits, lse_out, window, kv_base,
@@ -1158,6 +1176,7 @@ def tree_commit(draft_k, draft_v, cache_k, cache_v, path, n_accepted, kv_len, kv
         if draft.dim() != 4 or cache.dim() != dim or draft.shape[:2] != draft_k.shape[:2] or draft.shape[2] != draft_k.shape[2] \
                 or (draft.shape[0], draft.shape[1], draft.shape[3]) != (cache.shape[0], cache.shape[heads], cache.shape[-1]):
             raise ValueError("draft_%s %s does not fit cache_%s %s" % (name, tuple(draft.shape), name, tuple(cache.shape)))
+    _check_values(cache_k, cache_v, block_table, v_block_table, slots)
     if slots is None:
         slots = cache_k.shape[2] if block_table is None else 0
     layout = make_commit_layout(draft_k, draft_v, cache_k, cache_v, block_table, slots, err_flag)
