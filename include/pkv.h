@@ -575,7 +575,8 @@ size_t pkv_tree_attention_workspace_size(const pkv_attn_desc* desc, int32_t n_q_
  * change; it depends on nothing else outside the sequence.  A row that sees nothing is zeros
  * (lse_out -inf).  What a row does not see does not reach it,
  * NaN and infinities included; a visible drafted row whose score is -inf weighs nothing,
- * whatever its values.
+ * whatever its values.  A value of a visible drafted row that is NaN or infinite, at any other
+ * score, makes its channel of the output NaN or infinite, also where the weight vanishes.
  * Errors: as pkv_suffix_attention, _paged and _quant; PKV_ERR_NULL (draft, its k or v; scales
  * without paging), PKV_ERR_SHAPE and PKV_ERR_ALIGN (its fields), PKV_ERR_ALIAS (out overlaps
  * it too). */

@@ -348,6 +348,9 @@ __global__ __launch_bounds__(kJoinWaves * 64) void tree_join(AttnArgs a, DraftAr
     if (a.lse_out && lane == 0) a.lse_out[item] = row_lse2(m, l) * kLn2;
 }
 
+// The weight in a tile of a drafted row that is not seen, or whose score is -inf (of others: +0 or more).
+constexpr float kUnseen = -0.f;
+
 // The same for many rows of bf16 heads: a workgroup takes 128 (row, head-in-group) rows
 // of one KV head, 32 a wave, and the drafted rows 32 at a time through LDS and the
 // matrix cores, in the layouts of the many-row attention kernels (S^T = K Q^T, then
@@ -355,7 +358,8 @@ __global__ __launch_bounds__(kJoinWaves * 64) void tree_join(AttnArgs a, DraftAr
 // rows of a head cost about 0.7 us, most of it instructions; here keys, values and masks are
 // read once for 128 rows.
 // A value that is no finite number is left out of the tile (0 * inf would reach rows
-// that do not see it) and added by hand to the rows that do.
+// that do not see it) and added by hand to the rows that do, also where the weight of a
+// row that sees it vanishes (NaN then, as above).
 template <int D>
 __global__ __launch_bounds__(256, 2) void tree_join_tiles(AttnArgs a, DraftArgs d, int seq0) {
     constexpr int BN = 32, KS = D / 16, DB = D / 32, CH = D / 8;
@@ -498,7 +502,7 @@ __global__ __launch_bounds__(256, 2) void tree_join_tiles(AttnArgs a, DraftArgs 
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const int r = h * 8 + e;
-                s[r] = s[r] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s[r] - m_new);
+                s[r] = s[r] == -INFINITY ? kUnseen : __builtin_amdgcn_exp2f(s[r] - m_new);
                 p[e] = s[r];
             }
             pb[h] = __builtin_convertvector(p, bf16x8);
@@ -523,6 +527,7 @@ __global__ __launch_bounds__(256, 2) void tree_join_tiles(AttnArgs a, DraftArgs 
             for (int r = 0; r < 16; ++r) mine = r == (key >> 3) * 4 + (key & 3) ? s[r] : mine;
             const float other = __shfl_xor(mine, 32);
             const float p = hl == ((key >> 2) & 1) ? mine : other;
+            const bool weighs = __float_as_uint(p) != __float_as_uint(kUnseen);
             const uint16_t* const v = v0 + (int64_t)(t * BN + key) * d.v_stride[2] + hl * 4;
 #pragma unroll
             for (int db = 0; db < DB; ++db)
@@ -531,7 +536,7 @@ __global__ __launch_bounds__(256, 2) void tree_join_tiles(AttnArgs a, DraftArgs 
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const float z = load1(v + db * 32 + b * 8 + e);
-                        if (p != 0.f && !(fabsf(z) < INFINITY)) o[db][4 * b + e] += p * z;
+                        if (weighs && !(fabsf(z) < INFINITY)) o[db][4 * b + e] += p * z;
                     }
         }
     }
