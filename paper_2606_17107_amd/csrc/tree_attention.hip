@@ -557,6 +557,9 @@ __global__ __launch_bounds__(256, 2) void tree_join_tiles(AttnArgs a, DraftArgs 
     if (a.lse_out && hl == 0) a.lse_out[item] = row_lse2(mx, l_tot) * kLn2;
 }
 
+// Layers and KV heads share a grid dimension in tiles; a wave a row and head needs it for the layers alone.
+constexpr int64_t kMaxGridZ = 65535;
+
 // Tiles pay where they fill, and where there are enough workgroups to hide that each of
 // them waits for one record after another (a wave a row and head / tiles, us a call, 32
 // heads over 8 KV heads of 128; 16 sequences of 32 rows over 2000..9000 keys 109 / 115; 24
@@ -571,6 +574,7 @@ __global__ __launch_bounds__(256, 2) void tree_join_tiles(AttnArgs a, DraftArgs 
 // heads over 8, 5888 rows 18.0 / 21.9).
 bool tile_route(const AttnArgs& a) {
     if (a.variant == 1 || a.dtype == 1 || a.n_splits > 16) return false;
+    if ((int64_t)a.n_layers * a.n_kv_heads > kMaxGridZ) return false;
     const int64_t rows = (int64_t)a.max_q * (a.n_heads / a.n_kv_heads), total = rows * a.n_kv_heads * a.n_layers * a.n_seqs;
     return a.n_splits > 1 ? rows >= 64 && total >= 24576 : rows >= 16 && total >= 8192;
 }
@@ -578,7 +582,7 @@ bool tile_route(const AttnArgs& a) {
 template <int D>
 hipError_t launch_tiles(const AttnArgs& a, const DraftArgs& d, hipStream_t stream) {
     const int64_t rows = (int64_t)a.max_q * (a.n_heads / a.n_kv_heads), z = (int64_t)a.n_layers * a.n_kv_heads;
-    if (rows > 0x7fffffff || z > 65535) return hipErrorInvalidValue;
+    if (rows > 0x7fffffff || z > kMaxGridZ) return hipErrorInvalidValue;
     for (int seq0 = 0; seq0 < a.n_seqs; seq0 += 65535) {
         const int n = a.n_seqs - seq0 < 65535 ? a.n_seqs - seq0 : 65535;
         hipLaunchKernelGGL((tree_join_tiles<D>), dim3((unsigned)((rows + 127) / 128), (unsigned)n, (unsigned)z), dim3(256), 0, stream, a, d, seq0);
@@ -591,7 +595,7 @@ hipError_t launch_tiles(const AttnArgs& a, const DraftArgs& d, hipStream_t strea
 template <typename T, int D>
 hipError_t launch_d(const AttnArgs& a, const DraftArgs& d, hipStream_t stream) {
     const int64_t units = (int64_t)a.max_q * a.n_heads;
-    if (units > 0x7fffffff || a.n_layers > 65535) return hipErrorInvalidValue;
+    if (units > 0x7fffffff || a.n_layers > kMaxGridZ) return hipErrorInvalidValue;
     for (int seq0 = 0; seq0 < a.n_seqs; seq0 += 65535) {
         const int n = a.n_seqs - seq0 < 65535 ? a.n_seqs - seq0 : 65535;
         hipLaunchKernelGGL((tree_join<T, D>), dim3((unsigned)((units + kJoinWaves - 1) / kJoinWaves), (unsigned)n, (unsigned)a.n_layers),
