@@ -736,7 +736,8 @@ pkv_status splice_quant(const void* src_k, const void* src_v, void* k_pages, voi
     for (int i = 0; i < 6; ++i)   // (the two sources may be one tensor)
         for (int j = i < 2 ? 2 : i + 1; j < 6; ++j)
             if (overlap(r[i], r[j])) return fail(PKV_ERR_ALIAS, "sources, pools and scales must not overlap");
-    if (n_segs == 0 || max_seg_tokens == 0 || L->dst_capacity == 0) return ok();
+    // (accepted rows for a cache without slots are flagged by the kernel)
+    if (n_segs == 0 || max_seg_tokens == 0 || (L->dst_capacity == 0 && !accepted)) return ok();
     a.src_k = (const char*)src_k;
     a.src_v = (const char*)src_v;
     a.dst_k = (uint8_t*)k_pages;
@@ -1100,7 +1101,6 @@ PKV_EXPORT pkv_status pkv_tree_commit(const void* draft_k, const void* draft_v, 
     const pkv_status st = check_splice(draft_k, draft_v, cache_k, cache_v, 1.0f, 2 * (at.dtype == PKV_F32 ? 4 : 8), &at, false, a,
                                        paging);
     if (st != PKV_OK) return st;
-    if (a.n_tokens == 0 || a.dst_capacity == 0) return ok();
     t.src[0] = a.src_k;
     t.src[1] = a.src_v;
     t.dst[0] = a.dst_k;
