@@ -646,8 +646,8 @@ size_t pkv_tree_commit_workspace_size(int32_t n_seqs, int32_t max_path, int32_t 
  * sequence; the destination strides those of the cache (bytes with scales); v_dim 0 without values;
  * rope_offset and rope_style are not used.  kv_base: device int64 [n_seqs], as in
  * pkv_attn_desc (contiguous caches only).  A row, slot or page entry out of range is skipped (and
- * *layout->err_flag set); with n_tokens or dst_capacity 0 that is every accepted one.  Different
- * sequences must not write the same slot.
+ * *layout->err_flag set); with n_tokens or dst_capacity 0 that is every accepted one (with n_tokens 0
+ * draft_k and draft_v may be NULL).  Different sequences must not write the same slot.
  * Errors: as pkv_reposition_splice, _paged and _quant; PKV_ERR_SHAPE (kv_base with paging),
  * PKV_ERR_UNSUPPORTED (max_path above 65535, with scales also n_seqs). */
 pkv_status pkv_tree_commit(const void* draft_k, const void* draft_v, void* cache_k, void* cache_v, const int32_t* path,

@@ -1094,6 +1094,12 @@ PKV_EXPORT pkv_status pkv_tree_commit(const void* draft_k, const void* draft_v, 
     pkv_layout at = *L;
     at.rope_offset = 0;
     at.rope_style = PKV_ROPE_HALF;
+    if (L->n_tokens == 0) {   // no drafted rows, and so no tensors of them: whatever is accepted is flagged
+        static const char none[16] __attribute__((aligned(16))) = {0};   // (never read)
+        if (!draft_k) draft_k = none;
+        if (!draft_v && L->v_dim > 0) draft_v = none;
+        for (int i = 0; i < 3; ++i) at.src_k_stride[i] = at.src_v_stride[i] = 0;
+    }
     if (scales)
         return splice_quant(draft_k, draft_v, cache_k, cache_v, nullptr, n_seqs, max_path, kv_len, n_seqs, nullptr, 1.0f, 16, &at,
                             paging, scales, &t, stream);

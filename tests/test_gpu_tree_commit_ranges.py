@@ -43,3 +43,22 @@ def test_nothing_to_take_or_to_fill(kind, accepted, field):
                                scales, None, 0) == pkv.PKV_OK
     torch.cuda.synchronize()
     assert unchanged(c, before) and int(f) == int(accepted)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("values", [True, False])
+@pytest.mark.parametrize("accepted", [True, False])
+def test_no_drafted_rows(kind, values, accepted):
+    """A step in which no sequence has rows, whose tensors have no address; a path that names rows all the same is flagged."""
+    c = Case(kind, [10, 20], [3, 2], values=values, seed=30)
+    before = [t.clone() for t in tensors(c)]
+    c.dk = c.dk[:, :, :0]
+    c.dv = c.dv[:, :, :0] if values else None
+    f = flag()
+    c.call(f, counts=None if accepted else np.zeros(2, np.int32))
+    assert unchanged(c, before) and int(f) == int(accepted)
+    c.dk = torch.empty_like(c.dk)
+    c.dv = torch.empty_like(c.dv) if values else None
+    assert c.dk.data_ptr() == 0
+    c.call(f.zero_(), counts=None if accepted else np.zeros(2, np.int32))
+    assert unchanged(c, before) and int(f) == int(accepted)

@@ -110,3 +110,19 @@ def test_pools_of_codes(call, stand_ins):
         call(pool(9, 32, kind="quant"), pool(8, 32, kind="quant"), block_table=TABLE, k_scale=scale, v_scale=scale[:, :8])
     call(pool(9, 32, kind="quant"), pool(9, 32, kind="quant"), block_table=TABLE, k_scale=scale, v_scale=scale)
     assert len(stand_ins) == 1
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="fake device addresses, so only without a GPU")
+@pytest.mark.parametrize("form", [dict(), dict(paged=True), dict(quant=True)])
+@pytest.mark.parametrize("v_dim", [128, 0])
+def test_commit_without_drafted_rows_needs_no_tensors_of_them(form, v_dim, monkeypatch):
+    """Past the checks, to the launch that there is no device for; with rows a missing tensor is refused as ever."""
+    from test_tree_abi import commit_args
+    monkeypatch.undo()
+    values = {} if v_dim else dict(cache_v=None)
+    a = commit_args(**form, draft_k=None, draft_v=None, L__v_dim=v_dim, L__n_tokens=0, **values)
+    if not v_dim and a["scales"] is not None:
+        a["scales"].v_scale = None
+    assert pkv.pkv_tree_commit(**a) == pkv.PKV_ERR_DEVICE
+    a["layout"].n_tokens = 1
+    assert pkv.pkv_tree_commit(**a) == pkv.PKV_ERR_NULL
