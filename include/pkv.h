@@ -285,10 +285,11 @@ size_t pkv_attention_workspace_size(const pkv_attn_desc* desc, int32_t n_q_heads
  * q is post-RoPE (q_pos only masks).  bf16: QK^T and PV on bf16 MFMA with fp32
  * accumulation, softmax statistics in fp32, probabilities rounded to bf16
  * before PV, output rounded to bf16.  fp32: fp32 FMA throughout.  A row with no
- * visible slot is written as zeros.  Calls of few query rows (n_splits = 0) cut the
- * keys at places that follow the cache lengths of all their sequences: a sequence's
- * result may then differ in rounding when another one's length changes; it depends
- * on nothing else outside the sequence.  Rows of out (and lse_out) that no
+ * visible slot is written as zeros.  With n_splits = 0 the keys are cut by the call's
+ * sizes (total_q, with rows that no sequence owns, among them), and in calls of few
+ * query rows at places that follow the cache lengths of all their sequences: a sequence's
+ * result may then differ in rounding when a size or another one's length changes; it
+ * depends on nothing else outside the sequence.  Rows of out (and lse_out) that no
  * sequence owns (outside every [cu_q[s], cu_q[s+1]) range) are not written,
  * whatever the split count.  q_pos: device int32 [total_q]; kv_len:
  * device int32 [n_seqs].  workspace: device memory of at least
@@ -570,13 +571,15 @@ size_t pkv_tree_attention_workspace_size(const pkv_attn_desc* desc, int32_t n_q_
  * cache (bf16 or fp32 GQA, bf16 MLA); else a paged one (bf16); scales with paging: one
  * held in 8 bits (GQA).  Arithmetic as in suffix attention; over the drafted rows scores, sums
  * and products are fp32, save that calls of many bf16 GQA rows round their probabilities to
- * bf16 before the product there too.  How the keys are cut follows n_seqs, max_q, max_kv_len and
- * the cache lengths, so a sequence's result may differ in rounding when those of others
- * change; it depends on nothing else outside the sequence.  A row that sees nothing is zeros
- * (lse_out -inf).  What a row does not see does not reach it,
- * NaN and infinities included; a visible drafted row whose score is -inf weighs nothing,
- * whatever its values.  A value of a visible drafted row that is NaN or infinite, at any other
- * score, makes its channel of the output NaN or infinite, also where the weight vanishes.
+ * bf16 before the product there too.  How the keys are cut, and which calls are of many rows,
+ * follows the call's sizes (n_layers, the heads, n_seqs, total_q with rows that no sequence owns,
+ * max_q, max_kv_len, the window) and the cache lengths, so a sequence's result may differ in rounding
+ * when any of these change; with n_splits given it does not follow total_q or the other lengths.  It
+ * depends on nothing else outside the sequence.  A row that sees nothing is zeros (lse_out -inf).
+ * What a row does not see does not reach it, NaN and infinities included; a visible drafted row
+ * whose score is -inf weighs nothing, whatever its values.  A value of a visible drafted row that is
+ * NaN or infinite, at any other score, makes its channel of the output NaN or infinite, also where
+ * the weight vanishes.
  * Errors: as pkv_suffix_attention, _paged and _quant; PKV_ERR_NULL (draft, its k or v; scales
  * without paging), PKV_ERR_SHAPE and PKV_ERR_ALIGN (its fields), PKV_ERR_ALIAS (out overlaps
  * it too). */
