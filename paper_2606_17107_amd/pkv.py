@@ -1138,7 +1138,8 @@ def make_commit_layout(draft_k: torch.Tensor, draft_v: Optional[torch.Tensor], c
 
 def tree_commit(draft_k, draft_v, cache_k, cache_v, path, n_accepted, kv_len, kv_base=None, block_table=None, v_block_table=None,
                 k_scale=None, v_scale=None, slots=None, err_flag=None, workspace=None, stream=None) -> None:
-    """Tensor-level call of pkv_tree_commit (path int32 [n_seqs][max_path]); values may be None (MLA)."""
+    """Tensor-level call of pkv_tree_commit (path int32 [n_seqs][max_path]); values may be None (MLA).  No workspace is needed:
+    pkv_tree_commit_workspace_size is 0."""
     dev = _gpu_device(draft_k, "draft_k")
     quant = k_scale is not None or v_scale is not None
     _need(path, "path", dev, torch.int32, contiguous=True)
@@ -1180,11 +1181,9 @@ def tree_commit(draft_k, draft_v, cache_k, cache_v, path, n_accepted, kv_len, kv
     if slots is None:
         slots = cache_k.shape[2] if block_table is None else 0
     layout = make_commit_layout(draft_k, draft_v, cache_k, cache_v, block_table, slots, err_flag)
-    need = pkv_tree_commit_workspace_size(n_seqs, max_path, quant)
-    if need and (workspace is None or workspace.numel() * workspace.element_size() < need):
-        workspace = _scratch(need, dev, stream)
     paging = None if block_table is None else make_paging(block_table, cache_k, cache_v, v_block_table)
     scales = make_block_scales(k_scale, v_scale, cache_k.shape[2]) if quant else None
     with torch.cuda.device(dev):
         _check(pkv_tree_commit(draft_k, draft_v, cache_k, cache_v, path, n_accepted, kv_len, kv_base, n_seqs, max_path, layout,
-                               paging, scales, workspace, need, stream))
+                               paging, scales, workspace, 0 if workspace is None else workspace.numel() * workspace.element_size(),
+                               stream))
