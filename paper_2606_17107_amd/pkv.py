@@ -304,15 +304,32 @@ def _gpu_device(t: torch.Tensor, name: str) -> torch.device:
     return t.device
 
 
-def _check_splice_args(src_k, src_v, dst_k, dst_v, src_pos, dst_pos, err_flag, dst_slot=None,
-                       n_tokens: Optional[int] = None) -> None:
+def _room(t, name: str, *least) -> None:
+    """t has at least these sizes: what a call reads or writes lies in it."""
+    if t is not None and (t.dim() != len(least) or any(n < m for n, m in zip(t.shape, least))):
+        raise ValueError("%s %s must be at least %s" % (name, tuple(t.shape), least))
+
+
+def _check_splice_args(src_k, src_v, dst_k, dst_v, src_pos, dst_pos, err_flag, dst_slot=None) -> None:
     dev = _gpu_device(src_k, "src_k")
-    n = src_k.shape[2] if n_tokens is None else n_tokens
+    L, H, n, d = sk = src_k.shape
     for t, name in ((src_v, "src_v"), (dst_k, "dst_k"), (dst_v, "dst_v")):
         _need(t, name, dev, src_k.dtype)
     for t, name in ((src_pos, "src_pos"), (dst_pos, "dst_pos"), (dst_slot, "dst_slot")):
         _need(t, name, dev, torch.int32, n, contiguous=True)
     _need(err_flag, "err_flag", dev, torch.int32, 1)
+    # The library takes the sizes from src_k and the bounds of the destination from dst_k (a pool has 5 dimensions).
+    dv = 0 if src_v is None else src_v.shape[-1]
+    if src_v is not None and src_v.shape != sk:
+        _room(src_v, "src_v", L, H, n, dv)
+    if dst_k is None:
+        return
+    dk = dst_k.shape
+    heads = 3 if len(dk) == 5 else 1
+    if len(dk) < 4 or dk[0] != L or dk[heads] != H or dk[-1] != d or (dst_v is not None and (dv != d or dst_v.shape != dk)):
+        least = (L, *dk[1:3], H) if heads == 3 else (L, H, *dk[2:3])
+        _room(dst_k, "dst_k", *least, d)
+        _room(dst_v, "dst_v", *least, dv)
 
 
 def _check_attention_args(q, k_cache, v_cache, out, q_pos, kv_len, n_seqs, cu_q, kv_base, lse_out,
@@ -322,13 +339,28 @@ def _check_attention_args(q, k_cache, v_cache, out, q_pos, kv_len, n_seqs, cu_q,
         if t is None:
             raise TypeError("%s is required" % name)
         _need(t, name, dev, q.dtype)
-    L, rows, H = q.shape[0], q.shape[1], q.shape[2]
+    L, rows, H, d = shape = q.shape
     _need(q_pos, "q_pos", dev, torch.int32, rows, contiguous=True)
     _need(kv_len, "kv_len", dev, torch.int32, int(n_seqs), contiguous=True)
     _need(cu_q, "cu_q", dev, torch.int32, int(n_seqs) + 1, contiguous=True)
     _need(kv_base, "kv_base", dev, torch.int64, int(n_seqs), contiguous=True)
     _need(lse_out, "lse_out", dev, torch.float32, L * rows * H, contiguous=True)
     _need(workspace, "workspace", dev, contiguous=True)
+    # As above: sizes from q and out, heads and bounds of the cache from k_cache.
+    dv = out.shape[-1]
+    if out.shape != shape:
+        _room(out, "out", L, rows, H, dv)
+    ks = k_cache.shape
+    if ks[0] != L or ks[-1] != d or dv != d or (v_cache is not k_cache and v_cache.shape != ks):
+        _room(k_cache, "k_cache", L, *ks[1:-1], d)
+        _room(v_cache, "v_cache", L, *ks[1:-1], dv)
+
+
+def _check_tables(block_table, v_block_table, n_seqs: int) -> None:
+    if block_table.dim() != 2 or block_table.shape[0] < n_seqs:
+        raise ValueError("block_table is [n_seqs][max_pages]")
+    if v_block_table is not None and v_block_table.shape != block_table.shape:
+        raise ValueError("block_table and v_block_table have different shapes")
 
 
 # ---- raw C entry points (same names and arguments as pkv.h) -----------------
@@ -638,6 +670,7 @@ def reposition_splice_paged(src_k, src_v, k_pool, v_pool, src_pos, dst_pos, bloc
     _check_splice_args(src_k, src_v, k_pool, v_pool, src_pos, dst_pos, err_flag)
     _need(block_table, "block_table", src_k.device, torch.int32, contiguous=True)
     _need(v_block_table, "v_block_table", src_k.device, torch.int32, contiguous=True)
+    _check_tables(block_table, v_block_table, 1)
     L = make_layout(src_k, src_v, src_k, src_v, rope_offset, rope_style, err_flag=err_flag)
     L.dst_capacity = (block_table.shape[1] * k_pool.shape[2]) if dst_capacity is None else int(dst_capacity)
     L.dst_k_stride = pool_strides3(k_pool)
@@ -654,6 +687,7 @@ def suffix_attention_paged(q, k_pool, v_pool, out, q_pos, kv_len, block_table, s
     _check_attention_args(q, k_pool, v_pool, out, q_pos, kv_len, n_seqs, cu_q, None, lse_out, workspace)
     _need(block_table, "block_table", q.device, torch.int32, contiguous=True)
     _need(v_block_table, "v_block_table", q.device, torch.int32, contiguous=True)
+    _check_tables(block_table, v_block_table, int(n_seqs))
     H = q.shape[2]
     Hkv = k_pool.shape[3]
     D = q.shape[3]
