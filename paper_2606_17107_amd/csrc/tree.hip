@@ -198,8 +198,9 @@ __device__ __forceinline__ double piece_sum(const Weights<T>& r, int piece, cons
 // Sums of all pieces of a row, by NW waves of which this is number `wave`.  A wave has
 // the loads of four whole pieces in flight (4 trees of 32 drawn tokens, 3 children a
 // row, over 100000: 81 us a call; with one piece and the next one's loads 96 us).  A
-// pass of one workgroup is then bound by its conversions to 64 bits, 9 instructions
-// for each pair of probabilities.
+// pass of one workgroup is then held up about alike by its conversions to 64 bits, 9 instructions
+// for each pair of probabilities, and by its loads: VALU instructions issue in 52% of the
+// cycles of the SIMDs that hold its waves, which wait for 41% of theirs.
 template <int NW, bool DRAFT, typename T>
 __device__ __forceinline__ void sum_pieces(const Weights<T>& r, int pieces, int wave, double* sums) {
     constexpr int N = 4;
@@ -628,9 +629,10 @@ constexpr int kCommitThreads = 128;
 // its values, layer by layer; a workgroup has one step of one sequence.  Small calls are
 // a chain (counts, path and lengths; page entry; row), large ones a stream, whose
 // stores go past the caches: 64 sequences of 1..8 rows, 8 layers of 8 heads of 128 in
-// bf16 pages 6.6 us a call (with 256 threads 7.0, with cached stores 7.9, with eight
-// steps a thread, all their loads in flight, 11.3), 32 layers of 4 heads of 128 in fp32
-// 14.8 us (cached stores 19.1), 72 MB read and written.
+// bf16 pages 6.6 us a call replayed from a graph over four caches (6.0 issued one by
+// one; with 256 threads 7.1, with cached stores 7.3, with eight steps a thread, all
+// their loads in flight, 11.3), 32 layers of 4 heads of 128 in fp32 15.9 us (cached
+// stores 19.8), 72 MB read and written.
 __global__ __launch_bounds__(kCommitThreads) void tree_commit(TreeCommitArgs a, int seq0) {
     const int seq = seq0 + (int)blockIdx.z, step = (int)blockIdx.y;
     int64_t row, slot;
